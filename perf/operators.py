@@ -189,27 +189,24 @@ class _Attention:
         if own:
             import paper_2506_06472_amd as tio
             H, dh, rows = c["H"], c["dh"], self.qkv.shape[0]
-            self.packing = tio.tio_packing_build(_offsets(self.lens))
+            self.packing = tio.tio_packing_build(_offsets(self.lens), c["dtype"], H, c["Hkv"], dh)
             self.packed = torch.from_numpy(self.packing.export()["data"]).to(DEV)
             self.o = torch.empty((rows, H * dh), device=DEV, dtype=self.qkv.dtype)
             self.lse = torch.empty((H, rows), device=DEV)
             if c["train"]:
                 self.dqkv = torch.empty_like(self.qkv)
-                need = tio.tio_op_attention_packed_work(self.packing, c["dtype"], H, c["Hkv"], dh)
-                self.work = torch.empty(max(need, 16), device=DEV, dtype=torch.uint8)
+                self.work = torch.empty(tio.tio_op_attention_packed_work(self.packing), device=DEV, dtype=torch.uint8)
 
     def run_own(self, c):
         import paper_2506_06472_amd as tio
-        H, Hkv, dh = c["H"], c["Hkv"], c["dh"]
         stream = torch.cuda.current_stream().cuda_stream
         ld, ldo = self.qkv.stride(0), self.o.stride(0)
-        tio.tio_op_attention_packed(stream, c["dtype"], self.packing, self.packed.data_ptr(), H, Hkv, dh, self.qkv.data_ptr(), ld,
-                                    self.o.data_ptr(), ldo, self.lse.data_ptr())
+        tio.tio_op_attention_packed(stream, self.packing, self.packed.data_ptr(), self.qkv.data_ptr(), ld, self.o.data_ptr(), ldo,
+                                    self.lse.data_ptr())
         if not c["train"]:
             return {"o": self.o, "lse": self.lse}
-        tio.tio_op_attention_packed_bwd(stream, c["dtype"], self.packing, self.packed.data_ptr(), H, Hkv, dh, self.qkv.data_ptr(), ld,
-                                        self.o.data_ptr(), self.do.data_ptr(), ldo, self.lse.data_ptr(), self.work.data_ptr(),
-                                        self.dqkv.data_ptr())
+        tio.tio_op_attention_packed_bwd(stream, self.packing, self.packed.data_ptr(), self.qkv.data_ptr(), ld, self.o.data_ptr(),
+                                        self.do.data_ptr(), ldo, self.lse.data_ptr(), self.work.data_ptr(), self.dqkv.data_ptr())
         return {"o": self.o, "lse": self.lse, "dqkv": self.dqkv}
 
     def run_plain(self, c):
@@ -334,7 +331,7 @@ class _Preference:
             self.seq = torch.empty(2 * pairs, device=DEV)
             self.losses = torch.empty(pairs, device=DEV)
             self.loss = torch.empty(1, device=DEV)
-            self.work = torch.empty(max(tio.tio_op_preference_loss_work(self.packing), 16), device=DEV, dtype=torch.uint8)
+            self.work = torch.empty(tio.tio_op_preference_loss_work(self.packing), device=DEV, dtype=torch.uint8)
             self.dlogits = torch.empty_like(self.logits) if c["train"] else None
 
     def run_own(self, c):

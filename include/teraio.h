@@ -372,6 +372,81 @@ int tio_op_gemm_static_ws(void *stream, int32_t dtype, int32_t a_kmajor, int32_t
  * rowsum(dO * o)) and dqkv [B*T, 3*H*dh], which may lie over o.  Device pointers, 16-byte aligned; dh in {32, 64, 128}. */
 int tio_op_attention(void *stream, int32_t dtype, int64_t B, int64_t T, int64_t H, int64_t dh,
                      const void *qkv, void *o, float *lse, const void *dO, float *delta, void *dqkv);
+
+/* ---- fine-tuning on packed sequences: single operators on caller-provided device buffers ----------------------------
+ * A packed batch is n_seqs sequences of different lengths (zero among them) one behind the other, without padding: sequence s
+ * has rows offsets[s] .. offsets[s+1]-1.  tio_packing_build (pure CPU) checks the host array of n_seqs + 1 offsets (the first 0, never
+ * smaller than the one before) and decides how the batch is cut into workgroups for attention with H query heads in
+ * groups that share one of Hkv key heads (H a multiple of Hkv, at most 64 to a key head; dh 32, 64 or 128; rows * H < 2^31), in
+ * element type dtype.  H = Hkv = dh = 0: without attention (the preference loss needs none).  The caller copies the
+ * view's `data` (`bytes` bytes) to device memory, 16-byte aligned, before the first call that takes it, and passes handle and
+ * copy together; one packing serves all layers of a step, on any stream.  The calls below are asynchronous on `stream`, allocate
+ * nothing, keep nothing between calls, and may be captured into a graph (which then holds this packing).  Rows behind the
+ * last sequence are neither read nor written. */
+typedef struct tio_packing tio_packing;
+typedef struct tio_packing_view {
+    int32_t n_seqs, rows, max_len, reserved;
+    const int32_t *data;             /* begins with the n_seqs + 1 offsets */
+    uint64_t bytes;
+} tio_packing_view;
+int tio_packing_build(const int32_t *offsets, int32_t n_seqs, int32_t dtype, int64_t H, int64_t Hkv, int64_t dh, tio_packing **out);
+int tio_packing_export(const tio_packing *packing, tio_packing_view *out);
+void tio_packing_free(tio_packing *packing);
+
+/* Causal self-attention of every sequence over itself.  qkv: rows of ld_qkv elements that begin with H heads of q, Hkv of k and Hkv
+ * of v, dh elements each; query head h uses key head h / (H / Hkv).  o: rows of ld_o elements that begin with H heads; lse: fp32
+ * [H, rows], the log-sum-exp of the scores scaled by 1/sqrt(dh).  Strides are multiples of 8 elements, device pointers 16-byte
+ * aligned.  A sequence's rows, at the larger stride, must span less than 2 GiB (TIO_ERR_INVALID_ARG otherwise).  What stands between
+ * the heads and the stride is not touched.  Scores of -inf (an infinite component of a key) are probabilities of zero as long as
+ * a row sees another one. */
+int tio_op_attention_packed(void *stream, const tio_packing *packing, const void *packing_dev, const void *qkv, int64_t ld_qkv,
+                            void *o, int64_t ld_o, float *lse);
+/* Gradients of all of q | k | v (dqkv: rows as those of qkv, same stride; its heads only) from dO (rows as those of o), the forward
+ * pass's o and lse, and `work`: device memory of tio_op_attention_packed_work bytes, contents of no interest before and after, used
+ * by one call at a time.  dqkv overlaps none of the other buffers. */
+int tio_op_attention_packed_work(const tio_packing *packing, uint64_t *out_bytes);
+int tio_op_attention_packed_bwd(void *stream, const tio_packing *packing, const void *packing_dev, const void *qkv, int64_t ld_qkv,
+                                const void *o, const void *dO, int64_t ld_o, const float *lse, void *work, void *dqkv);
+
+/* Paired preference loss.  Sequences 2i and 2i+1 of the packing (an even number) are the preferred and the rejected answer of
+ * pair i.  logits: [rows, V] of dtype in rows of ld elements (a multiple of 16 bytes that holds V rounded up to 16 bytes); labels: device
+ * int32 [rows]; a row whose label is outside 0 .. V-1 (a prompt's) does not count.  With lp = the sum over a sequence's counted rows of
+ * logits[label] - log-sum-exp(logits), 0 without one, and ref_logp (device fp32 [n_seqs]) the same of the reference model:
+ *   z = beta ((lp[2i] - ref[2i]) - (lp[2i+1] - ref[2i+1])),  losses[i] = -(1 - smoothing) log sigmoid(z) - smoothing log sigmoid(-z)
+ * and loss[0] = sum of losses / total_pairs.  total_pairs: pairs of the whole batch where it comes in several calls (gradient accumulation
+ * over micro-batches), 0 = the pairs of this one.  seq_logp receives lp (device fp32 [n_seqs]).  dlogits (optional, NULL = loss only): the
+ * gradient of loss[0], in rows like the logits', with zeros in rows that do not count and up to the next multiple of 16 bytes behind
+ * V; it may be the logits' own buffer, and otherwise overlaps none.  beta > 0, 0 <= smoothing <= 1.  work: device memory of
+ * tio_op_preference_loss_work bytes, contents of no interest before and after, used by one call at a time.  16-byte aligned: logits,
+ * dlogits, work and the packing's copy. */
+int tio_op_preference_loss_work(const tio_packing *packing, uint64_t *out_bytes);
+int tio_op_preference_loss(void *stream, int32_t dtype, const tio_packing *packing, const void *packing_dev, int64_t V, const void *logits,
+                           int64_t ld, const int32_t *labels, const float *ref_logp, float beta, float smoothing, int64_t total_pairs,
+                           float *seq_logp, float *losses, float *loss, void *work, void *dlogits);
+
+/* Activations kept in 8 bits between the forward and the backward pass (half the bytes of bf16 to hold, or to move to a slow tier and
+ * back).  Blocks of 32 neighbours of a row share a power of two: with a the block's largest magnitude and e = max(floor(log2 a), -120),
+ * an element x becomes q = clamp(round(x 2^(6-e)), -127, 127), ties to even, and stands for q 2^(e-6).  These values are exact in bf16 and in
+ * fp32; they are at most half a step 2^(e-6) from x (a whole one where the clamp takes part).  A block with an infinity or a NaN
+ * stands for NaNs.  A checkpoint of [rows, cols] is tio_ckpt8_bytes bytes (a multiple of 16; 33 for each block) of one buffer, to be
+ * moved as a whole; its layout is the library's.  Matrices are rows of ld elements, a multiple of 8 and at least cols rounded up to 8;
+ * the padding up to there is not used where a matrix is read, and gets zeros where one is written.  Pointers are 16-byte aligned, buffers
+ * do not overlap, rows * cols (rounded up to 32) stays below 2^34. */
+enum { TIO_ACT_GELU = 0, TIO_ACT_SWIGLU = 1 };
+int tio_ckpt8_bytes(int64_t rows, int64_t cols, uint64_t *out_bytes);
+int tio_op_ckpt8_store(void *stream, int32_t dtype, int64_t rows, int64_t cols, const void *x, int64_t ldx, void *ckpt);
+/* The values that a checkpoint stands for, for the products and gradients of the backward pass. */
+int tio_op_ckpt8_load(void *stream, int32_t dtype, int64_t rows, int64_t cols, const void *ckpt, void *x, int64_t ldx);
+/* An activation of the MLP and the checkpoint of its input, in one pass: y = gelu(gate) (tanh form; up = NULL), or silu(gate) * up, of the
+ * inputs as they are, and the inputs in ckpt: for GELU a checkpoint of [rows, f], for SwiGLU the gate half's and behind it the up
+ * half's (each of tio_ckpt8_bytes(rows, f)).  gate, up and their gradients have stride ldu (the halves of one matrix, or two). */
+int tio_op_act_ckpt8(void *stream, int32_t dtype, int32_t act, int64_t rows, int64_t f, const void *gate, const void *up, int64_t ldu,
+                     void *y, int64_t ldy, void *ckpt);
+/* Its backward pass from the checkpoint: the gradients of gate (and up; NULL for GELU) at the values the checkpoint stands for, and, where
+ * y is given, the activation's output at those values, which the weight gradient of the next layer needs. */
+int tio_op_act_ckpt8_bwd(void *stream, int32_t dtype, int32_t act, int64_t rows, int64_t f, const void *ckpt, const void *dy,
+                         int64_t lddy, void *dgate, void *dup, int64_t ldu, void *y, int64_t ldy);
+
 /* Measuring aid: launch number kernel_index of the schedule, repeated reps times on the compute stream with the
  * uncapped layout (the arena must hold it) and whatever the arena contains, HIP events around the repetitions;
  * returns average ns per launch.  It overwrites that launch's outputs, and a launch that updates its operands in place

@@ -15,6 +15,7 @@ LIB_PATH = os.path.join(_HERE, "libteraio.so")
 
 ARCH = {"gpt": 0, "llama": 1}
 PREC = {"fp32": 0, "bf16": 1}
+ACT = {"gelu": 0, "swiglu": 1}
 PROFILE_MEASURED, PROFILE_MODELLED, PROFILE_OFFLOADED = 0, 1, 2
 OFFLOAD, PREFETCH = 0, 1
 
@@ -93,6 +94,11 @@ class StepStats(C.Structure):
                 ("h2d_busy_ns", C.c_int64), ("n_kernels", C.c_int32), ("n_migrations", C.c_int32)]
 
 
+class PackingView(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_seqs", "rows", "max_len", "reserved")] + \
+               [("data", C.POINTER(C.c_int32)), ("bytes", C.c_uint64)]
+
+
 _lib = None
 
 
@@ -107,7 +113,7 @@ def lib():
         _lib = C.CDLL(LIB_PATH)
         _lib.tio_last_error.restype = C.c_char_p
         _lib.tio_version.restype = C.c_char_p
-        for name in ("tio_trace_free", "tio_lifetimes_free", "tio_plan_free"):
+        for name in ("tio_trace_free", "tio_lifetimes_free", "tio_plan_free", "tio_packing_free"):
             getattr(_lib, name).restype = None
             getattr(_lib, name).argtypes = [C.c_void_p]
     return _lib
@@ -479,3 +485,90 @@ def tio_op_attention(stream_handle, dtype, B, T, H, dh, qkv_ptr, o_ptr, lse_ptr,
     vp = lambda p: C.c_void_p(p) if p else None
     _check(lib().tio_op_attention(vp(stream_handle), PREC[dtype], C.c_int64(B), C.c_int64(T), C.c_int64(H), C.c_int64(dh),
                                   vp(qkv_ptr), vp(o_ptr), vp(lse_ptr), vp(dO_ptr), vp(delta_ptr), vp(dqkv_ptr)))
+
+
+# ------------------------------------------------------------------ packed sequences, activations in 8 bits
+class Packing:
+    def __init__(self, handle):
+        self.h = handle
+
+    def __del__(self):
+        if getattr(self, "h", None):
+            lib().tio_packing_free(self.h)
+            self.h = None
+
+    def export(self):
+        """n_seqs, rows, max_len and `data`: an int32 array (a copy) to be put into device memory."""
+        v = PackingView()
+        _check(lib().tio_packing_export(self.h, C.byref(v)))
+        return dict(n_seqs=v.n_seqs, rows=v.rows, max_len=v.max_len, data=_arr(v.data, v.bytes // 4, np.int32))
+
+
+def tio_packing_build(offsets, dtype="bf16", H=0, Hkv=0, dh=0) -> Packing:
+    """offsets: first rows of the sequences, and the end of the last; without heads: for the preference loss only."""
+    o = np.ascontiguousarray(offsets, dtype=np.int64)
+    if o.ndim != 1 or len(o) < 1 or (o != o.astype(np.int32)).any():
+        raise ValueError("offsets must be a list of 32-bit numbers")
+    o = o.astype(np.int32)
+    h = C.c_void_p()
+    _check(lib().tio_packing_build(o.ctypes.data_as(C.POINTER(C.c_int32)), C.c_int32(len(o) - 1), PREC[dtype], C.c_int64(H), C.c_int64(Hkv),
+                                   C.c_int64(dh), C.byref(h)))
+    return Packing(h)
+
+
+def _vp(p):
+    return C.c_void_p(p) if p else None
+
+
+def tio_op_attention_packed(stream_handle, packing, packing_ptr, qkv_ptr, ld_qkv, o_ptr, ld_o, lse_ptr):
+    """Raw pointers (ints) of device buffers here and below; see include/teraio.h."""
+    _check(lib().tio_op_attention_packed(_vp(stream_handle), packing.h, _vp(packing_ptr), _vp(qkv_ptr), C.c_int64(ld_qkv), _vp(o_ptr), C.c_int64(ld_o),
+                                         _vp(lse_ptr)))
+
+
+def tio_op_attention_packed_work(packing) -> int:
+    n = C.c_uint64()
+    _check(lib().tio_op_attention_packed_work(packing.h, C.byref(n)))
+    return n.value
+
+
+def tio_op_attention_packed_bwd(stream_handle, packing, packing_ptr, qkv_ptr, ld_qkv, o_ptr, dO_ptr, ld_o, lse_ptr, work_ptr, dqkv_ptr):
+    _check(lib().tio_op_attention_packed_bwd(_vp(stream_handle), packing.h, _vp(packing_ptr), _vp(qkv_ptr), C.c_int64(ld_qkv), _vp(o_ptr), _vp(dO_ptr),
+                                             C.c_int64(ld_o), _vp(lse_ptr), _vp(work_ptr), _vp(dqkv_ptr)))
+
+
+def tio_op_preference_loss_work(packing) -> int:
+    n = C.c_uint64()
+    _check(lib().tio_op_preference_loss_work(packing.h, C.byref(n)))
+    return n.value
+
+
+def tio_op_preference_loss(stream_handle, dtype, packing, packing_ptr, V, logits_ptr, ld, labels_ptr, ref_logp_ptr, beta, smoothing, seq_logp_ptr,
+                           losses_ptr, loss_ptr, work_ptr, dlogits_ptr=0, total_pairs=0):
+    _check(lib().tio_op_preference_loss(_vp(stream_handle), PREC[dtype], packing.h, _vp(packing_ptr), C.c_int64(V), _vp(logits_ptr), C.c_int64(ld),
+                                        _vp(labels_ptr), _vp(ref_logp_ptr), C.c_float(beta), C.c_float(smoothing), C.c_int64(total_pairs),
+                                        _vp(seq_logp_ptr), _vp(losses_ptr), _vp(loss_ptr), _vp(work_ptr), _vp(dlogits_ptr)))
+
+
+def tio_ckpt8_bytes(rows, cols) -> int:
+    n = C.c_uint64()
+    _check(lib().tio_ckpt8_bytes(C.c_int64(rows), C.c_int64(cols), C.byref(n)))
+    return n.value
+
+
+def tio_op_ckpt8_store(stream_handle, dtype, rows, cols, x_ptr, ldx, ckpt_ptr):
+    _check(lib().tio_op_ckpt8_store(_vp(stream_handle), PREC[dtype], C.c_int64(rows), C.c_int64(cols), _vp(x_ptr), C.c_int64(ldx), _vp(ckpt_ptr)))
+
+
+def tio_op_ckpt8_load(stream_handle, dtype, rows, cols, ckpt_ptr, x_ptr, ldx):
+    _check(lib().tio_op_ckpt8_load(_vp(stream_handle), PREC[dtype], C.c_int64(rows), C.c_int64(cols), _vp(ckpt_ptr), _vp(x_ptr), C.c_int64(ldx)))
+
+
+def tio_op_act_ckpt8(stream_handle, dtype, act, rows, f, gate_ptr, up_ptr, ldu, y_ptr, ldy, ckpt_ptr):
+    _check(lib().tio_op_act_ckpt8(_vp(stream_handle), PREC[dtype], ACT[act], C.c_int64(rows), C.c_int64(f), _vp(gate_ptr), _vp(up_ptr), C.c_int64(ldu),
+                                  _vp(y_ptr), C.c_int64(ldy), _vp(ckpt_ptr)))
+
+
+def tio_op_act_ckpt8_bwd(stream_handle, dtype, act, rows, f, ckpt_ptr, dy_ptr, lddy, dgate_ptr, dup_ptr, ldu, y_ptr=0, ldy=0):
+    _check(lib().tio_op_act_ckpt8_bwd(_vp(stream_handle), PREC[dtype], ACT[act], C.c_int64(rows), C.c_int64(f), _vp(ckpt_ptr), _vp(dy_ptr), C.c_int64(lddy),
+                                      _vp(dgate_ptr), _vp(dup_ptr), C.c_int64(ldu), _vp(y_ptr), C.c_int64(ldy)))

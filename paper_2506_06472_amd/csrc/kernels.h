@@ -6,6 +6,8 @@
 
 #include <cstdint>
 
+#include "packing.h"
+
 namespace tio {
 namespace k {
 
@@ -93,6 +95,37 @@ bool attn_bwd_has_delta(int dtype, int64_t T, int64_t H, int64_t dh);
 // over O
 void attn_bwd(hipStream_t s, int dtype, const void *dO, const void *qkv, const void *O, const float *lse, float *delta,
               void *dqkv, int64_t B, int64_t T, int64_t H, int64_t dh);
+// ---- packed batches.  device: the packing's data in device memory; ld, ldo: from row to row of q | k | v and of o, in elements
+void attn_packed_fwd(hipStream_t s, const Packing &p, const void *device, const void *qkv, int64_t ld, void *o, int64_t ldo, float *lse);
+void attn_packed_bwd(hipStream_t s, const Packing &p, const void *device, const void *qkv, int64_t ld, const void *o, const void *dO, int64_t ldo,
+                     const float *lse, void *work, void *dqkv);
+// bytes of the backward pass's work; whether the longest sequence's rows are within the offsets the kernels use (host only)
+int64_t attn_packed_work(const Packing &p);
+bool attn_packed_fits(const Packing &p, int64_t ld, int64_t ldo);
+// in fp32 arithmetic (kernels_attn.hip)
+void attn_packed_fwd_f32(hipStream_t s, const Packing &p, const void *device, const void *qkv, int64_t ld, void *o, int64_t ldo, float *lse, float scale);
+void attn_packed_bwd_f32(hipStream_t s, const Packing &p, const void *device, const void *qkv, int64_t ld, const void *o, const void *dO, int64_t ldo,
+                         const float *lse, float *delta, void *dqkv, float scale);
+struct PreferenceArgs {
+    int64_t rows, pairs, total_pairs, V, ld;
+    const int32_t *offsets, *labels;             // device
+    const void *logits;
+    const float *ref;
+    float beta, smoothing;
+    float *seq, *losses, *loss;
+    void *work, *dlogits;                        // dlogits: nullptr for the loss alone
+};
+int64_t preference_work(int64_t rows);
+void preference_loss(hipStream_t s, int dtype, const PreferenceArgs &a);
+// ---- activations in eight bits (kernels_ckpt8.hip)
+bool ckpt8_fits(int64_t rows, int64_t cols);
+int64_t ckpt8_bytes(int64_t rows, int64_t cols);
+void ckpt8_store(hipStream_t s, int dtype, int64_t rows, int64_t cols, const void *x, int64_t ldx, void *kept);
+void ckpt8_load(hipStream_t s, int dtype, int64_t rows, int64_t cols, const void *kept, void *x, int64_t ldx);
+void act_ckpt8(hipStream_t s, int dtype, bool swiglu, int64_t rows, int64_t f, const void *gate, const void *up, int64_t ldu, void *y, int64_t ldy,
+               void *kept);
+void act_ckpt8_bwd(hipStream_t s, int dtype, bool swiglu, int64_t rows, int64_t f, const void *kept, const void *dy, int64_t lddy, void *dgate,
+                   void *dup, int64_t ldu, void *y, int64_t ldy);
 void embed_bwd(hipStream_t s, int dtype, const void *dx, const int32_t *tok, void *dwte, int64_t S, int64_t d,
                int64_t V, bool accumulate);
 void posemb_bwd(hipStream_t s, int dtype, const void *dx, void *dwpe, int64_t B, int64_t T, int64_t d, bool accumulate);

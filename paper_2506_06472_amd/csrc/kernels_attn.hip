@@ -20,6 +20,7 @@
 // Statistics are fp32 (log-sum-exp saved for the backward pass, which recomputes the probabilities from it); every sum has a
 // fixed order; the blocks of dQ and those of dK/dV are workgroups of their own, so that no atomics are needed.
 #include "../../include/teraio.h"
+#include "attn_packed.h"
 #include "device_common.h"
 #include "kernels.h"
 #include "mfma_tiles.h"
@@ -143,16 +144,68 @@ template <int DH> struct ColFrag {
     }
 };
 
-// Workgroup -> head and first own row; all row blocks of a head go to one XCD (its L2 then holds the head's other side).
-// false: no such head.
-__device__ __forceinline__ bool place(int64_t heads, int Tn, bool long_last, unsigned block, int64_t &bh, int &r0) {
-    const int nblk = (Tn + ROWS - 1) / ROWS;
-    const int slot = (int)(block >> 3);
-    bh = (int64_t)(slot / nblk) * 8 + (int)(block & 7);
-    const int blk = slot % nblk;
-    r0 = (long_last ? nblk - 1 - blk : blk) * ROWS;           // longest rows first
-    return bh < heads;
-}
+// Where a block of 32 rows is.  q, k, v: the sequence's first row at its heads; ld: from row to row; row, ldg: of that row and head in o and dO,
+// from row to row; stat: in lse and delta; Tn: rows of the sequence; r0: the block's first.  group, heads_ld: query heads of a block of keys, and
+// from one's lse to the next's.
+template <typename T> struct RowPlace {
+    const T *q, *k, *v;
+    int64_t ld, row, ldg, stat, heads_ld;
+    int Tn, r0, group;
+};
+// [B, T] rows of one length.  All row blocks of a head go to one XCD (its L2 then holds the head's other side).
+template <typename T> struct BatchRows {
+    static constexpr bool GROUPED = false;
+    const T *qkv;
+    int64_t heads, H;
+    int Tn;
+    template <int DH> __device__ __forceinline__ bool place(unsigned block, bool long_last, RowPlace<T> &at) const {
+        const int nblk = (Tn + ROWS - 1) / ROWS;
+        const int slot = (int)(block >> 3);
+        const int64_t bh = (int64_t)(slot / nblk) * 8 + (int)(block & 7);
+        const int blk = slot % nblk;
+        at.r0 = (long_last ? nblk - 1 - blk : blk) * ROWS;           // longest rows first
+        if (bh >= heads) return false;
+        const int64_t b = bh / H, h = bh % H, d = H * DH;
+        at.q = qkv + b * Tn * (3 * d) + h * DH;
+        at.k = at.q + d;
+        at.v = at.q + 2 * d;
+        at.ld = 3 * d;
+        at.row = b * Tn * d + h * DH;
+        at.ldg = d;
+        at.stat = bh * Tn;
+        at.heads_ld = 0;
+        at.Tn = Tn;
+        at.group = 1;
+        return true;
+    }
+};
+// A packed batch: blocks of query rows of every query head, blocks of key rows of every key head, which takes all query heads of its group.
+template <typename T> struct PackedBlocks {
+    static constexpr bool GROUPED = true;
+    const T *qkv;
+    int64_t ld, ldg;
+    int32_t H, Hkv;
+    PackedPlaces query, key;
+    template <int DH> __device__ __forceinline__ bool place(unsigned block, bool queries, RowPlace<T> &at) const {
+        const PackedPlaces &p = queries ? query : key;
+        int head;
+        const int32_t *item;
+        if (!p.find(block, head, item)) return false;
+        const int64_t first = item[0], group = H / Hkv, h = queries ? head : head * group, hk = queries ? head / group : head;
+        at.q = qkv + first * ld + h * DH;
+        at.k = qkv + first * ld + (H + hk) * DH;
+        at.v = at.k + (int64_t)Hkv * DH;
+        at.ld = ld;
+        at.row = first * ldg + h * DH;
+        at.ldg = ldg;
+        at.stat = h * p.rows + first;
+        at.heads_ld = p.rows;
+        at.Tn = item[1];
+        at.r0 = item[2];
+        at.group = (int)group;
+        return at.r0 >= 0 && at.r0 < at.Tn;
+    }
+};
 // LDS of the merge: the wavefronts' accumulators of one 32-column block
 template <int NW> constexpr int merge_floats() { return NW * 16 * 64; }
 // Sums of the wavefronts' accumulators, in wavefront order, stored to the rows the lanes hold (nullptr: no such row).  Wavefronts 0 to 3
@@ -182,21 +235,17 @@ __device__ __forceinline__ void merge_store(const floatx16 (&acc)[DH / 32], floa
 }
 
 // ---------------------------------------------------------------- forward
-template <template <typename> class R, typename T, int DH, int NW>
-__global__ void __launch_bounds__(NW * 64) attn_fwd_k(const T *__restrict__ qkv, T *__restrict__ o, float *__restrict__ lse,
-                                                  int64_t heads, int Tn, int64_t H, float scale) {
+template <template <typename> class R, typename T, int DH, int NW, typename W>
+__global__ void __launch_bounds__(NW * 64) attn_fwd_k(const W where, T *__restrict__ o, float *__restrict__ lse, float scale) {
     __shared__ float part[merge_floats<NW>()];
     __shared__ float stat[2][NW][ROWS];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, lhi = lane >> 5;
-    const int64_t d = H * DH, ld = 3 * d;
-    int64_t bh;
-    int q0;
-    if (!place(heads, Tn, true, blockIdx.x, bh, q0)) return;
-    const int64_t b = bh / H, h = bh % H;
-    const int q = q0 + l32;
-    const T *base = qkv + b * Tn * ld + h * DH;
+    RowPlace<T> at;
+    if (!where.template place<DH>(blockIdx.x, true, at)) return;
+    const int64_t ld = at.ld;
+    const int Tn = at.Tn, q0 = at.r0, q = q0 + l32;
     RowFrag<DH> qf;
-    qf.load(R<T>(base, ld, q0, Tn, DH), lane);
+    qf.load(R<T>(at.q, ld, q0, Tn, DH), lane);
     floatx16 acc[DH / 32];
 #pragma unroll
     for (int i = 0; i < DH / 32; ++i) acc[i] = zero16();
@@ -206,8 +255,8 @@ __global__ void __launch_bounds__(NW * 64) attn_fwd_k(const T *__restrict__ qkv,
         const int j0 = t * ROWS;
         RowFrag<DH> kf;
         ColFrag<DH> vf;
-        kf.load(R<T>(base + d, ld, j0, Tn, DH), lane);
-        vf.load(R<T>(base + 2 * d, ld, j0, Tn, DH), lane);
+        kf.load(R<T>(at.k, ld, j0, Tn, DH), lane);
+        vf.load(R<T>(at.v, ld, j0, Tn, DH), lane);
         floatx16 s = dot_rows(kf, qf);
         const float m_old = m;
         float tmax = -INFINITY;
@@ -241,8 +290,8 @@ __global__ void __launch_bounds__(NW * 64) attn_fwd_k(const T *__restrict__ qkv,
         l += stat[1][w][l32] * f[w];
     }
     m = M;
-    merge_store<T, DH, NW>(acc, part, wave, lane, f, 1.0f / l, q < Tn ? o + (b * Tn + q) * d + h * DH : nullptr);
-    if (wave == 0 && lhi == 0 && q < Tn) lse[bh * Tn + q] = m + logf(l);
+    merge_store<T, DH, NW>(acc, part, wave, lane, f, 1.0f / l, q < Tn ? o + (at.row + q * at.ldg) : nullptr);
+    if (wave == 0 && lhi == 0 && q < Tn) lse[at.stat + q] = m + logf(l);
 }
 
 // ---------------------------------------------------------------- backward
@@ -271,13 +320,12 @@ __global__ void __launch_bounds__(TPB) attn_bwd_pre_k(const T *__restrict__ dO, 
 }
 
 // Operands of the backward pass.  O: nullptr, or the forward pass's output, from which delta is then computed here and written.
-template <typename T> struct BwdArgs {
-    const T *dO, *qkv, *O;
+template <typename T, typename W> struct BwdArgs {
+    W where;
+    const T *dO, *O;
     const float *lse;
     float *delta;
     T *dqkv;
-    int64_t heads, H;
-    int Tn;
     float scale;
 };
 // sum over the head dimension of g * x, for the row a lane pair holds; the same in both lanes, and the bits of attn_bwd_pre_k, so that a
@@ -300,28 +348,25 @@ template <typename T, int DH> __device__ __forceinline__ float row_dot(const Row
 }
 
 // dQ: own query rows, keys and values stream
-template <template <typename> class R, typename T, int DH, int NW, bool OWN_DELTA>
-__device__ __forceinline__ void dq_rows(const BwdArgs<T> &a, unsigned block, float *part) {
+template <template <typename> class R, typename T, int DH, int NW, bool OWN_DELTA, typename W>
+__device__ __forceinline__ void dq_rows(const BwdArgs<T, W> &a, unsigned block, float *part) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, lhi = lane >> 5;
-    const int64_t H = a.H, d = H * DH, ld = 3 * d, Tn = a.Tn;
-    int64_t bh;
-    int q0;
-    if (!place(a.heads, a.Tn, true, block, bh, q0)) return;
-    const int64_t b = bh / H, h = bh % H;
-    const int q = q0 + l32, qc = min(q, a.Tn - 1);
-    const T *base = a.qkv + b * Tn * ld + h * DH;
+    RowPlace<T> at;
+    if (!a.where.template place<DH>(block, true, at)) return;
+    const int64_t ld = at.ld;
+    const int Tn = at.Tn, q0 = at.r0, q = q0 + l32, qc = min(q, Tn - 1);
     RowFrag<DH> qf, gf;
-    qf.load(R<T>(base, ld, q0, a.Tn, DH), lane);
-    gf.load(R<T>(a.dO + b * Tn * d + h * DH, d, q0, a.Tn, DH), lane);
-    const float li = a.lse[bh * Tn + qc];
+    qf.load(R<T>(at.q, ld, q0, Tn, DH), lane);
+    gf.load(R<T>(a.dO + at.row, at.ldg, q0, Tn, DH), lane);
+    const float li = a.lse[at.stat + qc];
     float di;
     if constexpr (OWN_DELTA) {
         RowFrag<DH> of;
-        of.load(R<T>(a.O + b * Tn * d + h * DH, d, q0, a.Tn, DH), lane);
+        of.load(R<T>(a.O + at.row, at.ldg, q0, Tn, DH), lane);
         di = row_dot<T>(gf, of, lane);
-        if (wave == 0 && lhi == 0 && q < a.Tn) a.delta[bh * Tn + q] = di;
+        if (wave == 0 && lhi == 0 && q < Tn) a.delta[at.stat + q] = di;
     } else {
-        di = a.delta[bh * Tn + qc];
+        di = a.delta[at.stat + qc];
     }
     floatx16 dq[DH / 32];
 #pragma unroll
@@ -329,7 +374,7 @@ __device__ __forceinline__ void dq_rows(const BwdArgs<T> &a, unsigned block, flo
     const int ntiles = q0 / ROWS + 1;
     for (int t = wave; t < ntiles; t += NW) {
         const int j0 = t * ROWS;
-        const R<T> k(base + d, ld, j0, a.Tn, DH), v(base + 2 * d, ld, j0, a.Tn, DH);
+        const R<T> k(at.k, ld, j0, Tn, DH), v(at.v, ld, j0, Tn, DH);
         RowFrag<DH> kf, vf;
         ColFrag<DH> kc;
         kf.load(k, lane);
@@ -347,30 +392,36 @@ __device__ __forceinline__ void dq_rows(const BwdArgs<T> &a, unsigned block, flo
     float one[NW];
 #pragma unroll
     for (int w = 0; w < NW; ++w) one[w] = 1.f;
-    merge_store<T, DH, NW>(dq, part, wave, lane, one, a.scale, q < a.Tn ? a.dqkv + (b * Tn + q) * ld + h * DH : nullptr);
+    merge_store<T, DH, NW>(dq, part, wave, lane, one, a.scale, q < Tn ? a.dqkv + (at.q - a.where.qkv) + q * ld : nullptr);
 }
 
 // dK, dV: own key rows, queries and output gradients stream
-template <template <typename> class R, typename T, int DH, int NW, bool OWN_DELTA>
-__device__ __forceinline__ void dkv_rows(const BwdArgs<T> &a, unsigned block, float *part) {
+template <template <typename> class R, typename T, int DH, int NW, bool OWN_DELTA, typename W>
+__device__ __forceinline__ void dkv_rows(const BwdArgs<T, W> &a, unsigned block, float *part) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, lhi = lane >> 5;
-    const int64_t H = a.H, d = H * DH, ld = 3 * d, Tn = a.Tn;
-    int64_t bh;
-    int kv0;
-    if (!place(a.heads, a.Tn, false, block, bh, kv0)) return;
-    const int64_t b = bh / H, h = bh % H;
-    const int kv = kv0 + l32;
-    const T *base = a.qkv + b * Tn * ld + h * DH, *gbase = a.dO + b * Tn * d + h * DH;
-    const float *ls = a.lse + bh * Tn, *dl = a.delta + bh * Tn;
+    RowPlace<T> at;
+    if (!a.where.template place<DH>(block, false, at)) return;
+    const int64_t ld = at.ld;
+    const int Tn = at.Tn, kv0 = at.r0, kv = kv0 + l32;
+    const T *base = at.q, *gbase = a.dO + at.row;
+    const float *ls = a.lse + at.stat, *dl = a.delta + at.stat;
     RowFrag<DH> kf, vf;
-    kf.load(R<T>(base + d, ld, kv0, a.Tn, DH), lane);
-    vf.load(R<T>(base + 2 * d, ld, kv0, a.Tn, DH), lane);
+    kf.load(R<T>(at.k, ld, kv0, Tn, DH), lane);
+    vf.load(R<T>(at.v, ld, kv0, Tn, DH), lane);
     floatx16 dk[DH / 32], dv[DH / 32];
 #pragma unroll
     for (int i = 0; i < DH / 32; ++i) { dk[i] = zero16(); dv[i] = zero16(); }
-    for (int i0 = kv0 + wave * ROWS; i0 < a.Tn; i0 += NW * ROWS) {
-        const R<T> qr(base, ld, i0, a.Tn, DH), gr(gbase, d, i0, a.Tn, DH);
-        const int row = min(i0 + l32, a.Tn - 1);
+    // all query heads' tiles in one chain, of which every wavefront takes every NW-th
+    const int tiles = (Tn - kv0 + ROWS - 1) / ROWS, all = W::GROUPED ? tiles * at.group : tiles;
+    int head = 0;
+    for (int n = wave; n < all; n += NW) {
+        while (W::GROUPED && n - head * tiles >= tiles) {
+            ++head;
+            base += DH, gbase += DH, ls += at.heads_ld, dl += at.heads_ld;
+        }
+        const int i0 = kv0 + (n - head * tiles) * ROWS;
+        const R<T> qr(base, ld, i0, Tn, DH), gr(gbase, at.ldg, i0, Tn, DH);
+        const int row = min(i0 + l32, Tn - 1);
         RowFrag<DH> qf, gf;
         ColFrag<DH> qc, gc;
         qf.load(qr, lane);
@@ -381,7 +432,7 @@ __device__ __forceinline__ void dkv_rows(const BwdArgs<T> &a, unsigned block, fl
         float delta_row;
         if constexpr (OWN_DELTA) {
             RowFrag<DH> of;
-            of.load(R<T>(a.O + b * Tn * d + h * DH, d, i0, a.Tn, DH), lane);
+            of.load(R<T>(a.O + (gbase - a.dO), at.ldg, i0, Tn, DH), lane);
             delta_row = row_dot<T>(gf, of, lane);
         } else {
             delta_row = dl[row];
@@ -393,7 +444,7 @@ __device__ __forceinline__ void dkv_rows(const BwdArgs<T> &a, unsigned block, fl
         for (int r = 0; r < 16; ++r) {
             const int q = i0 + acc_row(r, lhi);
             const float li = __shfl(lse_row, acc_row(r, lhi), 64), di = __shfl(delta_row, acc_row(r, lhi), 64);
-            const float p = (q >= kv && q < a.Tn) ? expf(s[r] * a.scale - li) : 0.f;
+            const float p = (q >= kv && q < Tn) ? expf(s[r] * a.scale - li) : 0.f;
             dp[r] = p * (dp[r] - di);
             s[r] = p;
         }
@@ -403,17 +454,17 @@ __device__ __forceinline__ void dkv_rows(const BwdArgs<T> &a, unsigned block, fl
     float one[NW];
 #pragma unroll
     for (int w = 0; w < NW; ++w) one[w] = 1.f;
-    T *krow = kv < a.Tn ? a.dqkv + (b * Tn + kv) * ld + d + h * DH : nullptr;
+    T *krow = kv < Tn ? a.dqkv + (at.k - a.where.qkv) + kv * ld : nullptr;
     merge_store<T, DH, NW>(dk, part, wave, lane, one, a.scale, krow);
-    merge_store<T, DH, NW>(dv, part, wave, lane, one, 1.0f, krow ? krow + d : nullptr);
+    merge_store<T, DH, NW>(dv, part, wave, lane, one, 1.0f, krow ? krow + (at.v - at.k) : nullptr);
 }
 
 // The blocks of key rows come first, they are the longer ones; then the blocks of query rows.  One launch for both: the sequences that
 // this path is for fill neither the chip with one of them, nor the time of a launch.  Two wavefronts per SIMD at head size 64 (235
 // registers; left to itself the compiler takes 288 and there is one), three at 32; one with 64-bit addresses.
 template <bool WIDE, int DH, int NW> constexpr int waves_per_simd() { return DH == 128 || WIDE ? 1 : DH == 64 || NW == 8 ? 2 : 3; }
-template <template <typename> class R, typename T, int DH, int NW, bool OWN_DELTA>
-__global__ void __launch_bounds__(NW * 64, (waves_per_simd<R<T>::WIDE, DH, NW>())) attn_bwd_k(const BwdArgs<T> a, unsigned blocks, unsigned first) {
+template <template <typename> class R, typename T, int DH, int NW, bool OWN_DELTA, typename W>
+__global__ void __launch_bounds__(NW * 64, (waves_per_simd<R<T>::WIDE, DH, NW>())) attn_bwd_k(const BwdArgs<T, W> a, unsigned blocks, unsigned first) {
     __shared__ float part[merge_floats<NW>()];
     const unsigned block = first + blockIdx.x;
     if (block < blocks) dkv_rows<R, T, DH, NW, OWN_DELTA>(a, block, part);
@@ -429,29 +480,51 @@ unsigned grid_for(int64_t heads, int64_t Tn) { return (unsigned)((Tn + ROWS - 1)
 bool eight_wavefronts(int64_t blocks, int64_t Tn, int64_t dh) { return dh == 32 && Tn > 4 * ROWS && blocks <= 512; }
 
 template <int DH> constexpr bool own_delta() { return DH == 32; }    // at 64 it does not fit the registers, and delta has a launch of its own
-// whether 32 rows of q, k and v are too wide for Rows
-bool wide(int dtype, int64_t H, int64_t dh) { return ROWS * 3 * H * dh * (dtype == TIO_PREC_BF16 ? 2 : 4) >= ((int64_t)1 << 32); }
-template <template <typename> class R, typename T, int DH, int NW, bool OWN_DELTA> void launch_both(hipStream_t s, const BwdArgs<T> &a, unsigned blocks) {
-    if ((uint64_t)2 * blocks * NW * 64 < ((uint64_t)1 << 32)) {
-        attn_bwd_k<R, T, DH, NW, OWN_DELTA><<<2 * blocks, NW * 64, 0, s>>>(a, blocks, 0);
+// whether 32 rows of ld elements are too wide for Rows
+bool wide(int dtype, int64_t ld) { return ROWS * ld * (dtype == TIO_PREC_BF16 ? 2 : 4) >= ((int64_t)1 << 32); }
+// key_blocks, query_blocks: workgroups of either kind
+template <template <typename> class R, typename T, int DH, int NW, bool OWN_DELTA, typename W>
+void launch_both(hipStream_t s, const BwdArgs<T, W> &a, unsigned key_blocks, unsigned query_blocks) {
+    if (((uint64_t)key_blocks + query_blocks) * NW * 64 < ((uint64_t)1 << 32)) {
+        attn_bwd_k<R, T, DH, NW, OWN_DELTA><<<key_blocks + query_blocks, NW * 64, 0, s>>>(a, key_blocks, 0);
     } else {                     // a grid has fewer than 2^32 threads
-        attn_bwd_k<R, T, DH, NW, OWN_DELTA><<<blocks, NW * 64, 0, s>>>(a, blocks, 0);
-        attn_bwd_k<R, T, DH, NW, OWN_DELTA><<<blocks, NW * 64, 0, s>>>(a, blocks, blocks);
+        attn_bwd_k<R, T, DH, NW, OWN_DELTA><<<key_blocks, NW * 64, 0, s>>>(a, key_blocks, 0);
+        attn_bwd_k<R, T, DH, NW, OWN_DELTA><<<query_blocks, NW * 64, 0, s>>>(a, key_blocks, key_blocks);
     }
 }
-template <typename T, int DH> void launch_bwd(hipStream_t s, const BwdArgs<T> &a, bool wide) {
-    const unsigned blocks = grid_for(a.heads, a.Tn);
-    if (wide) {
-        launch_both<WideRows, T, DH, 4, false>(s, a, blocks);
-    } else if constexpr (own_delta<DH>()) {
-        const bool eight = eight_wavefronts(2 * (int64_t)blocks, a.Tn, DH);
-        if (a.O && eight) launch_both<Rows, T, DH, 8, true>(s, a, blocks);
-        else if (a.O) launch_both<Rows, T, DH, 4, true>(s, a, blocks);
-        else if (eight) launch_both<Rows, T, DH, 8, false>(s, a, blocks);
-        else launch_both<Rows, T, DH, 4, false>(s, a, blocks);
-    } else {
-        launch_both<Rows, T, DH, 4, false>(s, a, blocks);
+template <typename T, int DH, typename W>
+void launch_bwd(hipStream_t s, const BwdArgs<T, W> &a, unsigned key_blocks, unsigned query_blocks, int64_t longest, bool wide) {
+    if constexpr (!W::GROUPED) {
+        if (wide) {
+            launch_both<WideRows, T, DH, 4, false>(s, a, key_blocks, query_blocks);
+            return;
+        }
     }
+    if constexpr (own_delta<DH>()) {
+        const bool eight = eight_wavefronts((int64_t)key_blocks + query_blocks, longest, DH);
+        if (a.O && eight) launch_both<Rows, T, DH, 8, true>(s, a, key_blocks, query_blocks);
+        else if (a.O) launch_both<Rows, T, DH, 4, true>(s, a, key_blocks, query_blocks);
+        else if (eight) launch_both<Rows, T, DH, 8, false>(s, a, key_blocks, query_blocks);
+        else launch_both<Rows, T, DH, 4, false>(s, a, key_blocks, query_blocks);
+    } else {
+        launch_both<Rows, T, DH, 4, false>(s, a, key_blocks, query_blocks);
+    }
+}
+template <typename T, int DH, typename W>
+void launch_fwd(hipStream_t s, const W &where, unsigned grid, T *o, float *lse, float scale, int64_t longest, bool wide) {
+    constexpr int MANY = DH == 32 ? 8 : 4;
+    if constexpr (!W::GROUPED) {
+        if (wide) {
+            attn_fwd_k<WideRows, T, DH, 4><<<grid, 256, 0, s>>>(where, o, lse, scale);
+            return;
+        }
+    }
+    if (eight_wavefronts(grid, longest, DH)) attn_fwd_k<Rows, T, DH, MANY><<<grid, MANY * 64, 0, s>>>(where, o, lse, scale);
+    else attn_fwd_k<Rows, T, DH, 4><<<grid, 256, 0, s>>>(where, o, lse, scale);
+}
+template <typename T> PackedBlocks<T> packed_blocks(const Packing &p, const void *device, const void *qkv, int64_t ld, int64_t ldg) {
+    return PackedBlocks<T>{(const T *)qkv, ld, ldg, p.H, p.Hkv, packed_places(p, device, p.fwd, sizeof(QueryItem) / 4, p.H),
+                           packed_places(p, device, p.key, sizeof(KeyItem) / 4, p.Hkv)};
 }
 
 }  // namespace
@@ -475,11 +548,8 @@ void attn_fwd(hipStream_t s, int dtype, const void *qkv, void *o, float *lse, in
     if (attn_mfma_supported(dtype, Tn, H, dh)) { attn_fwd_mfma(s, qkv, o, lse, B, Tn, H, dh); return; }
     const float scale = 1.0f / sqrtf((float)dh);
     TIO_ATTN_DISPATCH(dtype, dh, {
-        const unsigned grid = grid_for(B * H, Tn);
-        constexpr int MANY = DH == 32 ? 8 : 4;
-        if (wide(dtype, H, dh)) attn_fwd_k<WideRows, T, DH, 4><<<grid, 256, 0, s>>>((const T *)qkv, (T *)o, lse, B * H, (int)Tn, H, scale);
-        else if (eight_wavefronts(grid, Tn, DH)) attn_fwd_k<Rows, T, DH, MANY><<<grid, MANY * 64, 0, s>>>((const T *)qkv, (T *)o, lse, B * H, (int)Tn, H, scale);
-        else attn_fwd_k<Rows, T, DH, 4><<<grid, 256, 0, s>>>((const T *)qkv, (T *)o, lse, B * H, (int)Tn, H, scale);
+        const BatchRows<T> where{(const T *)qkv, B * H, H, (int)Tn};
+        launch_fwd<T, DH>(s, where, grid_for(B * H, Tn), (T *)o, lse, scale, Tn, wide(dtype, 3 * H * dh));
     });
 }
 
@@ -493,7 +563,7 @@ void attn_bwd_pre(hipStream_t s, int dtype, const void *dO, const void *O, float
 }
 
 bool attn_bwd_has_delta(int dtype, int64_t Tn, int64_t H, int64_t dh) {
-    return (dh == 32 && !wide(dtype, H, dh)) || attn_mfma_supported(dtype, Tn, H, dh);
+    return (dh == 32 && !wide(dtype, 3 * H * dh)) || attn_mfma_supported(dtype, Tn, H, dh);
 }
 
 void attn_bwd(hipStream_t s, int dtype, const void *dO, const void *qkv, const void *O, const float *lse, float *delta, void *dqkv,
@@ -502,8 +572,48 @@ void attn_bwd(hipStream_t s, int dtype, const void *dO, const void *qkv, const v
     if (attn_mfma_supported(dtype, Tn, H, dh)) { attn_bwd_mfma(s, dO, qkv, O, lse, delta, dqkv, B, Tn, H, dh); return; }
     const float scale = 1.0f / sqrtf((float)dh);
     TIO_ATTN_DISPATCH(dtype, dh, {
-        const BwdArgs<T> a{(const T *)dO, (const T *)qkv, (const T *)O, lse, delta, (T *)dqkv, B * H, H, (int)Tn, scale};
-        launch_bwd<T, DH>(s, a, wide(dtype, H, dh));
+        const BwdArgs<T, BatchRows<T>> a{{(const T *)qkv, B * H, H, (int)Tn}, (const T *)dO, (const T *)O, lse, delta, (T *)dqkv, scale};
+        const unsigned blocks = grid_for(B * H, Tn);
+        launch_bwd<T, DH>(s, a, blocks, blocks, Tn, wide(dtype, 3 * H * dh));
+    });
+}
+
+void attn_packed_fwd_f32(hipStream_t s, const Packing &p, const void *device, const void *qkv, int64_t ld, void *o, int64_t ldo, float *lse, float scale) {
+    TIO_ATTN_DISPATCH(p.dtype, p.dh, {
+        const PackedBlocks<T> where = packed_blocks<T>(p, device, qkv, ld, ldo);
+        launch_fwd<T, DH>(s, where, where.query.grid(), (T *)o, lse, scale, p.max_len, false);
+    });
+}
+
+// delta of a packed batch: a group of dh / (elements per 16 bytes) lanes to a row and head, as in attn_bwd_pre_k
+template <typename T>
+__global__ void __launch_bounds__(TPB) attn_packed_pre_k(const T *__restrict__ dO, const T *__restrict__ O, int64_t ldo, float *__restrict__ delta, int64_t rows,
+                                                         int H, int dh) {
+    constexpr int V = Vec16<T>::N;
+    const int lanes = dh / V, of_block = TPB / lanes;
+    const int64_t row = blockIdx.x;
+    const int g = threadIdx.x % lanes;
+    for (int h = threadIdx.x / lanes; h < H; h += of_block) {        // all lanes of a group together
+        Vec16<T> x, y;
+        x.load(dO + row * ldo + (int64_t)h * dh + g * V);
+        y.load(O + row * ldo + (int64_t)h * dh + g * V);
+        float fx[V], fy[V], sum = 0.f;
+        x.get(fx); y.get(fy);
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum = fmaf(fx[i], fy[i], sum);
+        for (int o = 1; o < lanes; o <<= 1) sum += __shfl_xor(sum, o, 64);
+        if (g == 0) delta[h * rows + row] = sum;
+    }
+}
+
+void attn_packed_bwd_f32(hipStream_t s, const Packing &p, const void *device, const void *qkv, int64_t ld, const void *o, const void *dO, int64_t ldo,
+                         const float *lse, float *delta, void *dqkv, float scale) {
+    const bool own = p.dh == 32;
+    TIO_ATTN_DISPATCH(p.dtype, p.dh, {
+        if (!own) attn_packed_pre_k<T><<<(unsigned)p.rows, TPB, 0, s>>>((const T *)dO, (const T *)o, ldo, delta, p.rows, p.H, p.dh);
+        const PackedBlocks<T> where = packed_blocks<T>(p, device, qkv, ld, ldo);
+        const BwdArgs<T, PackedBlocks<T>> a{where, (const T *)dO, own ? (const T *)o : nullptr, lse, delta, (T *)dqkv, scale};
+        launch_bwd<T, DH>(s, a, where.key.grid(), where.query.grid(), p.max_len, false);
     });
 }
 

@@ -1,0 +1,173 @@
+// Causal attention over a packed batch on the matrix cores (bf16, head size 64 or 128): sequences of different lengths one behind the other, query
+// heads in groups that share a key and value head.  The loops are those of attn_mfma_rows.h; here is where their rows lie and how the batch is cut.
+//
+// The G query heads of a key head count as G rows for each row of the sequence (row r, head i: r * G + i).  A block of query rows then reads K
+// and V once for all its heads, has G times fewer keys between its first and last row's diagonals, and a short sequence fills it G times
+// better; a block of keys takes the query rows of all its heads in one chain of tiles, so that dK and dV need no sums over heads.
+// Workgroups are dealt longest first (attn_packed.h).  A block of keys whose chain would outlast the others is cut into pieces, whose fp32 sums
+// a launch behind them adds in order: no atomics, and results that depend on nothing but the lengths.
+#include "../../include/teraio.h"
+#include "attn_mfma_rows.h"
+#include "attn_packed.h"
+#include "kernels.h"
+
+namespace tio {
+namespace k {
+
+namespace {
+
+struct PackedRows {
+    static constexpr bool GROUPED = true;
+    const uint16_t *qkv;
+    int64_t ld, ldg;
+    int32_t H, G;
+    PackedPlaces places;
+
+    template <int DH, typename P> __device__ __forceinline__ bool start(unsigned block, P &at, int &hk, const int32_t *&item) const {
+        if (!places.find(block, hk, item)) return false;
+        const int64_t first = item[0];
+        at.q = qkv + first * ld + (int64_t)hk * G * DH;
+        at.k = qkv + first * ld + (int64_t)(H + hk) * DH;
+        at.v = at.k + (int64_t)places.heads * DH;
+        at.ld = ld;
+        at.row = first * ldg + (int64_t)hk * G * DH;
+        at.ldg = ldg;
+        at.stat = (int64_t)hk * G * places.rows + first;
+        at.heads_ld = places.rows;
+        at.Tn = item[1];
+        at.G = G;
+        return true;
+    }
+    template <int DH, int ROWS> __device__ __forceinline__ bool place(unsigned block, QueryPlace &at) const {
+        const int32_t *item;
+        int hk;
+        if (!start<DH>(block, at, hk, item)) return false;
+        at.v0 = item[2];
+        return at.v0 >= 0 && at.v0 < at.Tn * G;
+    }
+    // hk: the key head; part: of its partial sums, or -1
+    template <int DH, int KEYS> __device__ __forceinline__ bool place(unsigned block, KeyPlace &at, int &hk, int &part, int &pieces) const {
+        const int32_t *item;
+        if (!start<DH>(block, at, hk, item)) return false;
+        at.kv0 = item[2];
+        at.t0 = item[3];
+        const int per_tile = 64 / G, tiles = (at.Tn - at.kv0 + per_tile - 1) / per_tile;
+        at.t1 = item[4] < tiles ? item[4] : tiles;
+        part = item[5];
+        pieces = item[6];
+        return at.kv0 >= 0 && at.kv0 < at.Tn && at.t0 >= 0;
+    }
+};
+
+template <int DH, int NG>
+__global__ void __launch_bounds__(NT, DH == 64 ? 3 : 2) attn_packed_dq_mfma_k(const PackedRows where, const uint16_t *__restrict__ dO,
+                                                                              const uint16_t *__restrict__ O, const float *__restrict__ lse,
+                                                                              float *__restrict__ delta, uint16_t *__restrict__ dqkv, float scale) {
+    QueryPlace at;
+    if (!where.place<DH, NT / 64 * 16 * NG>(blockIdx.x, at)) return;
+    dq_rows<DH, NT / 64, NG, true>(at, dO + at.row, O + at.row, lse + at.stat, delta + at.stat, dqkv + (at.q - where.qkv), scale);
+}
+
+// parts: blocks of partial sums of each key head, at `partial`
+template <int DH, int NW, int NG, bool TAIL>
+__global__ void __launch_bounds__(NW * 64, DH == 64 ? 3 : 2) attn_packed_dkv_mfma_k(const PackedRows where, const uint16_t *__restrict__ dO,
+                                                                                    const float *__restrict__ lse, const float *__restrict__ delta,
+                                                                                    uint16_t *__restrict__ dqkv, float *__restrict__ partial, int parts,
+                                                                                    float scale) {
+    KeyPlace at;
+    int hk, part, pieces;
+    if (!where.place<DH, NW * 16 * NG>(blockIdx.x, at, hk, part, pieces) || at.t0 >= at.t1 || part >= parts) return;
+    float *const mine = part < 0 ? nullptr : partial + ((int64_t)hk * parts + part) * key_partial<DH, NW, NG>();
+    dkv_rows<DH, NW, NG, false, true, TAIL>(at, dO + at.row, nullptr, lse + at.stat, delta + at.stat, dqkv + (at.k - where.qkv),
+                                            dqkv + (at.v - where.qkv), mine, scale);
+}
+
+template <int DH, int NW, int NG>
+__global__ void __launch_bounds__(NW * 64) attn_packed_sums_k(const PackedRows where, const float *__restrict__ partial, int parts, uint16_t *__restrict__ dqkv,
+                                                              float scale) {
+    KeyPlace at;
+    int hk, part, pieces;
+    if (!where.place<DH, NW * 16 * NG>(blockIdx.x, at, hk, part, pieces) || part < 0 || pieces < 1 || part > parts - pieces) return;
+    key_sums<DH, NW, NG>(at, partial + ((int64_t)hk * parts + part) * key_partial<DH, NW, NG>(), pieces, (int)blockIdx.y, dqkv + (at.k - where.qkv),
+                         dqkv + (at.v - where.qkv), scale);
+}
+
+template <int DH> constexpr size_t fwd_smem() { return (size_t)3 * 2 * 32 * DH * 2; }      // three pairs of tiles
+template <int DH> constexpr size_t kv_smem() { return (size_t)2 * 2 * 64 * DH * 2; }       // two buffers of two tiles
+template <int DH, int NW, int NG> constexpr size_t dkv_smem() {         // tiles, V rows, then statistics
+    return (size_t)2 * 2 * 64 * DH * 2 + (dkv_v_in_lds<DH, NG>() ? (size_t)NW * 16 * NG * DH * 2 : 0) + 2 * 128 * 4;
+}
+
+PackedRows rows_of(const Packing &p, const void *device, const ItemList &list, int words, const void *qkv, int64_t ld, int64_t ldg) {
+    return PackedRows{(const uint16_t *)qkv, ld, ldg, p.H, p.group(), packed_places(p, device, list, words, p.Hkv)};
+}
+constexpr int QUERY_WORDS = sizeof(QueryItem) / 4, KEY_WORDS = sizeof(KeyItem) / 4;
+
+template <int DH> void fwd(hipStream_t s, const Packing &p, const void *device, const void *qkv, int64_t ld, void *o, int64_t ldo, float *lse, float scale) {
+    const PackedRows w = rows_of(p, device, p.fwd, QUERY_WORDS, qkv, ld, ldo);
+    if (p.fwd_rows == 64) attn_fwd_mfma_k<DH, 1><<<w.places.grid(), NT, fwd_smem<DH>(), s>>>(w, (uint16_t *)o, lse, scale);
+    else attn_fwd_mfma_k<DH, 2><<<w.places.grid(), NT, fwd_smem<DH>(), s>>>(w, (uint16_t *)o, lse, scale);
+}
+
+// the launches of a kind of block of keys: NW wavefronts of 16 NG keys
+template <int DH, int NW, int NG>
+void key_blocks(hipStream_t s, const Packing &p, const void *device, const void *qkv, int64_t ld, const void *dO, int64_t ldo, const float *lse,
+                const float *delta, float *partial, void *dqkv, float scale) {
+    const PackedRows w = rows_of(p, device, p.key, KEY_WORDS, qkv, ld, ldo);
+    auto go = [&](auto TAIL) {
+        const auto kernel = attn_packed_dkv_mfma_k<DH, NW, NG, TAIL()>;
+        (void)hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)dkv_smem<DH, NW, NG>());
+        kernel<<<w.places.grid(), NW * 64, dkv_smem<DH, NW, NG>(), s>>>(w, (const uint16_t *)dO, lse, delta, (uint16_t *)dqkv, partial, p.parts, scale);
+    };
+    if (rows_between_loads<DH, NW>() % p.group()) go(std::true_type{});
+    else go(std::false_type{});
+    if (p.sums.n) {
+        const PackedRows r = rows_of(p, device, p.sums, KEY_WORDS, qkv, ld, ldo);
+        attn_packed_sums_k<DH, NW, NG><<<dim3(r.places.grid(), DH / 32), NW * 64, 0, s>>>(r, partial, p.parts, (uint16_t *)dqkv, scale);
+    }
+}
+
+template <int DH> void bwd(hipStream_t s, const Packing &p, const void *device, const void *qkv, int64_t ld, const void *o, const void *dO, int64_t ldo,
+                           const float *lse, float *delta, float *partial, void *dqkv, float scale) {
+    const PackedRows q = rows_of(p, device, p.dq, QUERY_WORDS, qkv, ld, ldo);
+    const auto kernel = attn_packed_dq_mfma_k<DH, 2>;
+    (void)hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kv_smem<DH>());
+    kernel<<<q.places.grid(), NT, kv_smem<DH>(), s>>>(q, (const uint16_t *)dO, (const uint16_t *)o, lse, delta, (uint16_t *)dqkv, scale);
+    key_blocks<DH, dkv_waves<DH>(), 2>(s, p, device, qkv, ld, dO, ldo, lse, delta, partial, dqkv, scale);
+}
+
+int64_t delta_bytes(const Packing &p) { return ((int64_t)p.H * p.rows * 4 + 255) / 256 * 256; }
+
+}  // namespace
+
+int64_t attn_packed_work(const Packing &p) {
+    const int64_t part = (int64_t)p.keys * p.dh * 2 * 4;
+    return delta_bytes(p) + (int64_t)p.parts * p.Hkv * part + 256;
+}
+
+// 32-bit offsets, as in kernels_attn_mfma.hip: a sequence's rows, and the rows past it that a block asks for, span less than 2 GiB
+// (in fp32 arithmetic: 32 rows less than 4 GiB).
+bool attn_packed_fits(const Packing &p, int64_t ld, int64_t ldo) {
+    constexpr int64_t PAST = 512;
+    const int64_t most = ld > ldo ? ld : ldo;
+    return most < ((int64_t)1 << 24) && (!p.mfma || ((int64_t)p.max_len + PAST) * most * 2 < ((int64_t)1 << 31));
+}
+
+void attn_packed_fwd(hipStream_t s, const Packing &p, const void *device, const void *qkv, int64_t ld, void *o, int64_t ldo, float *lse) {
+    const float scale = 1.0f / sqrtf((float)p.dh);
+    if (!p.mfma) attn_packed_fwd_f32(s, p, device, qkv, ld, o, ldo, lse, scale);
+    else if (p.dh == 64) fwd<64>(s, p, device, qkv, ld, o, ldo, lse, scale);
+    else fwd<128>(s, p, device, qkv, ld, o, ldo, lse, scale);
+}
+
+void attn_packed_bwd(hipStream_t s, const Packing &p, const void *device, const void *qkv, int64_t ld, const void *o, const void *dO, int64_t ldo,
+                     const float *lse, void *work, void *dqkv) {
+    const float scale = 1.0f / sqrtf((float)p.dh);
+    float *const delta = (float *)work, *const partial = (float *)((char *)work + delta_bytes(p));
+    if (!p.mfma) attn_packed_bwd_f32(s, p, device, qkv, ld, o, dO, ldo, lse, delta, dqkv, scale);
+    else if (p.dh == 64) bwd<64>(s, p, device, qkv, ld, o, dO, ldo, lse, delta, partial, dqkv, scale);
+    else bwd<128>(s, p, device, qkv, ld, o, dO, ldo, lse, delta, partial, dqkv, scale);
+}
+
+}  // namespace k
+}  // namespace tio

@@ -1,0 +1,113 @@
+// How a packed batch is cut into workgroups.  Every list is sorted by the time its items take, the longest first: workgroups start in the order of
+// their numbers, so that what is left when the chip runs empty are the shortest.
+#include "packing.h"
+
+#include <algorithm>
+#include <cstring>
+#include <stdexcept>
+#include <string>
+
+#include "../../include/teraio.h"
+
+namespace tio {
+
+namespace {
+
+constexpr int COMPUTE_UNITS = 256;
+
+template <typename Item> ItemList append(Packing &p, std::vector<std::pair<int64_t, Item>> &items) {
+    std::stable_sort(items.begin(), items.end(), [](const auto &a, const auto &b) { return a.first > b.first; });
+    ItemList l;
+    l.at = (int32_t)p.data.size();
+    l.n = (int32_t)items.size();
+    p.data.resize(p.data.size() + items.size() * (sizeof(Item) / 4));
+    for (size_t i = 0; i < items.size(); ++i) std::memcpy(p.data.data() + l.at + i * (sizeof(Item) / 4), &items[i].second, sizeof(Item));
+    return l;
+}
+
+// blocks of `rows` query rows; group heads' rows count as one sequence
+ItemList query_items(Packing &p, const int32_t *offsets, int rows, int group) {
+    std::vector<std::pair<int64_t, QueryItem>> items;
+    for (int s = 0; s < p.n_seqs; ++s) {
+        const int32_t first = offsets[s], len = offsets[s + 1] - first;
+        for (int64_t v0 = 0; v0 < (int64_t)len * group; v0 += rows) {
+            const int64_t last = std::min<int64_t>((v0 + rows - 1) / group, len - 1);
+            items.push_back({last, QueryItem{first, len, (int32_t)v0, 0}});
+        }
+    }
+    return append(p, items);
+}
+
+int64_t query_blocks(const Packing &p, const int32_t *offsets, int rows, int group) {
+    int64_t n = 0;
+    for (int s = 0; s < p.n_seqs; ++s) n += ((int64_t)(offsets[s + 1] - offsets[s]) * group + rows - 1) / rows;
+    return n;
+}
+
+// Blocks of `keys` key rows.  A block whose tiles are more than a piece's is shared by several items, whose sums are added afterwards.
+void key_items(Packing &p, const int32_t *offsets, int keys, int per_tile, int64_t piece) {
+    std::vector<std::pair<int64_t, KeyItem>> items, sums;
+    for (int s = 0; s < p.n_seqs; ++s) {
+        const int32_t first = offsets[s], len = offsets[s + 1] - first;
+        for (int32_t kv0 = 0; kv0 < len; kv0 += keys) {
+            const int64_t tiles = ((int64_t)len - kv0 + per_tile - 1) / per_tile, pieces = tiles > piece + piece / 2 ? (tiles + piece - 1) / piece : 1;
+            if (pieces == 1) {
+                items.push_back({tiles, KeyItem{first, len, kv0, 0, (int32_t)tiles, -1, 0, 0}});
+                continue;
+            }
+            sums.push_back({pieces, KeyItem{first, len, kv0, 0, 0, p.parts, (int32_t)pieces, 0}});
+            for (int64_t i = 0; i < pieces; ++i) {
+                const int64_t t0 = tiles * i / pieces, t1 = tiles * (i + 1) / pieces;
+                items.push_back({t1 - t0, KeyItem{first, len, kv0, (int32_t)t0, (int32_t)t1, p.parts++, 0, 0}});
+            }
+        }
+    }
+    p.key = append(p, items);
+    p.sums = append(p, sums);
+}
+
+}  // namespace
+
+Packing build_packing(const int32_t *offsets, int32_t n_seqs, int32_t dtype, int64_t H, int64_t Hkv, int64_t dh) {
+    if (n_seqs < 1) throw std::invalid_argument("a packing needs at least one sequence");
+    if (offsets[0] != 0) throw std::invalid_argument("the first offset must be 0");
+    Packing p;
+    p.n_seqs = n_seqs;
+    for (int s = 0; s < n_seqs; ++s) {
+        if (offsets[s + 1] < offsets[s]) throw std::invalid_argument("offset " + std::to_string(s + 1) + " is smaller than the one before it");
+        p.max_len = std::max(p.max_len, offsets[s + 1] - offsets[s]);
+    }
+    p.rows = offsets[n_seqs];
+    p.dtype = dtype;
+    p.data.assign(offsets, offsets + n_seqs + 1);
+    p.data.resize((p.data.size() + 3) / 4 * 4, 0);
+    if (H == 0 && Hkv == 0 && dh == 0) return p;
+    if (dtype != TIO_PREC_FP32 && dtype != TIO_PREC_BF16) throw std::invalid_argument("unknown element type");
+    if (dh != 32 && dh != 64 && dh != 128) throw std::invalid_argument("head dimension must be 32, 64 or 128");
+    if (H < 1 || Hkv < 1 || H % Hkv) throw std::invalid_argument("the query heads must be a multiple of the key heads");
+    if (H / Hkv > 64) throw std::invalid_argument("at most 64 query heads to a key head");
+    if (H > 65536) throw std::invalid_argument("too many heads");
+    if ((int64_t)p.rows * H >= ((int64_t)1 << 31)) throw std::invalid_argument("rows times heads must stay below 2^31");
+    p.H = (int32_t)H, p.Hkv = (int32_t)Hkv, p.dh = (int32_t)dh;
+    p.mfma = dtype == TIO_PREC_BF16 && dh != 32;
+    const int group = p.group();
+    if (!p.mfma) {                                   // every query head by itself
+        p.fwd_rows = p.dq_rows = p.keys = 32;
+        p.fwd = p.dq = query_items(p, offsets, 32, 1);
+        key_items(p, offsets, 32, 32, (int64_t)1 << 40);
+        return p;
+    }
+    p.fwd_rows = query_blocks(p, offsets, 64, group) * Hkv <= (dh == 64 ? 1280 : 1024) ? 64 : 128;
+    p.dq_rows = 128;
+    p.fwd = query_items(p, offsets, p.fwd_rows, group);
+    p.dq = p.fwd_rows == p.dq_rows ? p.fwd : query_items(p, offsets, p.dq_rows, group);
+    p.keys = dh == 64 ? 128 : 256;
+    const int per_tile = rows_per_tile(true, group), per_cu = dh == 64 ? 3 : 1;
+    int64_t tiles = 0;
+    for (int s = 0; s < n_seqs; ++s)
+        for (int64_t left = offsets[s + 1] - offsets[s]; left > 0; left -= p.keys) tiles += (left + per_tile - 1) / per_tile;
+    key_items(p, offsets, p.keys, per_tile, std::max<int64_t>(8, (tiles * Hkv + COMPUTE_UNITS * per_cu - 1) / (COMPUTE_UNITS * per_cu)));
+    return p;
+}
+
+}  // namespace tio

@@ -1,0 +1,184 @@
+"""GPU: causal attention over packed sequences with grouped heads, against the definition in 64 bits element by element."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+def _inputs(lens, H, Hkv, dh, dtype, gain=1.0, seed=0):
+    from synth import to_bf16_round
+    rng = np.random.default_rng(sum(lens) * 131 + H * 17 + Hkv + dh + seed)
+    qkv = rng.standard_normal((sum(lens), (H + 2 * Hkv) * dh)).astype(np.float32)
+    qkv[:, :(H + Hkv) * dh] *= gain
+    dO = rng.standard_normal((sum(lens), H * dh)).astype(np.float32)
+    return (to_bf16_round(qkv), to_bf16_round(dO)) if dtype == "bf16" else (qkv, dO)
+
+
+def _check(lens, dtype, H, Hkv, dh, gain=1.0, **more):
+    import packedlib as pl
+    print(f"packed attention {dtype} lens={lens} H={H} Hkv={Hkv} dh={dh} gain={gain} {more}", flush=True)
+    qkv, dO = _inputs(lens, H, Hkv, dh, dtype, gain)
+    u = 2.0 ** -8 if dtype == "bf16" else 1e-5              # fp32: sums of up to a few thousand terms in 32 bits
+    o, lse, d, ob, db = pl.attention(lens, H, Hkv, dh, qkv, dO, u)
+    got = pl.run_attention(lens, dtype, H, Hkv, dh, qkv, dO, **more)
+    err = np.abs(got[0].double().cpu().numpy() - o)
+    assert np.all(err <= ob + 1e-30), ("o", float((err / (ob + 1e-30)).max()))
+    # products of up to 128 terms and sums of exponentials in 32 bits: relative to the scores' size
+    assert np.abs(got[1].double().cpu().numpy() - lse).max() <= 2e-5 * (1 + np.abs(lse).max())
+    # where the reference and its bound vanish (one row: dQ, dK), dP - delta is what the rounding of O leaves of two equal sums
+    err = np.abs(got[2].double().cpu().numpy() - d)
+    at = np.unravel_index(np.argmax(err / (db + 1e-30)), err.shape)
+    assert np.all(err <= db + 1e-30), ("dqkv", at, float(err[at]), float(db[at]))
+    print("  worst error / bound", float((err / (db + 1e-30)).max()), flush=True)
+
+
+LENS = [1, 45, 0, 17, 33, 64, 65, 130]
+
+
+@pytest.mark.parametrize("H,Hkv", [(1, 1), (4, 2), (6, 2), (8, 2), (5, 1), (7, 1), (8, 8), (16, 2), (13, 1), (9, 3), (32, 1), (33, 1), (64, 1)])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_groups(H, Hkv, dh):
+    _check(LENS, "bf16", H, Hkv, dh)
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,dh", [("fp32", 4, 2, 32), ("fp32", 3, 1, 64), ("fp32", 2, 2, 128), ("fp32", 8, 1, 32), ("bf16", 4, 1, 32), ("bf16", 6, 6, 32)])
+@pytest.mark.parametrize("lens", [LENS, [1], [32], [33, 31], [200, 0, 1]])
+def test_fp32_arithmetic(dtype, H, Hkv, dh, lens):
+    _check(lens, dtype, H, Hkv, dh)
+
+
+# one row; ends of tiles of 32 and 64 keys and of blocks of 64, 128 and 256 rows, alone and behind one another
+@pytest.mark.parametrize("lens", [[1], [2], [1, 1, 1], [31], [32], [63], [64, 64], [127, 1, 128], [129], [255], [256, 257], [321, 320], [0, 0, 5, 0]])
+@pytest.mark.parametrize("H,Hkv,dh", [(4, 1, 64), (3, 3, 64), (6, 2, 128), (8, 2, 128)])
+def test_ends_of_tiles_and_blocks(lens, H, Hkv, dh):
+    _check(lens, "bf16", H, Hkv, dh)
+
+
+# blocks of keys whose tiles are shared by several workgroups; many heads, so that a wavefront has 32 query rows instead of 16
+@pytest.mark.parametrize("lens,H,Hkv,dh", [([1500], 4, 1, 64), ([900, 40], 6, 2, 128), ([1111, 700], 5, 1, 128), ([1024], 2, 2, 64),
+                                           ([700, 650, 30, 512], 48, 8, 64), ([600, 555, 800], 40, 10, 128), ([2048], 7, 1, 64)])
+def test_long_and_many(lens, H, Hkv, dh):
+    _check(lens, "bf16", H, Hkv, dh)
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("H,Hkv", [(4, 1), (3, 1)])
+def test_scores_whose_maximum_keeps_rising(dh, H, Hkv):
+    """Scores of +-50: the softmax's reference exponent is raised many times and by more than the range it tolerates."""
+    _check([300, 33, 170], "bf16", H, Hkv, dh, gain=4.0)
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 64), ("bf16", 128), ("bf16", 32), ("fp32", 32), ("fp32", 64)])
+def test_strides_and_rows_behind_the_last_sequence(dtype, dh):
+    """Columns behind the heads and rows behind the batch hold NaN where they are read from, and keep what they held where they are not written."""
+    _check([70, 3, 131], dtype, 6, 2, dh, extra_rows=40, pad=24, pad_o=8)
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,dh", [("bf16", 4, 2, 64), ("bf16", 6, 2, 128), ("bf16", 4, 1, 32), ("fp32", 4, 2, 32), ("fp32", 2, 1, 64)])
+def test_sequences_do_not_see_each_other(dtype, H, Hkv, dh):
+    """Every other sequence NaN: the rest has the bits that it has alone."""
+    import torch
+    import packedlib as pl
+    lens = [50, 64, 7, 129, 300, 31]
+    print(f"packed attention beside NaN {dtype} H={H} Hkv={Hkv} dh={dh}", flush=True)
+    qkv, dO = _inputs(lens, H, Hkv, dh, dtype)
+    off = pl.offsets(lens)
+    for bad in range(2):
+        x, g = qkv.copy(), dO.copy()
+        for i in range(bad, len(lens), 2):
+            x[off[i]:off[i + 1]] = np.nan
+            g[off[i]:off[i + 1]] = np.nan
+        o, lse, d = pl.run_attention(lens, dtype, H, Hkv, dh, x, g)
+        for i in range(1 - bad, len(lens), 2):
+            r = slice(off[i], off[i + 1])
+            a = pl.run_attention([lens[i]], dtype, H, Hkv, dh, qkv[r], dO[r])
+            assert torch.isfinite(d[r]).all()
+            assert torch.equal(o[r], a[0]) and torch.equal(lse[:, r], a[1])
+            # blocks of keys may be cut differently: their sums are then in another order
+            assert torch.equal(d[r][:, :H * dh], a[2][:, :H * dh])
+
+
+@pytest.mark.parametrize("H,Hkv,dh", [(4, 2, 64), (3, 1, 64), (8, 2, 128), (5, 1, 128)])
+def test_gradients_of_keys_at_minus_infinity(H, Hkv, dh):
+    """A key whose scores are all -inf takes part in nothing: the gradients are those of a key far below every other.  The forward pass
+    rescales at other tiles then, which changes the rounding of probabilities, their gradients and the outputs to bf16: 2^-8 each."""
+    import torch
+    import packedlib as pl
+    lens = [50, 333, 64, 1, 129]
+    qkv, dO = _inputs(lens, H, Hkv, dh, "bf16")
+    off = pl.offsets(lens)
+    x = qkv.reshape(-1, H + 2 * Hkv, dh)
+    x[:, :H, 5] = np.abs(x[:, :H, 5]) + 0.25
+    keys = [int(r) for a, n in zip(off, lens) if n > 4 for r in (a + 1, a + n // 2, a + n - 1)]
+
+    def run(value):
+        y = x.copy()
+        y[keys, H:H + Hkv, 5] = value
+        return pl.run_attention(lens, "bf16", H, Hkv, dh, y.reshape(len(y), -1), dO)
+    low, far = run(-np.inf), run(-1e30)
+    for name, a, b in (("o", low[0], far[0]), ("lse", low[1], far[1]), ("dk, dv", low[2][:, H * dh:], far[2][:, H * dh:])):
+        assert torch.isfinite(a).all(), name
+        a, b = a.double(), b.double()
+        assert ((a - b).norm() <= 3 * 2.0 ** -8 * b.norm()).item(), name
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,dh", [("bf16", 4, 2, 64), ("bf16", 5, 1, 128), ("fp32", 4, 2, 32)])
+def test_gradients_against_differences(dtype, H, Hkv, dh):
+    """Directional differences of the forward pass's own log-sum-exp and output in fp32-readable steps: the gradient of sum(w * o) along a random
+    direction against (f(x + t v) - f(x - t v)) / 2 t of the definition in 64 bits, from the kernel's gradient."""
+    import packedlib as pl
+    lens = [40, 1, 77]
+    qkv, dO = _inputs(lens, H, Hkv, dh, dtype)
+    v = np.random.default_rng(5).standard_normal(qkv.shape)
+    t = 1e-5
+    f = [float((pl.attention(lens, H, Hkv, dh, qkv.astype(np.float64) + s * t * v, dO, 0.0)[0] * dO).sum()) for s in (1, -1)]
+    got = pl.run_attention(lens, dtype, H, Hkv, dh, qkv, dO)[2].double().cpu().numpy()
+    bound = pl.attention(lens, H, Hkv, dh, qkv, dO, 2.0 ** -8 if dtype == "bf16" else 1e-5)[4]
+    assert abs((f[0] - f[1]) / (2 * t) - (got * v).sum()) <= np.sqrt((bound * v) ** 2).sum() * 0.1 + 1e-4
+
+
+def test_same_bits_again_and_on_another_stream():
+    import torch
+    import packedlib as pl
+    lens, H, Hkv, dh = [900, 33, 257], 6, 2, 64
+    qkv, dO = _inputs(lens, H, Hkv, dh, "bf16")
+    first = pl.run_attention(lens, "bf16", H, Hkv, dh, qkv, dO)
+    s = torch.cuda.Stream()
+    again = pl.run_attention(lens, "bf16", H, Hkv, dh, qkv, dO, stream=s.cuda_stream)
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,dh", [("bf16", 6, 2, 64), ("bf16", 8, 2, 128), ("fp32", 4, 2, 32)])
+def test_captured_and_replayed(dtype, H, Hkv, dh):
+    """Forward and backward in a graph, replayed on new inputs with eager work in between: the eager bits every time."""
+    import torch
+    import paper_2506_06472_amd as tio
+    import packedlib as pl
+    lens = [700, 1, 65, 128]
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    p, dev = packed = pl.packing(lens, dtype, H, Hkv, dh)
+    qkv, dO = (torch.zeros((sum(lens), n * dh), device="cuda", dtype=t) for n in (H + 2 * Hkv, H))
+    o, dqkv, lse = torch.zeros_like(dO), torch.zeros_like(qkv), torch.zeros((H, sum(lens)), device="cuda")
+    work = torch.zeros(tio.tio_op_attention_packed_work(p), device="cuda", dtype=torch.uint8)
+
+    def call(stream):
+        tio.tio_op_attention_packed(stream, p, dev.data_ptr(), qkv.data_ptr(), qkv.stride(0), o.data_ptr(), o.stride(0), lse.data_ptr())
+        tio.tio_op_attention_packed_bwd(stream, p, dev.data_ptr(), qkv.data_ptr(), qkv.stride(0), o.data_ptr(), dO.data_ptr(), o.stride(0),
+                                        lse.data_ptr(), work.data_ptr(), dqkv.data_ptr())
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        call(s.cuda_stream)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        call(torch.cuda.current_stream().cuda_stream)
+    for seed in range(3):
+        a, b = _inputs(lens, H, Hkv, dh, dtype, seed=seed)
+        qkv.copy_(torch.from_numpy(a))
+        dO.copy_(torch.from_numpy(b))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = pl.run_attention(lens, dtype, H, Hkv, dh, a, b, packed=packed)
+        for name, x, y in zip(("o", "lse", "dqkv"), (o, lse, dqkv), eager):
+            assert torch.equal(x, y), (seed, name)

@@ -1,0 +1,216 @@
+"""GPU: activations kept in eight bits, and the activations whose gradients come from them, against the definitions in 64 bits."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+def _types(dtype):
+    import torch
+    return torch.bfloat16 if dtype == "bf16" else torch.float32
+
+
+def _padded(a, dtype, fill, extra=8):
+    """[rows, cols] on the GPU in rows of the next multiple of eight and `extra` more, which hold `fill`; and the tensor's stride"""
+    import torch
+    rows, cols = a.shape
+    ld = (cols + 7) // 8 * 8 + extra
+    t = torch.full((rows, ld), fill, device="cuda", dtype=_types(dtype))
+    t[:, :cols] = torch.from_numpy(np.ascontiguousarray(a)).cuda().to(t.dtype)
+    return t, ld
+
+
+def _values(rows, cols, dtype, seed=0, scale=1.0):
+    from synth import to_bf16_round
+    rng = np.random.default_rng(rows * 1000 + cols + seed)
+    x = (rng.standard_normal((rows, cols)) * scale * np.exp2(rng.integers(-6, 7, (rows, 1)))).astype(np.float32)
+    return to_bf16_round(x) if dtype == "bf16" else x
+
+
+def _round_trip(x, dtype):
+    """The values read back from a checkpoint of x; nothing else is written."""
+    import torch
+    import paper_2506_06472_amd as tio
+    rows, cols = x.shape
+    t, ld = _padded(x, dtype, float("nan"))
+    need = tio.tio_ckpt8_bytes(rows, cols)
+    kept = torch.full((need + 64,), 77, device="cuda", dtype=torch.uint8)
+    out = torch.full_like(t, 7.0)
+    torch.cuda.synchronize()
+    tio.tio_op_ckpt8_store(0, dtype, rows, cols, t.data_ptr(), ld, kept.data_ptr())
+    tio.tio_op_ckpt8_load(0, dtype, rows, cols, kept.data_ptr(), out.data_ptr(), ld)
+    torch.cuda.synchronize()
+    up = (cols + 7) // 8 * 8
+    assert (kept[need:] == 77).all() and (out[:, up:] == 7.0).all() and (out[:, cols:up] == 0.0).all()
+    return out[:, :cols].double().cpu().numpy()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 8), (1, 31), (2, 32), (3, 33), (5, 40), (7, 100), (64, 64), (9, 257), (1021, 273), (4096, 96)])
+def test_round_trip(dtype, rows, cols):
+    import packedlib as pl
+    print(f"checkpoint {dtype} {rows} x {cols}", flush=True)
+    x = _values(rows, cols, dtype)
+    assert np.array_equal(_round_trip(x, dtype), pl.kept_values(x))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_round_trip_of_special_values(dtype):
+    """Zeros, ties, the clamp, subnormal and huge magnitudes, blocks that are not finite: the definition's values, exactly."""
+    import packedlib as pl
+    x = np.zeros((12, 64), np.float32)
+    x[1, :32] = np.arange(32) * 2.0 + 0.5                                  # ties at a step of one
+    x[1, 31] = 64.0
+    x[2, 0], x[2, 1] = 127.5, -127.5                                       # would round to 128
+    x[2, 32:] = -np.linspace(1, 127, 32)
+    x[3] = 3.3e38
+    x[3, 5] = -1e30
+    x[4] = 1e-39                                                           # subnormal
+    x[5, 7], x[5, 40] = 2.0 ** -120, 2.0 ** -127
+    x[6, 3] = np.inf
+    x[7, 35] = np.nan
+    x[8, 63], x[8, 0] = -np.inf, 1.0
+    x[9] = np.exp2(np.arange(64) - 32.0)                                   # powers of two up to the block's largest
+    x[10, 0], x[10, 1:32] = 1.9999999, -0.0
+    x[11, 33] = -2.0 ** -119
+    if dtype == "bf16":
+        from synth import to_bf16_round
+        with np.errstate(all="ignore"):
+            fine = np.isfinite(x)
+            x = np.where(fine, to_bf16_round(np.where(fine, x, 0)), x)
+    got, want = _round_trip(x, dtype), pl.kept_values(x)
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    assert np.array_equal(np.nan_to_num(got, nan=5.0), np.nan_to_num(want, nan=5.0))
+
+
+def _sigmoid(z):
+    e = np.exp(-np.abs(z))
+    return np.where(z >= 0, 1 / (1 + e), e / (1 + e))
+
+
+A, B = 2 * np.sqrt(2 / np.pi), 0.044715
+
+
+def _act(act, g, u):
+    """The output, the gradients of g and u for dy = 1, and how far 32-bit arithmetic may be off, less the result's rounding.
+
+    The logistic function's argument z has a relative error of four roundings (2^-24 each), that is 4 |z| 2^-24 of the function, and the
+    exponential, reciprocal or division some more; products add a rounding each.  Below 2^-126 the function may be zero (the hardware's
+    reciprocal has no subnormal results): an error of 2^-126 of it, of g times as much of g s."""
+    e, least = 2.0 ** -24, 2.0 ** -126
+    if act == "gelu":
+        z = A * (g + B * g ** 3)
+        s, q = _sigmoid(z), A * (1 + 3 * B * g * g)
+    else:
+        z, s, q = g, _sigmoid(g), np.ones_like(g)
+    d = (4 * np.abs(z) + 16) * e
+    y, grad = g * s, s + g * s * (1 - s) * q
+    of_y = np.abs(y) * (d + 2 * e) + np.abs(g) * least
+    near = s * d + np.abs(g * s * q) * ((1 - s) * (d + 16 * e) + s * d + e) + (1 + np.abs(g * q)) * least
+    if act == "gelu":
+        return y, grad, None, of_y, near, None
+    return y * u, u * grad, y, np.abs(u) * (of_y + np.abs(y) * e), np.abs(u) * (near + np.abs(grad) * 2 * e), of_y
+
+
+@pytest.mark.parametrize("act", ["gelu", "swiglu"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,f,again", [(1, 1, True), (2, 8, True), (3, 33, False), (128, 512, True), (37, 273, True), (300, 136, False), (1021, 41, True)])
+def test_activation(act, dtype, rows, f, again):
+    import torch
+    import paper_2506_06472_amd as tio
+    import packedlib as pl
+    print(f"{act} with a checkpoint {dtype} {rows} x {f}", flush=True)
+    two = act == "swiglu"
+    g, u, dy = _values(rows, f, dtype, 1), _values(rows, f, dtype, 2), _values(rows, f, dtype, 3, 1e-2)
+    tg, ld = _padded(g, dtype, float("nan"))
+    tu, _ = _padded(u, dtype, float("nan"))
+    td, ldd = _padded(dy, dtype, float("nan"), 16)
+    need = tio.tio_ckpt8_bytes(rows, f)
+    kept = torch.full((need * (2 if two else 1) + 64,), 77, device="cuda", dtype=torch.uint8)
+    y, dg, du, y2 = (torch.full_like(t, 7.0) for t in (td, tg, tu, td))
+    ptr = lambda t: t.data_ptr() if two else 0
+    torch.cuda.synchronize()
+    tio.tio_op_act_ckpt8(0, dtype, act, rows, f, tg.data_ptr(), ptr(tu), ld, y.data_ptr(), ldd, kept.data_ptr())
+    tio.tio_op_act_ckpt8_bwd(0, dtype, act, rows, f, kept.data_ptr(), td.data_ptr(), ldd, dg.data_ptr(), ptr(du), ld, y2.data_ptr() if again else 0, ldd)
+    torch.cuda.synchronize()
+    half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    up = (f + 7) // 8 * 8
+    assert (kept[len(kept) - 64:] == 77).all()
+    tiny = 2.0 ** -126                                     # below the normal numbers of 32 bits results have fewer bits
+
+    def near(t, want, bound, name):
+        got = t[:, :f].double().cpu().numpy()
+        lim = bound + half * (np.abs(want) + bound) + tiny
+        assert np.all(np.abs(got - want) <= lim), (name, float((np.abs(got - want) / lim).max()))
+        assert (t[:, up:] == 7.0).all(), name
+    G, U = g.astype(np.float64), u.astype(np.float64)
+    out = _act(act, G, U)
+    near(y, out[0], out[3], "y")
+    kg, ku = pl.kept_values(G), pl.kept_values(U)
+    out = _act(act, kg, ku)
+    D = dy.astype(np.float64)
+    near(dg, D * out[1], np.abs(D) * out[4] + 2.0 ** -24 * np.abs(D * out[1]), "dgate")
+    if two:
+        near(du, D * out[2], np.abs(D) * out[5] + 2.0 ** -24 * np.abs(D * out[2]), "dup")
+    else:
+        assert (du == 7.0).all()
+    if again:
+        near(y2, out[0], out[3], "y again")
+    else:
+        assert (y2 == 7.0).all()
+    # the checkpoint is one of each input, which load reads
+    for i, k in enumerate((kg, ku)[:2 if two else 1]):
+        x = torch.full_like(tg, 7.0)
+        tio.tio_op_ckpt8_load(0, dtype, rows, f, kept.data_ptr() + i * need, x.data_ptr(), ld)
+        torch.cuda.synchronize()
+        assert np.array_equal(x[:, :f].double().cpu().numpy(), k)
+
+
+@pytest.mark.parametrize("act", ["gelu", "swiglu"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_activation_gradient_against_differences(act, dtype):
+    """The gradient at the values the checkpoint stands for, against central differences of the definition there."""
+    import torch
+    import paper_2506_06472_amd as tio
+    import packedlib as pl
+    rows, f = 8, 64
+    g, u = _values(rows, f, dtype, 5) * 0.25, _values(rows, f, dtype, 6) * 0.25
+    one = np.ones((rows, f), np.float32)
+    (tg, ld), (tu, _), (td, _) = (_padded(a, dtype, 0.0) for a in (g, u, one))
+    two = act == "swiglu"
+    kept = torch.zeros(2 * tio.tio_ckpt8_bytes(rows, f), device="cuda", dtype=torch.uint8)
+    y, dg, du = (torch.zeros_like(tg) for _ in range(3))
+    tio.tio_op_act_ckpt8(0, dtype, act, rows, f, tg.data_ptr(), tu.data_ptr() if two else 0, ld, y.data_ptr(), ld, kept.data_ptr())
+    tio.tio_op_act_ckpt8_bwd(0, dtype, act, rows, f, kept.data_ptr(), td.data_ptr(), ld, dg.data_ptr(), du.data_ptr() if two else 0, ld)
+    torch.cuda.synchronize()
+    kg, ku = pl.kept_values(g), pl.kept_values(u)
+    t = 1e-5
+    diff = (_act(act, kg + t, ku)[0] - _act(act, kg - t, ku)[0]) / (2 * t)
+    half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -20
+    got = dg[:, :f].double().cpu().numpy()
+    assert np.all(np.abs(got - diff) <= half * np.abs(diff) + 1e-5 * (1 + np.abs(ku)))          # differences: t^2 and 1e-16 / t
+    if two:
+        diff = (_act(act, kg, ku + t)[0] - _act(act, kg, ku - t)[0]) / (2 * t)
+        assert np.all(np.abs(du[:, :f].double().cpu().numpy() - diff) <= half * np.abs(diff) + 1e-5 * (1 + np.abs(kg)))
+
+
+def test_activation_of_extreme_inputs():
+    """Large magnitudes of either sign: the logistic function's ends, no NaN; an infinite input makes its block's gradients NaN."""
+    import torch
+    import paper_2506_06472_amd as tio
+    for dtype in ("bf16", "fp32"):
+        for act in ("gelu", "swiglu"):
+            x = np.zeros((2, 64), np.float32)
+            x[0, :8] = [1e4, -1e4, 100.0, -100.0, 1e8, -1e8, 0.0, -30.0]
+            x[1, 40] = np.inf
+            t, ld = _padded(x, dtype, 0.0)
+            one, _ = _padded(np.ones_like(x), dtype, 0.0)
+            kept = torch.zeros(2 * tio.tio_ckpt8_bytes(2, 64), device="cuda", dtype=torch.uint8)
+            y, dg, du = (torch.zeros_like(t) for _ in range(3))
+            two = act == "swiglu"
+            tio.tio_op_act_ckpt8(0, dtype, act, 2, 64, t.data_ptr(), one.data_ptr() if two else 0, ld, y.data_ptr(), ld, kept.data_ptr())
+            tio.tio_op_act_ckpt8_bwd(0, dtype, act, 2, 64, kept.data_ptr(), one.data_ptr(), ld, dg.data_ptr(), du.data_ptr() if two else 0, ld)
+            torch.cuda.synchronize()
+            assert torch.isfinite(y[0]).all() and torch.isfinite(dg[0]).all()
+            assert y[0, 1] == 0 and y[0, 5] == 0 and y[0, 0] == t[0, 0] and y[1, 40] == float("inf")
+            assert torch.isnan(dg[1, 32:64]).all() and torch.isfinite(dg[1, :32]).all()

@@ -100,6 +100,14 @@ class PackingView(C.Structure):
 
 
 _lib = None
+# Argument types of the operators on packed batches and 8-bit checkpoints (p: pointer, i: int32, l: int64, f: float), declared once: their smallest calls take
+# a few microseconds on the GPU, and an object for each argument of a call took as long (GELU of 128 x 512 with its gradient, two calls: 16.1 -> 8.6 us).
+_KINDS = {"p": C.c_void_p, "i": C.c_int32, "l": C.c_int64, "f": C.c_float}
+_SIGNATURES = {
+    "tio_op_attention_packed": "ppppl" "plp", "tio_op_attention_packed_bwd": "ppppl" "pplppp",
+    "tio_op_preference_loss": "pipplplppfflppppp", "tio_op_ckpt8_store": "pillplp", "tio_op_ckpt8_load": "pillppl",
+    "tio_op_act_ckpt8": "piillpplplp", "tio_op_act_ckpt8_bwd": "piillpplpplpl",
+}
 
 
 def lib():
@@ -116,6 +124,8 @@ def lib():
         for name in ("tio_trace_free", "tio_lifetimes_free", "tio_plan_free", "tio_packing_free"):
             getattr(_lib, name).restype = None
             getattr(_lib, name).argtypes = [C.c_void_p]
+        for name, kinds in _SIGNATURES.items():
+            getattr(_lib, name).argtypes = [_KINDS[k] for k in kinds]
     return _lib
 
 
@@ -516,14 +526,11 @@ def tio_packing_build(offsets, dtype="bf16", H=0, Hkv=0, dh=0) -> Packing:
     return Packing(h)
 
 
-def _vp(p):
-    return C.c_void_p(p) if p else None
-
-
+# Raw pointers (ints, 0 for none) of device buffers here and below; see include/teraio.h.
 def tio_op_attention_packed(stream_handle, packing, packing_ptr, qkv_ptr, ld_qkv, o_ptr, ld_o, lse_ptr):
-    """Raw pointers (ints) of device buffers here and below; see include/teraio.h."""
-    _check(lib().tio_op_attention_packed(_vp(stream_handle), packing.h, _vp(packing_ptr), _vp(qkv_ptr), C.c_int64(ld_qkv), _vp(o_ptr), C.c_int64(ld_o),
-                                         _vp(lse_ptr)))
+    rc = lib().tio_op_attention_packed(stream_handle, packing.h, packing_ptr, qkv_ptr, ld_qkv, o_ptr, ld_o, lse_ptr)
+    if rc:
+        _check(rc)
 
 
 def tio_op_attention_packed_work(packing) -> int:
@@ -533,8 +540,9 @@ def tio_op_attention_packed_work(packing) -> int:
 
 
 def tio_op_attention_packed_bwd(stream_handle, packing, packing_ptr, qkv_ptr, ld_qkv, o_ptr, dO_ptr, ld_o, lse_ptr, work_ptr, dqkv_ptr):
-    _check(lib().tio_op_attention_packed_bwd(_vp(stream_handle), packing.h, _vp(packing_ptr), _vp(qkv_ptr), C.c_int64(ld_qkv), _vp(o_ptr), _vp(dO_ptr),
-                                             C.c_int64(ld_o), _vp(lse_ptr), _vp(work_ptr), _vp(dqkv_ptr)))
+    rc = lib().tio_op_attention_packed_bwd(stream_handle, packing.h, packing_ptr, qkv_ptr, ld_qkv, o_ptr, dO_ptr, ld_o, lse_ptr, work_ptr, dqkv_ptr)
+    if rc:
+        _check(rc)
 
 
 def tio_op_preference_loss_work(packing) -> int:
@@ -545,9 +553,10 @@ def tio_op_preference_loss_work(packing) -> int:
 
 def tio_op_preference_loss(stream_handle, dtype, packing, packing_ptr, V, logits_ptr, ld, labels_ptr, ref_logp_ptr, beta, smoothing, seq_logp_ptr,
                            losses_ptr, loss_ptr, work_ptr, dlogits_ptr=0, total_pairs=0):
-    _check(lib().tio_op_preference_loss(_vp(stream_handle), PREC[dtype], packing.h, _vp(packing_ptr), C.c_int64(V), _vp(logits_ptr), C.c_int64(ld),
-                                        _vp(labels_ptr), _vp(ref_logp_ptr), C.c_float(beta), C.c_float(smoothing), C.c_int64(total_pairs),
-                                        _vp(seq_logp_ptr), _vp(losses_ptr), _vp(loss_ptr), _vp(work_ptr), _vp(dlogits_ptr)))
+    rc = lib().tio_op_preference_loss(stream_handle, PREC[dtype], packing.h, packing_ptr, V, logits_ptr, ld, labels_ptr, ref_logp_ptr, beta, smoothing,
+                                      total_pairs, seq_logp_ptr, losses_ptr, loss_ptr, work_ptr, dlogits_ptr)
+    if rc:
+        _check(rc)
 
 
 def tio_ckpt8_bytes(rows, cols) -> int:
@@ -557,18 +566,24 @@ def tio_ckpt8_bytes(rows, cols) -> int:
 
 
 def tio_op_ckpt8_store(stream_handle, dtype, rows, cols, x_ptr, ldx, ckpt_ptr):
-    _check(lib().tio_op_ckpt8_store(_vp(stream_handle), PREC[dtype], C.c_int64(rows), C.c_int64(cols), _vp(x_ptr), C.c_int64(ldx), _vp(ckpt_ptr)))
+    rc = lib().tio_op_ckpt8_store(stream_handle, PREC[dtype], rows, cols, x_ptr, ldx, ckpt_ptr)
+    if rc:
+        _check(rc)
 
 
 def tio_op_ckpt8_load(stream_handle, dtype, rows, cols, ckpt_ptr, x_ptr, ldx):
-    _check(lib().tio_op_ckpt8_load(_vp(stream_handle), PREC[dtype], C.c_int64(rows), C.c_int64(cols), _vp(ckpt_ptr), _vp(x_ptr), C.c_int64(ldx)))
+    rc = lib().tio_op_ckpt8_load(stream_handle, PREC[dtype], rows, cols, ckpt_ptr, x_ptr, ldx)
+    if rc:
+        _check(rc)
 
 
 def tio_op_act_ckpt8(stream_handle, dtype, act, rows, f, gate_ptr, up_ptr, ldu, y_ptr, ldy, ckpt_ptr):
-    _check(lib().tio_op_act_ckpt8(_vp(stream_handle), PREC[dtype], ACT[act], C.c_int64(rows), C.c_int64(f), _vp(gate_ptr), _vp(up_ptr), C.c_int64(ldu),
-                                  _vp(y_ptr), C.c_int64(ldy), _vp(ckpt_ptr)))
+    rc = lib().tio_op_act_ckpt8(stream_handle, PREC[dtype], ACT[act], rows, f, gate_ptr, up_ptr, ldu, y_ptr, ldy, ckpt_ptr)
+    if rc:
+        _check(rc)
 
 
 def tio_op_act_ckpt8_bwd(stream_handle, dtype, act, rows, f, ckpt_ptr, dy_ptr, lddy, dgate_ptr, dup_ptr, ldu, y_ptr=0, ldy=0):
-    _check(lib().tio_op_act_ckpt8_bwd(_vp(stream_handle), PREC[dtype], ACT[act], C.c_int64(rows), C.c_int64(f), _vp(ckpt_ptr), _vp(dy_ptr), C.c_int64(lddy),
-                                      _vp(dgate_ptr), _vp(dup_ptr), C.c_int64(ldu), _vp(y_ptr), C.c_int64(ldy)))
+    rc = lib().tio_op_act_ckpt8_bwd(stream_handle, PREC[dtype], ACT[act], rows, f, ckpt_ptr, dy_ptr, lddy, dgate_ptr, dup_ptr, ldu, y_ptr, ldy)
+    if rc:
+        _check(rc)

@@ -115,7 +115,7 @@ struct PreferenceArgs {
     float *seq, *losses, *loss;
     void *work, *dlogits;                        // dlogits: nullptr for the loss alone
 };
-int64_t preference_work(int64_t rows);
+int64_t preference_work(int64_t rows, int64_t pairs);
 void preference_loss(hipStream_t s, int dtype, const PreferenceArgs &a);
 // ---- activations in eight bits (kernels_ckpt8.hip)
 bool ckpt8_fits(int64_t rows, int64_t cols);

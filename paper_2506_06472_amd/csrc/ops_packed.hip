@@ -128,7 +128,7 @@ int tio_op_attention_packed_bwd(void *stream, const tio_packing *packing, const 
 
 int tio_op_preference_loss_work(const tio_packing *packing, uint64_t *out_bytes) {
     if (!packing || !out_bytes) return fail(TIO_ERR_INVALID_ARG, "null argument");
-    *out_bytes = (uint64_t)k::preference_work(packing->p.rows);
+    *out_bytes = (uint64_t)k::preference_work(packing->p.rows, (packing->p.n_seqs + 1) / 2);
     return TIO_OK;
 }
 

@@ -101,7 +101,7 @@ class PackingView(C.Structure):
 
 _lib = None
 # Argument types of the operators on packed batches and 8-bit checkpoints (p: pointer, i: int32, l: int64, f: float), declared once: their smallest calls take
-# a few microseconds on the GPU, and an object for each argument of a call took as long (GELU of 128 x 512 with its gradient, two calls: 16.1 -> 8.6 us).
+# a few microseconds on the GPU, and an object for each argument costs 0.4 us of the 3.7 that a call takes the host.
 _KINDS = {"p": C.c_void_p, "i": C.c_int32, "l": C.c_int64, "f": C.c_float}
 _SIGNATURES = {
     "tio_op_attention_packed": "ppppl" "plp", "tio_op_attention_packed_bwd": "ppppl" "pplppp",
@@ -503,7 +503,7 @@ class Packing:
         self.h = handle
 
     def __del__(self):
-        if getattr(self, "h", None):
+        if getattr(self, "h", None) and lib is not None:     # None: the interpreter is on its way out
             lib().tio_packing_free(self.h)
             self.h = None
 

@@ -585,32 +585,41 @@ void attn_packed_fwd_f32(hipStream_t s, const Packing &p, const void *device, co
     });
 }
 
-// delta of a packed batch: a group of dh / (elements per 16 bytes) lanes to a row and head, as in attn_bwd_pre_k
+// delta of a packed batch, as attn_bwd_pre_k: dh / (elements per 16 bytes) consecutive lanes share a row and head
 template <typename T>
-__global__ void __launch_bounds__(TPB) attn_packed_pre_k(const T *__restrict__ dO, const T *__restrict__ O, int64_t ldo, float *__restrict__ delta, int64_t rows,
-                                                         int H, int dh) {
+__global__ void __launch_bounds__(TPB) attn_packed_pre_k(const T *__restrict__ dO, const T *__restrict__ O, int64_t ldo, float *__restrict__ delta,
+                                                         uint32_t rows, uint32_t H, uint32_t lanes) {
     constexpr int V = Vec16<T>::N;
-    const int lanes = dh / V, of_block = TPB / lanes;
-    const int64_t row = blockIdx.x;
-    const int g = threadIdx.x % lanes;
-    for (int h = threadIdx.x / lanes; h < H; h += of_block) {        // all lanes of a group together
+    const int64_t idx = (int64_t)blockIdx.x * TPB + threadIdx.x;     // (row * H + h) * lanes + g
+    const uint32_t rh = (uint32_t)(idx / lanes), g = (uint32_t)idx % lanes, row = rh / H, h = rh - row * H;
+    float sum = 0.f;
+    if (row < rows) {
+        const int64_t at = row * ldo + (h * lanes + g) * V;
         Vec16<T> x, y;
-        x.load(dO + row * ldo + (int64_t)h * dh + g * V);
-        y.load(O + row * ldo + (int64_t)h * dh + g * V);
-        float fx[V], fy[V], sum = 0.f;
+        x.load(dO + at);
+        y.load(O + at);
+        float fx[V], fy[V];
         x.get(fx); y.get(fy);
 #pragma unroll
         for (int i = 0; i < V; ++i) sum = fmaf(fx[i], fy[i], sum);
-        for (int o = 1; o < lanes; o <<= 1) sum += __shfl_xor(sum, o, 64);
-        if (g == 0) delta[h * rows + row] = sum;
     }
+    for (uint32_t o = 1; o < lanes; o <<= 1) sum += __shfl_xor(sum, (int)o, 64);
+    if (row < rows && g == 0) delta[(int64_t)h * rows + row] = sum;
+}
+void attn_packed_pre(hipStream_t s, int dtype, const void *dO, const void *o, int64_t ldo, float *delta, int64_t rows, int64_t H, int64_t dh) {
+    const int64_t lanes = dh / (dtype == TIO_PREC_BF16 ? 8 : 4), n = rows * H * lanes;
+    const unsigned grid = (unsigned)((n + TPB - 1) / TPB);
+    if (dtype == TIO_PREC_BF16)
+        attn_packed_pre_k<bf16_t><<<grid, TPB, 0, s>>>((const bf16_t *)dO, (const bf16_t *)o, ldo, delta, (uint32_t)rows, (uint32_t)H, (uint32_t)lanes);
+    else
+        attn_packed_pre_k<float><<<grid, TPB, 0, s>>>((const float *)dO, (const float *)o, ldo, delta, (uint32_t)rows, (uint32_t)H, (uint32_t)lanes);
 }
 
 void attn_packed_bwd_f32(hipStream_t s, const Packing &p, const void *device, const void *qkv, int64_t ld, const void *o, const void *dO, int64_t ldo,
                          const float *lse, float *delta, void *dqkv, float scale) {
     const bool own = p.dh == 32;
+    if (!own) attn_packed_pre(s, p.dtype, dO, o, ldo, delta, p.rows, p.H, p.dh);
     TIO_ATTN_DISPATCH(p.dtype, p.dh, {
-        if (!own) attn_packed_pre_k<T><<<(unsigned)p.rows, TPB, 0, s>>>((const T *)dO, (const T *)o, ldo, delta, p.rows, p.H, p.dh);
         const PackedBlocks<T> where = packed_blocks<T>(p, device, qkv, ld, ldo);
         const BwdArgs<T, PackedBlocks<T>> a{where, (const T *)dO, own ? (const T *)o : nullptr, lse, delta, (T *)dqkv, scale};
         launch_bwd<T, DH>(s, a, where.key.grid(), where.query.grid(), p.max_len, false);

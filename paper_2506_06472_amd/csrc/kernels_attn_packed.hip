@@ -59,27 +59,24 @@ struct PackedRows {
     }
 };
 
-template <int DH, int NG>
-__global__ void __launch_bounds__(NT, DH == 64 ? 3 : 2) attn_packed_dq_mfma_k(const PackedRows where, const uint16_t *__restrict__ dO,
-                                                                              const uint16_t *__restrict__ O, const float *__restrict__ lse,
-                                                                              float *__restrict__ delta, uint16_t *__restrict__ dqkv, float scale) {
-    QueryPlace at;
-    if (!where.place<DH, NT / 64 * 16 * NG>(blockIdx.x, at)) return;
-    dq_rows<DH, NT / 64, NG, true>(at, dO + at.row, O + at.row, lse + at.stat, delta + at.stat, dqkv + (at.q - where.qkv), scale);
-}
-
-// parts: blocks of partial sums of each key head, at `partial`
+// Both gradients in one launch: the blocks of keys, then those of queries.
 template <int DH, int NW, int NG, bool TAIL>
-__global__ void __launch_bounds__(NW * 64, DH == 64 ? 3 : 2) attn_packed_dkv_mfma_k(const PackedRows where, const uint16_t *__restrict__ dO,
-                                                                                    const float *__restrict__ lse, const float *__restrict__ delta,
-                                                                                    uint16_t *__restrict__ dqkv, float *__restrict__ partial, int parts,
-                                                                                    float scale) {
-    KeyPlace at;
-    int hk, part, pieces;
-    if (!where.place<DH, NW * 16 * NG>(blockIdx.x, at, hk, part, pieces) || at.t0 >= at.t1 || part >= parts) return;
-    float *const mine = part < 0 ? nullptr : partial + ((int64_t)hk * parts + part) * key_partial<DH, NW, NG>();
-    dkv_rows<DH, NW, NG, false, true, TAIL>(at, dO + at.row, nullptr, lse + at.stat, delta + at.stat, dqkv + (at.k - where.qkv),
-                                            dqkv + (at.v - where.qkv), mine, scale);
+__global__ void __launch_bounds__(NW * 64, NG == 1 ? 2 : DH == 64 ? 3 : 2)
+    attn_packed_both_mfma_k(const PackedRows keys, const PackedRows queries, unsigned key_blocks, const uint16_t *__restrict__ dO,
+                            const float *__restrict__ lse, float *__restrict__ delta, uint16_t *__restrict__ dqkv, float *__restrict__ partial, int parts,
+                            float scale) {
+    if (blockIdx.x < key_blocks) {
+        KeyPlace at;
+        int hk, part, pieces;
+        if (!keys.place<DH, NW * 16 * NG>(blockIdx.x, at, hk, part, pieces) || at.t0 >= at.t1 || part >= parts) return;
+        float *const mine = part < 0 ? nullptr : partial + ((int64_t)hk * parts + part) * key_partial<DH, NW, NG>();
+        dkv_rows<DH, NW, NG, false, true, TAIL>(at, dO + at.row, nullptr, lse + at.stat, delta + at.stat, dqkv + (at.k - keys.qkv),
+                                                dqkv + (at.v - keys.qkv), mine, scale);
+    } else {
+        QueryPlace at;
+        if (!queries.place<DH, NW * 16 * NG>(blockIdx.x - key_blocks, at)) return;
+        dq_rows<DH, NW, NG, true>(at, dO + at.row, nullptr, lse + at.stat, delta + at.stat, dqkv + (at.q - queries.qkv), scale);
+    }
 }
 
 template <int DH, int NW, int NG>
@@ -93,7 +90,6 @@ __global__ void __launch_bounds__(NW * 64) attn_packed_sums_k(const PackedRows w
 }
 
 template <int DH> constexpr size_t fwd_smem() { return (size_t)3 * 2 * 32 * DH * 2; }      // three pairs of tiles
-template <int DH> constexpr size_t kv_smem() { return (size_t)2 * 2 * 64 * DH * 2; }       // two buffers of two tiles
 template <int DH, int NW, int NG> constexpr size_t dkv_smem() {         // tiles, V rows, then statistics
     return (size_t)2 * 2 * 64 * DH * 2 + (dkv_v_in_lds<DH, NG>() ? (size_t)NW * 16 * NG * DH * 2 : 0) + 2 * 128 * 4;
 }
@@ -109,15 +105,17 @@ template <int DH> void fwd(hipStream_t s, const Packing &p, const void *device, 
     else attn_fwd_mfma_k<DH, 2><<<w.places.grid(), NT, fwd_smem<DH>(), s>>>(w, (uint16_t *)o, lse, scale);
 }
 
-// the launches of a kind of block of keys: NW wavefronts of 16 NG keys
+// blocks of NW wavefronts of 16 NG keys or query rows
 template <int DH, int NW, int NG>
-void key_blocks(hipStream_t s, const Packing &p, const void *device, const void *qkv, int64_t ld, const void *dO, int64_t ldo, const float *lse,
-                const float *delta, float *partial, void *dqkv, float scale) {
-    const PackedRows w = rows_of(p, device, p.key, KEY_WORDS, qkv, ld, ldo);
+void both(hipStream_t s, const Packing &p, const void *device, const void *qkv, int64_t ld, const void *dO, int64_t ldo, const float *lse, float *delta,
+          float *partial, void *dqkv, float scale) {
+    const PackedRows keys = rows_of(p, device, p.key, KEY_WORDS, qkv, ld, ldo), queries = rows_of(p, device, p.dq, QUERY_WORDS, qkv, ld, ldo);
+    const unsigned key_blocks = keys.places.grid();
     auto go = [&](auto TAIL) {
-        const auto kernel = attn_packed_dkv_mfma_k<DH, NW, NG, TAIL()>;
+        const auto kernel = attn_packed_both_mfma_k<DH, NW, NG, TAIL()>;
         (void)hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)dkv_smem<DH, NW, NG>());
-        kernel<<<w.places.grid(), NW * 64, dkv_smem<DH, NW, NG>(), s>>>(w, (const uint16_t *)dO, lse, delta, (uint16_t *)dqkv, partial, p.parts, scale);
+        kernel<<<key_blocks + queries.places.grid(), NW * 64, dkv_smem<DH, NW, NG>(), s>>>(keys, queries, key_blocks, (const uint16_t *)dO, lse, delta,
+                                                                                          (uint16_t *)dqkv, partial, p.parts, scale);
     };
     if (rows_between_loads<DH, NW>() % p.group()) go(std::true_type{});
     else go(std::false_type{});
@@ -129,11 +127,9 @@ void key_blocks(hipStream_t s, const Packing &p, const void *device, const void 
 
 template <int DH> void bwd(hipStream_t s, const Packing &p, const void *device, const void *qkv, int64_t ld, const void *o, const void *dO, int64_t ldo,
                            const float *lse, float *delta, float *partial, void *dqkv, float scale) {
-    const PackedRows q = rows_of(p, device, p.dq, QUERY_WORDS, qkv, ld, ldo);
-    const auto kernel = attn_packed_dq_mfma_k<DH, 2>;
-    (void)hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kv_smem<DH>());
-    kernel<<<q.places.grid(), NT, kv_smem<DH>(), s>>>(q, (const uint16_t *)dO, (const uint16_t *)o, lse, delta, (uint16_t *)dqkv, scale);
-    key_blocks<DH, dkv_waves<DH>(), 2>(s, p, device, qkv, ld, dO, ldo, lse, delta, partial, dqkv, scale);
+    attn_packed_pre(s, TIO_PREC_BF16, dO, o, ldo, delta, p.rows, p.H, DH);
+    if (p.keys == 64) both<DH, 4, 1>(s, p, device, qkv, ld, dO, ldo, lse, delta, partial, dqkv, scale);
+    else both<DH, dkv_waves<DH>(), 2>(s, p, device, qkv, ld, dO, ldo, lse, delta, partial, dqkv, scale);
 }
 
 int64_t delta_bytes(const Packing &p) { return ((int64_t)p.H * p.rows * 4 + 255) / 256 * 256; }

@@ -13,8 +13,6 @@ namespace tio {
 
 namespace {
 
-constexpr int COMPUTE_UNITS = 256;
-
 template <typename Item> ItemList append(Packing &p, std::vector<std::pair<int64_t, Item>> &items) {
     std::stable_sort(items.begin(), items.end(), [](const auto &a, const auto &b) { return a.first > b.first; });
     ItemList l;
@@ -44,13 +42,17 @@ int64_t query_blocks(const Packing &p, const int32_t *offsets, int rows, int gro
     return n;
 }
 
+// into how many items a block of keys with that many tiles is cut
+int64_t pieces_of(int64_t tiles, int64_t piece) { return tiles > piece + piece / 4 ? (tiles + piece - 1) / piece : 1; }
+constexpr int64_t WHOLE = (int64_t)1 << 40;          // a piece that no block is larger than
+
 // Blocks of `keys` key rows.  A block whose tiles are more than a piece's is shared by several items, whose sums are added afterwards.
 void key_items(Packing &p, const int32_t *offsets, int keys, int per_tile, int64_t piece) {
     std::vector<std::pair<int64_t, KeyItem>> items, sums;
     for (int s = 0; s < p.n_seqs; ++s) {
         const int32_t first = offsets[s], len = offsets[s + 1] - first;
         for (int32_t kv0 = 0; kv0 < len; kv0 += keys) {
-            const int64_t tiles = ((int64_t)len - kv0 + per_tile - 1) / per_tile, pieces = tiles > piece + piece / 2 ? (tiles + piece - 1) / piece : 1;
+            const int64_t tiles = ((int64_t)len - kv0 + per_tile - 1) / per_tile, pieces = pieces_of(tiles, piece);
             if (pieces == 1) {
                 items.push_back({tiles, KeyItem{first, len, kv0, 0, (int32_t)tiles, -1, 0, 0}});
                 continue;
@@ -64,6 +66,60 @@ void key_items(Packing &p, const int32_t *offsets, int keys, int per_tile, int64
     }
     p.key = append(p, items);
     p.sums = append(p, sums);
+}
+
+// How the backward pass is cut: the keys of a block (64 of four wavefronts with 16 keys each; or 128 of four, head size 64, and 256 of eight,
+// head size 128, with 32 each, which do a product for half the reads but are fewer and take longer for a tile) and the tiles of a piece.
+// The time is estimated as that of the tiles, dealt evenly, or of the longest chain of them if that is longer, a quarter of the shorter of the two, and
+// the partial sums' way to memory and back.  us; fitted to 300 ways to cut 25 batches (52 heads to one, groups of 1 to 8, 400 to 8000 rows), of which
+// it picks the fastest or one within 4 %, 0.3 % on average.  12 heads in 4 groups, 64, 8192 rows of 17 sequences: 256 x 1 piece 98 us,
+// 64 x 1 piece 77, 128 x 16 tiles 59; 32 heads in 8 groups, 128, 8192 rows of 8: 396 whole, 365 in pieces of 64, 410 with 64 keys; 7 heads, 128, 2600
+// rows of two: 514 whole, 75 in pieces of 16, 53 with 64 keys.
+struct Way {
+    int keys;
+    double tile, chain, fixed;                       // a tile among others (per compute unit), a tile of a chain, the rest
+};
+constexpr Way WAYS[2][2] = {{{128, 0.83, 1.41, 7.1}, {64, 0.51, 0.98, 7.0}}, {{256, 2.72, 2.28, 14.6}, {64, 1.02, 1.33, 7.4}}};     // head size 64, 128
+constexpr int64_t PIECES[] = {WHOLE, 96, 64, 48, 32, 24, 16, 12, 8, 6, 4};
+constexpr int64_t MOST_PARTIAL = (int64_t)512 << 20;  // bytes of partial sums
+
+int64_t cut_backward(Packing &p, const int32_t *offsets, int per_tile) {
+    double best = 0.0;
+    int64_t best_piece = WHOLE;
+    p.keys = 0;
+    for (const Way &way : WAYS[p.dh == 128]) {
+        const int64_t group = p.group();
+        int64_t tiles = 0, query_tiles = 0, longest_query = 0;
+        std::vector<int64_t> blocks;                 // their tiles
+        for (int s = 0; s < p.n_seqs; ++s) {
+            const int64_t len = offsets[s + 1] - offsets[s];
+            for (int64_t left = len; left > 0; left -= way.keys) {
+                blocks.push_back((left + per_tile - 1) / per_tile);
+                tiles += blocks.back();
+            }
+            for (int64_t v0 = 0; v0 < len * group; v0 += way.keys) {
+                const int64_t t = std::min<int64_t>((v0 + way.keys - 1) / group, len - 1) / 64 + 1;
+                query_tiles += t;
+                longest_query = std::max(longest_query, t);
+            }
+        }
+        const double work = ((double)tiles + 0.75 * (double)query_tiles) * p.Hkv * way.tile / 256.0;
+        for (const int64_t piece : PIECES) {
+            int64_t parts = 0, longest = 0;
+            for (const int64_t t : blocks) {
+                const int64_t n = pieces_of(t, piece);
+                longest = std::max(longest, (t + n - 1) / n);
+                if (n > 1) parts += n;
+            }
+            if (piece != WHOLE && !parts) continue;  // no block is that large
+            const int64_t bytes = parts * p.Hkv * way.keys * p.dh * 8;
+            if (bytes > MOST_PARTIAL) continue;
+            const double chain = (double)longest * way.chain, rows = 0.75 * (double)longest_query * way.chain;
+            const double us = way.fixed + std::max(std::max(work, chain), rows) + 0.25 * std::min(work, chain) + 0.48e-6 * (double)bytes + (parts ? 2.7 : 0.0);
+            if (!p.keys || us < best) best = us, best_piece = piece, p.keys = way.keys;
+        }
+    }
+    return best_piece;
 }
 
 }  // namespace
@@ -98,15 +154,12 @@ Packing build_packing(const int32_t *offsets, int32_t n_seqs, int32_t dtype, int
         return p;
     }
     p.fwd_rows = query_blocks(p, offsets, 64, group) * Hkv <= (dh == 64 ? 1280 : 1024) ? 64 : 128;
-    p.dq_rows = 128;
+    const int per_tile = rows_per_tile(true, group);
+    const int64_t piece = cut_backward(p, offsets, per_tile);
+    p.dq_rows = p.keys;
     p.fwd = query_items(p, offsets, p.fwd_rows, group);
     p.dq = p.fwd_rows == p.dq_rows ? p.fwd : query_items(p, offsets, p.dq_rows, group);
-    p.keys = dh == 64 ? 128 : 256;
-    const int per_tile = rows_per_tile(true, group), per_cu = dh == 64 ? 3 : 1;
-    int64_t tiles = 0;
-    for (int s = 0; s < n_seqs; ++s)
-        for (int64_t left = offsets[s + 1] - offsets[s]; left > 0; left -= p.keys) tiles += (left + per_tile - 1) / per_tile;
-    key_items(p, offsets, p.keys, per_tile, std::max<int64_t>(8, (tiles * Hkv + COMPUTE_UNITS * per_cu - 1) / (COMPUTE_UNITS * per_cu)));
+    key_items(p, offsets, p.keys, per_tile, piece);
     return p;
 }
 

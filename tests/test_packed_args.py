@@ -27,7 +27,7 @@ def test_items_cover_the_batch_once(lens, heads):
     dtype, H, Hkv, dh = heads
     mfma = dtype == "bf16" and dh > 32
     G = H // Hkv if mfma else 1
-    per_tile, keys = (64 // G, 128 if dh == 64 else 256) if mfma else (32, 32)
+    per_tile = 64 // G if mfma else 32
     lists = data[at:]
     where = {int(o): n for o, n in zip(off[:-1], lens) if n}
 
@@ -36,8 +36,8 @@ def test_items_cover_the_batch_once(lens, heads):
     # query lists: until every (sequence, block) of one block size has been seen
     i, seen = 0, []
     total = sum(lens) * G
-    while len(seen) < (1 if not mfma else 2) and i + 4 <= len(lists):
-        for rows in ((64, 128) if mfma else (32,)):
+    while len(seen) < 2 and i + 4 <= len(lists):
+        for rows in ((64, 128, 256) if mfma else (32,)):
             n = sum((k * G + rows - 1) // rows for k in lens)
             items = lists[i:i + 4 * n].reshape(-1, 4)
             got = {(int(w[0]), int(w[2])) for w in items}
@@ -52,6 +52,8 @@ def test_items_cover_the_batch_once(lens, heads):
     assert seen and total
     rest = lists[i:].reshape(-1, 8)
     items, sums = rest[rest[:, 6] == 0], rest[rest[:, 6] > 0]
+    keys = min([int(k) for k in items[:, 2] if k] + [256])                  # of a block: the second one of some sequence begins behind it
+    assert keys in ((64, 128, 256) if mfma else (32,)) or max(lens) <= 256
     tiles = {}
     for first, n, kv0, t0, t1, part, _, _ in items:
         assert where[int(first)] == n and t0 < t1

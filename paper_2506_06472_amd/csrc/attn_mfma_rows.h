@@ -686,7 +686,7 @@ __device__ __forceinline__ void dkv_rows(const KeyPlace &at, const uint16_t *__r
     static_assert(!DELTA || NW == 4, "four lanes to each of 64 rows");
     float st = 0.f;
     bf16x8 go[DELTA ? CH : 1], oo[DELTA ? CH : 1];
-    const __amdgpu_buffer_rsrc_t rsD = head_rsrc(dO, Tn, at.ldg, DH), rsO = head_rsrc(DELTA ? O : dO, Tn, at.ldg, DH);
+    const __amdgpu_buffer_rsrc_t rsD = head_rsrc(dO, Tn, at.ldg, DH * G), rsO = head_rsrc(DELTA ? O : dO, Tn, at.ldg, DH * G);
     float *stats = reinterpret_cast<float *>(smem + 2 * BUF + (VLDS ? KEYS * DH : 0));
     auto load_stats = [&](int i0) {
         if (GROUPED) {
@@ -697,7 +697,9 @@ __device__ __forceinline__ void dkv_rows(const KeyPlace &at, const uint16_t *__r
         } else if (wave < STATS) st = buffer_load4(rsS, (uint32_t)(i0 + lane_here()) * 4);
         if (DELTA) {
             const int ln = lane_here();
-            const uint32_t at = (uint32_t)(i0 + wave * 16 + (ln >> 2)) * ldg + (ln & 3) * CH * 16;
+            const int v = wave * 16 + (ln >> 2), r = GROUPED ? v / G : v;
+            uint32_t at = (uint32_t)(i0 + r) * ldg + (GROUPED ? (v - r * G) * (DH * 2) : 0) + (ln & 3) * CH * 16;
+            if (TAIL && r >= per_tile) at = PAST_ALL;
 #pragma unroll
             for (int c = 0; c < (DELTA ? CH : 0); ++c) {
                 go[c] = buf_frag(rsD, at + c * 16);

@@ -147,7 +147,9 @@ __global__ void __launch_bounds__(TPB) pref_mean_k(const float *__restrict__ los
 // 16-byte chunk blockIdx.x TPB + the thread of row rows - 1 - blockIdx.y.  d may be the logits.  Bound: HBM.  The rows are taken from the last one, and the
 // gradient goes past the caches: what the first launch has read last is then still in the memory-side cache, and neither launch waits for
 // dirty lines.  8192 x 32000 and 4093 x 50257, whole pass: rows in order 253 / 165 us, gradient through the caches 269 / 199, as it is 219 / 156 (also
-// at 1024 x 32000, whose gradient would fit the caches: 43 against 49); two chunks to a thread 226 / 160, four 236 / 165.
+// at 1024 x 32000, whose gradient would fit the caches: 43 against 49); two chunks to a thread 226 / 160, four 236 / 165.  Not kept: pairs in groups of
+// 64 MiB, each group's gradient in one launch with the sums of the next but one (269 / 196).  Two readings and the writing, at the rates that each
+// reaches alone, would take 210.
 template <typename T>
 __global__ void __launch_bounds__(TPB) pref_grad_k(const T *logits, T *d, int64_t ld, const int32_t *__restrict__ labels, int64_t Vn, int64_t rows,
                                                    const int32_t *__restrict__ offsets, int pairs, const RowStat *__restrict__ stats,
@@ -210,9 +212,10 @@ template <typename T> void launch(hipStream_t s, const PreferenceArgs &a) {
         pref_mean_k<<<1, TPB, 0, s>>>(a.losses, (int)a.pairs, total, a.loss);
         return;
     }
-    // a grid has at most 2^16 - 1 rows of workgroups
-    for (int64_t rows = a.rows; rows > 0; rows -= 65535) {
-        const dim3 grid((unsigned)((nchunk + TPB - 1) / TPB), (unsigned)(rows < 65535 ? rows : 65535));
+    // a grid has at most 2^16 - 1 rows of workgroups, and fewer than 2^32 threads
+    const int64_t segments = (nchunk + TPB - 1) / TPB, most = ((int64_t)1 << 23) / segments, at_once = most < 65535 ? most : 65535;
+    for (int64_t rows = a.rows; rows > 0; rows -= at_once) {
+        const dim3 grid((unsigned)segments, (unsigned)(rows < at_once ? rows : at_once));
         pref_grad_k<T><<<grid, TPB, 0, s>>>((const T *)a.logits, (T *)a.dlogits, a.ld, a.labels, a.V, rows, a.offsets, (int)a.pairs, stats, weight, a.losses,
                                             total, rows == a.rows ? a.loss : nullptr);
     }

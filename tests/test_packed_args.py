@@ -130,6 +130,12 @@ def test_preference_refusals(bad):
     assert e.value.code == -1
 
 
+def test_preference_batches_beyond_a_launch():
+    p = tio.tio_packing_build([0, 1 << 21, 1 << 22])
+    with pytest.raises(tio.TioError, match="2.22"):
+        tio.tio_op_preference_loss(0, "bf16", p, P, 8, P, 8, P, P, 0.1, 0.0, P, P, P, P, P)
+
+
 @pytest.mark.parametrize("rows,cols,want", [(1, 1, 48), (1, 32, 48), (3, 33, 208), (128, 512, 128 * 512 + 128 * 16), (1021, 2730, (1021 * 86 * 33 + 15) // 16 * 16)])
 def test_checkpoint_bytes(rows, cols, want):
     assert tio.tio_ckpt8_bytes(rows, cols) == want

@@ -100,12 +100,13 @@ template <int NW> __device__ __forceinline__ double block_sum_f64(double v, doub
 // A workgroup to a pair.  weight: the derivative of the loss by the sum of a pair's preferred sequence.  The pairs' mean is left to the next launch: a
 // counter that tells the last workgroup cost 6 us, for the caches it has to write back first.
 constexpr int PAIR_THREADS = 1024;
-__global__ void __launch_bounds__(PAIR_THREADS) pref_pairs_k(const int32_t *__restrict__ offsets, const double *__restrict__ logp,
+__global__ void __launch_bounds__(PAIR_THREADS) pref_pairs_k(const int32_t *__restrict__ offsets, int rows, const double *__restrict__ logp,
                                                              const float *__restrict__ ref, float beta, float smoothing, float total_pairs,
                                                              float *__restrict__ seq, float *__restrict__ losses, float *__restrict__ weight) {
     __shared__ double red[2][PAIR_THREADS / 64];
     const int64_t pair = blockIdx.x;
-    const int32_t at[3] = {offsets[2 * pair], offsets[2 * pair + 1], offsets[2 * pair + 2]};
+    int32_t at[3];
+    for (int i = 0; i < 3; ++i) at[i] = min(max(offsets[2 * pair + i], 0), rows);        // nothing outside the batch is read, whatever they are
     double sum[2] = {0.0, 0.0};
     for (int i = 0; i < 2; ++i) {
         int64_t r = at[i] + threadIdx.x;
@@ -207,7 +208,7 @@ template <typename T> void launch(hipStream_t s, const PreferenceArgs &a) {
 #undef TIO_ROWS
     }
     const float total = (float)a.total_pairs;
-    pref_pairs_k<<<(unsigned)a.pairs, PAIR_THREADS, 0, s>>>(a.offsets, logp, a.ref, a.beta, a.smoothing, total, a.seq, a.losses, weight);
+    pref_pairs_k<<<(unsigned)a.pairs, PAIR_THREADS, 0, s>>>(a.offsets, (int)a.rows, logp, a.ref, a.beta, a.smoothing, total, a.seq, a.losses, weight);
     if (!a.dlogits || !a.rows) {
         pref_mean_k<<<1, TPB, 0, s>>>(a.losses, (int)a.pairs, total, a.loss);
         return;

@@ -122,6 +122,12 @@ int64_t cut_backward(Packing &p, const int32_t *offsets, int per_tile) {
     return best_piece;
 }
 
+// a grid has fewer than 2^32 threads, of which a workgroup here has at most 512 (and the kernels in fp32 arithmetic one for every query head)
+void check_grids(const Packing &p) {
+    const int64_t heads = p.mfma ? p.Hkv : p.H, items = std::max<int64_t>(p.fwd.n, (int64_t)p.dq.n + p.key.n) + 32;
+    if (items * heads >= ((int64_t)1 << 23)) throw std::invalid_argument("too many blocks of rows: cut the batch");
+}
+
 }  // namespace
 
 Packing build_packing(const int32_t *offsets, int32_t n_seqs, int32_t dtype, int64_t H, int64_t Hkv, int64_t dh) {
@@ -150,7 +156,8 @@ Packing build_packing(const int32_t *offsets, int32_t n_seqs, int32_t dtype, int
     if (!p.mfma) {                                   // every query head by itself
         p.fwd_rows = p.dq_rows = p.keys = 32;
         p.fwd = p.dq = query_items(p, offsets, 32, 1);
-        key_items(p, offsets, 32, 32, (int64_t)1 << 40);
+        key_items(p, offsets, 32, 32, WHOLE);
+        check_grids(p);
         return p;
     }
     p.fwd_rows = query_blocks(p, offsets, 64, group) * Hkv <= (dh == 64 ? 1280 : 1024) ? 64 : 128;
@@ -160,6 +167,7 @@ Packing build_packing(const int32_t *offsets, int32_t n_seqs, int32_t dtype, int
     p.fwd = query_items(p, offsets, p.fwd_rows, group);
     p.dq = p.fwd_rows == p.dq_rows ? p.fwd : query_items(p, offsets, p.dq_rows, group);
     key_items(p, offsets, p.keys, per_tile, piece);
+    check_grids(p);
     return p;
 }
 

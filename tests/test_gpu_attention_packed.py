@@ -61,6 +61,11 @@ def test_long_and_many(lens, H, Hkv, dh):
     _check(lens, "bf16", H, Hkv, dh)
 
 
+@pytest.mark.parametrize("dtype,H,Hkv,dh", [("bf16", 4, 2, 64), ("bf16", 3, 1, 128), ("fp32", 2, 1, 32)])
+def test_a_thousand_sequences(dtype, H, Hkv, dh):
+    _check([1, 2, 0, 3, 1] * 250, dtype, H, Hkv, dh)
+
+
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("H,Hkv", [(4, 1), (3, 1)])
 def test_scores_whose_maximum_keeps_rising(dh, H, Hkv):
@@ -146,6 +151,31 @@ def test_same_bits_again_and_on_another_stream():
     s = torch.cuda.Stream()
     again = pl.run_attention(lens, "bf16", H, Hkv, dh, qkv, dO, stream=s.cuda_stream)
     assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+def test_two_streams_at_once():
+    """Two batches on two streams, buffers of their own: neither changes the other's bits."""
+    import torch
+    import paper_2506_06472_amd as tio
+    import packedlib as pl
+    cases = [([900, 33, 257], "bf16", 6, 2, 64), ([400, 31, 700], "bf16", 8, 2, 128)]
+    alone, states = [], []
+    for lens, dtype, H, Hkv, dh in cases:
+        qkv, dO = _inputs(lens, H, Hkv, dh, dtype)
+        alone.append(pl.run_attention(lens, dtype, H, Hkv, dh, qkv, dO))
+        p, dev = pl.packing(lens, dtype, H, Hkv, dh)
+        q, g = (torch.from_numpy(a).cuda().bfloat16() for a in (qkv, dO))
+        states.append((p, dev, q, g, torch.zeros_like(g), torch.zeros_like(q), torch.zeros((H, sum(lens)), device="cuda"),
+                       torch.zeros(tio.tio_op_attention_packed_work(p), device="cuda", dtype=torch.uint8), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for p, dev, q, g, o, d, lse, work, s in states:
+            tio.tio_op_attention_packed(s.cuda_stream, p, dev.data_ptr(), q.data_ptr(), q.stride(0), o.data_ptr(), o.stride(0), lse.data_ptr())
+            tio.tio_op_attention_packed_bwd(s.cuda_stream, p, dev.data_ptr(), q.data_ptr(), q.stride(0), o.data_ptr(), g.data_ptr(), o.stride(0),
+                                            lse.data_ptr(), work.data_ptr(), d.data_ptr())
+    torch.cuda.synchronize()
+    for want, (_, _, _, _, o, d, lse, _, _) in zip(alone, states):
+        assert torch.equal(o, want[0]) and torch.equal(lse, want[1]) and torch.equal(d, want[2])
 
 
 @pytest.mark.parametrize("dtype,H,Hkv,dh", [("bf16", 6, 2, 64), ("bf16", 8, 2, 128), ("fp32", 4, 2, 32)])

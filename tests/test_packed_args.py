@@ -73,7 +73,7 @@ def test_items_cover_the_batch_once(lens, heads):
 
 @pytest.mark.parametrize("off,heads", [([0], ()), ([1, 4], ()), ([0, 5, 4], ()), ([0, 4], ("bf16", 3, 2, 64)), ([0, 4], ("bf16", 0, 2, 64)),
                                        ([0, 4], ("bf16", 4, 2, 48)), ([0, 4], ("bf16", 130, 2, 64)), ([0, 4], ("bf16", 4, 0, 64)),
-                                       ([0, 1 << 29], ("bf16", 4, 2, 64)), ([0, 4], ("fp32", -4, -2, 32))])
+                                       ([0, 1 << 29], ("bf16", 4, 2, 64)), (range(0, 1 << 22), ("fp32", 4, 2, 32)), ([0, 4], ("fp32", -4, -2, 32))])
 def test_packings_that_are_refused(off, heads):
     with pytest.raises(tio.TioError) as e:
         tio.tio_packing_build(off, *heads)

@@ -883,32 +883,43 @@ __device__ __forceinline__ void dkv_rows(const KeyPlace &at, const uint16_t *__r
 }
 // floats of a workgroup's partial sums
 template <int DH, int NW, int NG> constexpr int key_partial() { return NW * 2 * (DH / 16) * NG * 256; }
-// The sums of `pieces` workgroups' partial ones of a block of keys, in order, to dk and dv; wavefronts as in dkv_rows, block i of 32 columns.
+// The sums of `pieces` workgroups' partial ones of a block of keys, in order, to dk (which = 0) or dv (1); wavefronts as in dkv_rows, block i of 32
+// columns.  Bound: HBM.
 template <int DH, int NW, int NG>
-__device__ __forceinline__ void key_sums(const KeyPlace &at, const float *__restrict__ partial, int pieces, int i, uint16_t *__restrict__ dk_out,
-                                         uint16_t *__restrict__ dv_out, float scale) {
+__device__ __forceinline__ void key_sums(const KeyPlace &at, const float *__restrict__ partial, int pieces, int which, int i, uint16_t *__restrict__ out,
+                                         float scale) {
     constexpr int DT = DH / 16;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    floatx4 sum[2][2][NG];                                // [dk, dv][half of the columns][keys 16 k ..]
-    const float *mine = partial + (wave * 2 * DT * NG * 64 + lane) * 4;
-    for (int p = 0; p < pieces; ++p, mine += key_partial<DH, NW, NG>()) {
+    const float *mine = partial + ((wave * 2 + which) * DT + 2 * i) * NG * 256 + lane * 4;
+    auto load = [&](int p, int e, int k) __attribute__((always_inline)) {
+        return *reinterpret_cast<const floatx4 *>(mine + (int64_t)p * key_partial<DH, NW, NG>() + (e * NG + k) * 256);
+    };
+    floatx4 sum[2][NG];                                   // [half of the columns][keys 16 k ..]
 #pragma unroll
-        for (int w = 0; w < 2; ++w)
+    for (int e = 0; e < 2; ++e)
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
+        for (int k = 0; k < NG; ++k) sum[e][k] = load(0, e, k);
+    int p = 1;
+    for (; p + 2 < pieces; p += 2) {                      // two pieces' loads on their way
+        floatx4 a[2][NG], b[2][NG];
 #pragma unroll
-                for (int k = 0; k < NG; ++k) {
-                    const floatx4 x = *reinterpret_cast<const floatx4 *>(mine + ((w * DT + 2 * i + e) * NG + k) * 256);
-                    sum[w][e][k] = p ? sum[w][e][k] + x : x;
-                }
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int k = 0; k < NG; ++k) a[e][k] = load(p, e, k), b[e][k] = load(p + 1, e, k);
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int k = 0; k < NG; ++k) sum[e][k] = (sum[e][k] + a[e][k]) + b[e][k];
     }
+    for (; p < pieces; ++p)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int k = 0; k < NG; ++k) sum[e][k] += load(p, e, k);
 #pragma unroll
     for (int k = 0; k < NG; ++k) {
         const int key = at.kv0 + wave * 16 * NG + 16 * k + (lane & 15);
-        if (key < at.Tn) {
-            store32(dk_out + key * at.ld + 32 * i, sum[0][0][k], sum[0][1][k], scale, lane >> 4);
-            store32(dv_out + key * at.ld + 32 * i, sum[1][0][k], sum[1][1][k], 1.0f, lane >> 4);
-        }
+        if (key < at.Tn) store32(out + key * at.ld + 32 * i, sum[0][k], sum[1][k], which ? 1.0f : scale, lane >> 4);
     }
 }
 

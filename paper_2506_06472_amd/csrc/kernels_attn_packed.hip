@@ -87,8 +87,9 @@ __global__ void __launch_bounds__(NW * 64) attn_packed_sums_k(const PackedRows w
     KeyPlace at;
     int hk, part, pieces;
     if (!where.place<DH, NW * 16 * NG>(blockIdx.x, at, hk, part, pieces) || part < 0 || pieces < 1 || part > parts - pieces) return;
-    key_sums<DH, NW, NG>(at, partial + ((int64_t)hk * parts + part) * key_partial<DH, NW, NG>(), pieces, (int)blockIdx.y, dqkv + (at.k - where.qkv),
-                         dqkv + (at.v - where.qkv), scale);
+    const int which = (int)blockIdx.y & 1;
+    key_sums<DH, NW, NG>(at, partial + ((int64_t)hk * parts + part) * key_partial<DH, NW, NG>(), pieces, which, (int)blockIdx.y >> 1,
+                         dqkv + ((which ? at.v : at.k) - where.qkv), scale);
 }
 
 template <int DH> constexpr size_t fwd_smem() { return (size_t)3 * 2 * 32 * DH * 2; }      // three pairs of tiles
@@ -135,7 +136,7 @@ void both(hipStream_t s, const Packing &p, const void *device, const void *qkv, 
     }
     if (p.sums.n) {
         const PackedRows r = rows_of(p, device, p.sums, KEY_WORDS, qkv, ld, ldo);
-        attn_packed_sums_k<DH, NW, NG><<<dim3(r.places.grid(), DH / 32), NW * 64, 0, s>>>(r, partial, p.parts, (uint16_t *)dqkv, scale);
+        attn_packed_sums_k<DH, NW, NG><<<dim3(r.places.grid(), DH / 16), NW * 64, 0, s>>>(r, partial, p.parts, (uint16_t *)dqkv, scale);
     }
 }
 

@@ -71,15 +71,15 @@ void key_items(Packing &p, const int32_t *offsets, int keys, int per_tile, int64
 // How the backward pass is cut: the keys of a block (64 of four wavefronts with 16 keys each; or 128 of four, head size 64, and 256 of eight,
 // head size 128, with 32 each, which do a product for half the reads but are fewer and take longer for a tile) and the tiles of a piece.
 // The time is estimated as that of the tiles, dealt evenly, or of the longest chain of them if that is longer, a quarter of the shorter of the two, and
-// the partial sums' way to memory and back.  us; fitted to 300 ways to cut 25 batches (52 heads to one, groups of 1 to 8, 400 to 8000 rows), of which
-// it picks the fastest or one within 4 %, 0.3 % on average.  12 heads in 4 groups, 64, 8192 rows of 17 sequences: 256 x 1 piece 98 us,
+// the partial sums' way to memory and back.  us; fitted to 480 ways to cut 30 batches (2 to 52 heads, groups of 1 to 13, 370 to 8192 rows), of which
+// it picks the fastest or one within 6 %, 0.6 % behind on average.  12 heads in 4 groups, 64, 8192 rows of 17 sequences: 256 x 1 piece 98 us,
 // 64 x 1 piece 77, 128 x 16 tiles 59; 32 heads in 8 groups, 128, 8192 rows of 8: 396 whole, 365 in pieces of 64, 410 with 64 keys; 7 heads, 128, 2600
 // rows of two: 514 whole, 75 in pieces of 16, 53 with 64 keys.
 struct Way {
     int keys;
     double tile, chain, fixed;                       // a tile among others (per compute unit), a tile of a chain, the rest
 };
-constexpr Way WAYS[2][2] = {{{128, 0.83, 1.41, 7.1}, {64, 0.51, 0.98, 7.0}}, {{256, 2.72, 2.28, 14.6}, {64, 1.02, 1.33, 7.4}}};     // head size 64, 128
+constexpr Way WAYS[2][2] = {{{128, 0.78, 1.47, 9.1}, {64, 0.53, 1.02, 7.0}}, {{256, 3.0, 2.35, 12.0}, {64, 1.03, 1.32, 7.9}}};     // head size 64, 128
 constexpr int64_t PIECES[] = {WHOLE, 96, 64, 48, 32, 24, 16, 12, 8, 6, 4};
 constexpr int64_t MOST_PARTIAL = (int64_t)512 << 20;  // bytes of partial sums
 
@@ -115,7 +115,7 @@ int64_t cut_backward(Packing &p, const int32_t *offsets, int per_tile) {
             const int64_t bytes = parts * p.Hkv * way.keys * p.dh * 8;
             if (bytes > MOST_PARTIAL) continue;
             const double chain = (double)longest * way.chain, rows = 0.75 * (double)longest_query * way.chain;
-            const double us = way.fixed + std::max(std::max(work, chain), rows) + 0.25 * std::min(work, chain) + 0.48e-6 * (double)bytes + (parts ? 2.7 : 0.0);
+            const double us = way.fixed + std::max(std::max(work, chain), rows) + 0.25 * std::min(work, chain) + 0.5e-6 * (double)bytes + (parts ? 2.4 : 0.0);
             if (!p.keys || us < best) best = us, best_piece = piece, p.keys = way.keys;
         }
     }

@@ -209,24 +209,28 @@ template <int DH, int NW> struct GroupTile {
 // NG: groups of 16 query rows of a wavefront.
 // W: where a workgroup's rows are (its place() says so, or that there are none).  The loop stands in the kernel itself: as a function of its
 // own, the same code took 12 registers more, and at head size 128 spilled.
-template <int DH, int NG, class W>
-__global__ void __launch_bounds__(NT, DH == 64 || NG == 1 ? 4 : 3) attn_fwd_mfma_k(const W where, uint16_t *__restrict__ o, float *__restrict__ lse, float scale) {
+// SPLIT: that many sets of four wavefronts share the workgroup's rows, each with every SPLIT-th tile of keys (a step of the ring is SPLIT tiles, which all
+// of them load together), and join their sums at the end, in order: for batches whose longest chain of tiles counts.
+template <int DH, int NG, int SPLIT, class W>
+__global__ void __launch_bounds__(NT *SPLIT, SPLIT > 1 ? 2 : DH == 64 || NG == 1 ? 4 : 3)
+    attn_fwd_mfma_k(const W where, uint16_t *__restrict__ o, float *__restrict__ lse, float scale) {
     constexpr bool GROUPED = W::GROUPED;
-    constexpr int KS = DH / 32, DT = DH / 16, TE = 32 * DH, RING = 4, ROWS = NT / 64 * 16 * NG;
-    extern __shared__ __attribute__((aligned(1024))) uint16_t smem[];    // ring of three pairs of tiles: 32 rows of K | 32 rows of V
+    constexpr int KS = DH / 32, DT = DH / 16, TE = 32 * DH, TS = TE * SPLIT, RING = 4, ROWS = NT / 64 * 16 * NG;
+    extern __shared__ __attribute__((aligned(1024))) uint16_t smem[];    // ring of three steps: 32 SPLIT rows of K | as many of V
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l16 = lane & 15, grp = lane >> 4;
+    const int set = SPLIT == 1 ? 0 : wave / (NT / 64);
     QueryPlace at;
     if (!where.template place<DH, ROWS>(blockIdx.x, at)) return;
     const int64_t ld = at.ld;
     const uint32_t ldb = (uint32_t)(ld * 2);
     const int Tn = at.Tn, q0 = at.v0, G = GROUPED ? at.G : 1;
-    const int q0w = q0 + wave * 16 * NG;
+    const int q0w = q0 + (SPLIT == 1 ? wave : wave % (NT / 64)) * 16 * NG;
     const __amdgpu_buffer_rsrc_t rsQ = head_rsrc(at.q, Tn, ld, DH * G);
     const uint32_t head_bytes = (uint32_t)(((Tn - 1) * ld + DH) * 2);
     const i32x4 rsK = make_rsrc(at.k, head_bytes), rsV = make_rsrc(at.v, head_bytes);
     const float c = scale * LOG2E;
     const TileLanes<DH> L(lane);
-    using Dma = DmaTile<DH, NT / 64, 32>;
+    using Dma = DmaTile<DH, NT / 64 * SPLIT, 32 * SPLIT>;
     const Dma dma(ldb, wave, lane);
     constexpr int PER = Dma::PER;
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem));
@@ -246,35 +250,35 @@ __global__ void __launch_bounds__(NT, DH == 64 || NG == 1 ? 4 : 3) attn_fwd_mfma
         for (int i = 0; i < DT; ++i) oacc[i][u] = zero4();
     }
     const int past = GROUPED ? (q0 + ROWS - 1) / G + 1 : q0 + ROWS, kv_end = past < Tn ? past : Tn;
-    const int ntiles = (kv_end + 31) / 32;
+    const int steps = (kv_end + 32 * SPLIT - 1) / (32 * SPLIT);
 
     dma.load(rsK, 0, ldb, lds0, wave);
-    dma.load(rsV, 0, ldb, lds0 + TE * 2, wave);
-    dma.load(rsK, 32, ldb, lds0 + 2 * TE * 2, wave);
-    dma.load(rsV, 32, ldb, lds0 + 3 * TE * 2, wave);
+    dma.load(rsV, 0, ldb, lds0 + TS * 2, wave);
+    dma.load(rsK, 32 * SPLIT, ldb, lds0 + 2 * TS * 2, wave);
+    dma.load(rsV, 32 * SPLIT, ldb, lds0 + 3 * TS * 2, wave);
     __builtin_amdgcn_s_waitcnt(0x0F70);                 // vmcnt(0): this wavefront's part of tile 0 has landed (and Q, which the compiler knows of)
     __builtin_amdgcn_s_barrier();
-    int slot = 0;                                       // of tile t in the ring
-    // Tile t + 2 goes to the slot of tile t - 1, free since the barrier that ended it; past the last tile the loads lie outside the
+    int slot = 0;                                       // of step t in the ring
+    // Step t + 2 goes to the slot of step t - 1, free since the barrier that ended it; past the last step the loads lie outside the
     // descriptor and bring zeros that nobody reads.  They are issued one at a time between the score products: issued together
     // right after the barrier, the loads of all wavefronts of a compute unit queue up behind one another and every wavefront stalls.
     struct Next { uint32_t soff, to; };
     auto next_of = [&](int t) __attribute__((always_inline)) {
-        return Next{(uint32_t)__builtin_amdgcn_readfirstlane(t + 2 < ntiles ? (uint32_t)(t + 2) * 32 * ldb : PAST_ALL),
-                    lds0 + (uint32_t)(slot == 0 ? 2 : slot - 1) * 2 * TE * 2};
+        return Next{(uint32_t)__builtin_amdgcn_readfirstlane(t + 2 < steps ? (uint32_t)(t + 2) * (32 * SPLIT) * ldb : PAST_ALL),
+                    lds0 + (uint32_t)(slot == 0 ? 2 : slot - 1) * 2 * TS * 2};
     };
     auto next_load = [&](int i, const Next &n) __attribute__((always_inline)) {         // PER loads of K, then as many of V
         if (i < PER) dma.load_one(i, rsK, n.soff, n.to, wave);
-        else dma.load_one(i - PER, rsV, n.soff, n.to + TE * 2, wave);
+        else dma.load_one(i - PER, rsV, n.soff, n.to + TS * 2, wave);
     };
     auto end_of_tile = [&]() __attribute__((always_inline)) {
         slot = slot == 2 ? 0 : slot + 1;
-        __builtin_amdgcn_s_waitcnt(0x0070 | 2 * PER);   // tile t+1 has landed, tile t+2 may be on its way; lgkmcnt(0)
+        __builtin_amdgcn_s_waitcnt(0x0070 | 2 * PER);   // step t+1 has landed, step t+2 may be on its way; lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
     };
-    // DIAG: the tile on the diagonal, which has key q0w (GROUPED: the tiles that a row of the wavefront sees part of)
+    // Tile t * SPLIT + set.  DIAG: the tile on the diagonal, which has key q0w (GROUPED: the tiles that a row of the wavefront sees part of)
     auto tile = [&](int t, auto DIAG) __attribute__((always_inline)) {
-        const uint16_t *Ks = smem + slot * 2 * TE, *Vs = Ks + TE;
+        const uint16_t *Ks = smem + slot * 2 * TS + set * TE, *Vs = Ks + TS;
         const Next next = next_of(t);
         floatx4 s[2][NG];                               // [keys 16 k ..][queries 16 u ..]
         {
@@ -310,7 +314,7 @@ __global__ void __launch_bounds__(NT, DH == 64 || NG == 1 ? 4 : 3) attn_fwd_mfma
                 for (int u = 0; u < NG; ++u)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        if (GROUPED ? 16 * k + r > (q0w + 16 * u + l16) / G - 32 * t - 4 * grp
+                        if (GROUPED ? 16 * k + r > (q0w + 16 * u + l16) / G - 32 * (t * SPLIT + set) - 4 * grp
                                     : 16 * (k - u) + r > (NG == 1 ? q0w % 32 : 0) + l16 - 4 * grp)
                             s[k][u][r] = -INFINITY;
                     }
@@ -344,7 +348,9 @@ __global__ void __launch_bounds__(NT, DH == 64 || NG == 1 ? 4 : 3) attn_fwd_mfma
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) tmax = fmaxf(tmax, s[k][u][r]);
-                const float mn = fmaxf(m[u], max_groups(tmax) * c), corr = __builtin_amdgcn_exp2f(m[u] - mn);
+                // GROUPED: m is never below -2^20, so that tiles with nothing but scores of -inf, or so low that m would lose what exp2 needs of them, add
+                // zeros to a row, whichever tile it begins with (a set's first may hold no key that a row sees)
+                const float mt = fmaxf(m[u], max_groups(tmax) * c), mn = GROUPED ? fmaxf(mt, -1048576.0f) : mt, corr = __builtin_amdgcn_exp2f(m[u] - mn);
                 l[u] *= corr;
                 m[u] = mn;
 #pragma unroll
@@ -387,14 +393,15 @@ __global__ void __launch_bounds__(NT, DH == 64 || NG == 1 ? 4 : 3) attn_fwd_mfma
     if constexpr (GROUPED) {
         if (q0w / G < Tn) {
             const int whole = (q0w / G + 1) / 32, last = (q0w + 16 * NG - 1) / G, some = (last < Tn ? last : Tn - 1) / 32;
-            for (; t < whole; ++t) tile(t, std::false_type{});
-            for (; t <= some; ++t) tile(t, std::true_type{});
+            for (; t * SPLIT + set < whole; ++t) tile(t, std::false_type{});
+            for (; t * SPLIT + set <= some; ++t) tile(t, std::true_type{});
         }
     } else if (q0w < Tn) {
+        static_assert(GROUPED || SPLIT == 1, "tiles of one set");
         for (; t < q0w / 32; ++t) tile(t, std::false_type{});
         tile(t++, std::true_type{});
     }
-    for (; t < ntiles; ++t) {
+    for (; t < steps; ++t) {
         const Next next = next_of(t);
 #pragma unroll
         for (int i = 0; i < 2 * PER; ++i) next_load(i, next);
@@ -403,6 +410,40 @@ __global__ void __launch_bounds__(NT, DH == 64 || NG == 1 ? 4 : 3) attn_fwd_mfma
     __builtin_amdgcn_s_waitcnt(0x0F70);                 // no load may be on its way to LDS that this workgroup gives back
 #pragma unroll
     for (int u = 0; u < NG; ++u) l[u] = sum_halves(sum_neighbours(l[u]));
+    if constexpr (SPLIT > 1) {
+        // the sets' exponents, sums and accumulators, in the ring's place
+        constexpr int LANE = NG * (2 + 4 * DT);                             // floats of a lane
+        static_assert((SPLIT - 1) * (NT / 64) * 64 * LANE * 4 <= 3 * 2 * TS * 2, "room in the ring");
+        __builtin_amdgcn_s_barrier();                   // nobody reads tiles any more
+        float *const part = reinterpret_cast<float *>(smem);
+        auto at_lane = [&](int of, int i) __attribute__((always_inline)) { return ((of * (NT / 64) + wave % (NT / 64)) * LANE + i) * 64 + lane; };
+        if (set) {
+#pragma unroll
+            for (int u = 0; u < NG; ++u) {
+                part[at_lane(set - 1, 2 * u)] = m[u];
+                part[at_lane(set - 1, 2 * u + 1)] = l[u];
+#pragma unroll
+                for (int i = 0; i < DT; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) part[at_lane(set - 1, 2 * NG + (u * DT + i) * 4 + r)] = oacc[i][u][r];
+            }
+        }
+        __syncthreads();
+        if (set) return;
+#pragma unroll
+        for (int of = 0; of < SPLIT - 1; ++of)
+#pragma unroll
+            for (int u = 0; u < NG; ++u) {
+                const float mo = part[at_lane(of, 2 * u)], M = fmaxf(m[u], mo), ref = M == -INFINITY ? 0.f : M;
+                const float fa = __builtin_amdgcn_exp2f(m[u] - ref), fb = __builtin_amdgcn_exp2f(mo - ref);
+                l[u] = l[u] * fa + part[at_lane(of, 2 * u + 1)] * fb;
+                m[u] = M;
+#pragma unroll
+                for (int i = 0; i < DT; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) oacc[i][u][r] = oacc[i][u][r] * fa + part[at_lane(of, 2 * NG + (u * DT + i) * 4 + r)] * fb;
+            }
+    }
 #pragma unroll
     for (int u = 0; u < NG; ++u) {
         const int v = q0w + 16 * u + l16, q = GROUPED ? v / G : v, head = GROUPED ? v - q * G : 0;

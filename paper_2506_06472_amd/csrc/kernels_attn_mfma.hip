@@ -187,7 +187,7 @@ void attn_fwd_mfma(hipStream_t s, const void *qkv, void *o, float *lse, int64_t 
 #define TIO_ATTN_FWD(DH, NG)                                                                                                                   \
     {                                                                                                                                          \
         const Launch l(B * H, Tn, DH, NT / 64 * 16 * NG, DH == 64 ? 4 : 3);                                                                    \
-        attn_fwd_mfma_k<DH, NG><<<l.grid, NT, fwd_smem<DH>(), s>>>(BatchRows{(const uint16_t *)qkv, B, Tn, H, l.order}, (uint16_t *)o, lse, scale); \
+        attn_fwd_mfma_k<DH, NG, 1><<<l.grid, NT, fwd_smem<DH>(), s>>>(BatchRows{(const uint16_t *)qkv, B, Tn, H, l.order}, (uint16_t *)o, lse, scale); \
     }
     // Sixteen rows to a wavefront while the chip holds about all workgroups of 64 rows at once: half the work in a tile, where the chain
     // of a wavefront's tiles is what counts; more of them would load K and V twice as often.  us, 32 / 16 rows (workgroups of 64, the heads

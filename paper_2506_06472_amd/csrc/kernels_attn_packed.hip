@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(NW * 64) attn_packed_sums_k(const PackedRows w
                          dqkv + ((which ? at.v : at.k) - where.qkv), scale);
 }
 
-template <int DH> constexpr size_t fwd_smem() { return (size_t)3 * 2 * 32 * DH * 2; }      // three pairs of tiles
+template <int DH, int SPLIT> constexpr size_t fwd_smem() { return (size_t)3 * 2 * 32 * SPLIT * DH * 2; }      // three steps
 template <int DH, int NW, int NG> constexpr size_t dkv_smem() {         // tiles, V rows, then statistics
     return (size_t)2 * 2 * 64 * DH * 2 + (dkv_v_in_lds<DH, NG>() ? (size_t)NW * 16 * NG * DH * 2 : 0) + 2 * 128 * 4;
 }
@@ -104,8 +104,16 @@ constexpr int QUERY_WORDS = sizeof(QueryItem) / 4, KEY_WORDS = sizeof(KeyItem) /
 
 template <int DH> void fwd(hipStream_t s, const Packing &p, const void *device, const void *qkv, int64_t ld, void *o, int64_t ldo, float *lse, float scale) {
     const PackedRows w = rows_of(p, device, p.fwd, QUERY_WORDS, qkv, ld, ldo);
-    if (p.fwd_rows == 64) attn_fwd_mfma_k<DH, 1><<<w.places.grid(), NT, fwd_smem<DH>(), s>>>(w, (uint16_t *)o, lse, scale);
-    else attn_fwd_mfma_k<DH, 2><<<w.places.grid(), NT, fwd_smem<DH>(), s>>>(w, (uint16_t *)o, lse, scale);
+    auto go = [&](auto NG, auto SPLIT) {
+        const auto kernel = attn_fwd_mfma_k<DH, NG(), SPLIT(), PackedRows>;
+        (void)hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)fwd_smem<DH, SPLIT()>());
+        kernel<<<w.places.grid(), NT * SPLIT(), fwd_smem<DH, SPLIT()>(), s>>>(w, (uint16_t *)o, lse, scale);
+    };
+    using One = std::integral_constant<int, 1>;
+    using Two = std::integral_constant<int, 2>;
+    if (p.fwd_rows == 128) go(Two{}, One{});
+    else if (p.fwd_sets == 1) go(One{}, One{});
+    else go(One{}, Two{});
 }
 
 // The delta of short sequences is computed where it is needed, by every block of keys that a row meets, which saves a launch of 3 us (eight sequences of up

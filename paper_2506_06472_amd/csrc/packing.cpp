@@ -160,7 +160,15 @@ Packing build_packing(const int32_t *offsets, int32_t n_seqs, int32_t dtype, int
         check_grids(p);
         return p;
     }
-    p.fwd_rows = query_blocks(p, offsets, 64, group) * Hkv <= (dh == 64 ? 1280 : 1024) ? 64 : 128;
+    // Forward pass: sixteen rows to a wavefront while there are few blocks of 64 rows, and two sets of wavefronts to a block, which take every other tile of
+    // keys, while the longest chain of tiles is what counts.  us, 32 rows / 16 / two sets (blocks of 64 rows):
+    //   heads of 64:  8192 rows of 17 sequences, 12/4 20.9 / 19.3 / 21.9 (1550)  4096, 32/8 81.8 / 85.0 / 87.8 (2048)  2 x 1024, 24 19.3 / 16.0 / 16.2 (768)
+    //                 2 x 1024, 12 17.3 / 13.6 / 11.2 (384)    2048 and 1000, 8 29.4 / 22.5 / 17.2 (381)    4096, 4/1 52.9 / 39.5 / 27.5 (256)
+    //   of 128:       3 x 1024, 32/8 35.0 / 37.5 / 58.8 (1536)  2048, 32/8 48.2 / 45.6 / 57.5 (1024)   1200 and 700, 16/4 26.6 / 22.2 / 22.7 (506)
+    //                 1700 and 900, 7/1 33.6 / 25.8 / 21.4 (285)  4 x 300, 16/4 11.0 / 9.4 / 12.1 (304)  4096, 4/1 69.9 / 52.7 / 40.4 (256)
+    const int64_t blocks = query_blocks(p, offsets, 64, group) * Hkv;
+    p.fwd_rows = blocks <= (dh == 64 ? 1800 : 1024) ? 64 : 128;
+    p.fwd_sets = blocks <= (dh == 64 ? 512 : p.max_len >= 700 ? 400 : 256) ? 2 : 1;
     const int per_tile = rows_per_tile(true, group);
     const int64_t piece = cut_backward(p, offsets, per_tile);
     p.dq_rows = p.keys;

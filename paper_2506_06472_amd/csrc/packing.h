@@ -31,6 +31,7 @@ struct Packing {
     std::vector<int32_t> data;                   // the n_seqs + 1 offsets, padding to a multiple of four words, then the lists
     bool mfma = false;                           // bf16 matrix cores (head size 64 or 128); otherwise fp32 arithmetic
     int32_t fwd_rows = 0, dq_rows = 0, keys = 0; // rows of an item
+    int32_t fwd_sets = 1;                        // sets of wavefronts that share a forward item's rows
     ItemList fwd, dq, key, sums;
     int32_t parts = 0;                           // blocks of partial sums for each key head
     int group() const { return Hkv ? H / Hkv : 1; }

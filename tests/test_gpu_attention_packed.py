@@ -103,6 +103,38 @@ def test_sequences_do_not_see_each_other(dtype, H, Hkv, dh):
             assert torch.equal(d[r][:, :H * dh], a[2][:, :H * dh])
 
 
+@pytest.mark.parametrize("dtype,H,Hkv,dh", [("bf16", 4, 2, 64), ("bf16", 3, 1, 64), ("bf16", 48, 8, 64), ("bf16", 8, 2, 128), ("bf16", 5, 1, 128), ("bf16", 32, 8, 128),
+                                            ("fp32", 4, 2, 32), ("bf16", 4, 1, 32)])
+@pytest.mark.parametrize("value", [-np.inf, -1e30])
+def test_whole_tiles_of_keys_that_count_for_nothing(dtype, H, Hkv, dh, value):
+    """The first 70 keys of a sequence, and others, far below the rest: rows that see another one have the values of a batch in which these keys
+    and their values are not there.  Bounds as above: the sums' order and the roundings of P are others."""
+    import packedlib as pl
+    lens, first, n = [20, 400, 5], 20, 400
+    print(f"packed attention, keys that count for nothing {dtype} H={H} Hkv={Hkv} dh={dh} {value}", flush=True)
+    qkv, dO = _inputs(lens, H, Hkv, dh, dtype)
+    x = qkv.reshape(-1, H + 2 * Hkv, dh).copy()
+    x[:, :H, 5] = np.abs(x[:, :H, 5]) + 0.25
+    if dtype == "bf16":
+        from synth import to_bf16_round
+        x = to_bf16_round(x)
+    gone = list(range(70)) + list(range(128, 160)) + [200]
+    x[[first + k for k in gone], H:H + Hkv, 5] = value
+    o, lse, _ = pl.run_attention(lens, dtype, H, Hkv, dh, x.reshape(len(x), -1), dO)
+    keep = [k for k in range(n) if k not in gone]
+    u, G = 2.0 ** -8 if dtype == "bf16" else 1e-5, H // Hkv
+    got, got_lse = o.double().cpu().numpy().reshape(-1, H, dh)[first:first + n], lse.double().cpu().numpy()[:, first:first + n]
+    q = x[first:first + n].astype(np.float64)
+    for h in range(H):
+        s = np.where(np.array(keep)[None, :] > np.arange(70, n)[:, None], -np.inf, q[70:, h] @ q[keep, H + h // G].T / np.sqrt(dh))
+        m = s.max(1, keepdims=True)
+        e = np.exp(s - m)
+        p = e / e.sum(1, keepdims=True)
+        v = q[keep, H + Hkv + h // G]
+        assert np.all(np.abs(got[70:, h] - p @ v) <= u * (np.abs(p @ v) + p @ np.abs(v))), h
+        assert np.abs(got_lse[h, 70:] - (m + np.log(e.sum(1, keepdims=True)))[:, 0]).max() <= 1e-3
+
+
 @pytest.mark.parametrize("H,Hkv,dh", [(4, 2, 64), (3, 1, 64), (8, 2, 128), (5, 1, 128)])
 def test_gradients_of_keys_at_minus_infinity(H, Hkv, dh):
     """A key whose scores are all -inf takes part in nothing: the gradients are those of a key far below every other.  The forward pass

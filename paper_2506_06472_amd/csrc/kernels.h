@@ -109,7 +109,7 @@ void attn_packed_fwd_f32(hipStream_t s, const Packing &p, const void *device, co
 void attn_packed_bwd_f32(hipStream_t s, const Packing &p, const void *device, const void *qkv, int64_t ld, const void *o, const void *dO, int64_t ldo,
                          const float *lse, float *delta, void *dqkv, float scale);
 struct PreferenceArgs {
-    int64_t rows, pairs, total_pairs, V, ld;
+    int64_t rows, pairs, total_pairs, longest_pair, V, ld;           // longest_pair: rows of the longest pair
     const int32_t *offsets, *labels;             // device
     const void *logits;
     const float *ref;

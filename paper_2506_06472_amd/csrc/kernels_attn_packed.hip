@@ -5,7 +5,7 @@
 // and V once for all its heads, has G times fewer keys between its first and last row's diagonals, and a short sequence fills it G times
 // better; a block of keys takes the query rows of all its heads in one chain of tiles, so that dK and dV need no sums over heads.
 // Workgroups are dealt longest first (attn_packed.h).  A block of keys whose chain would outlast the others is cut into pieces, whose fp32 sums
-// a launch behind them adds in order: no atomics, and results that depend on nothing but the lengths.
+// a launch behind them adds in order: no atomics, and results that depend on nothing but the lengths and heads.
 #include "../../include/teraio.h"
 #include "attn_mfma_rows.h"
 #include "attn_packed.h"

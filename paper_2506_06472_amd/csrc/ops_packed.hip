@@ -2,6 +2,7 @@
 // them are.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <new>
 #include <stdexcept>
@@ -152,9 +153,11 @@ int tio_op_preference_loss(void *stream, int32_t dtype, const tio_packing *packi
     if (!aligned(packing_dev) || !aligned(logits) || !aligned(dlogits) || !aligned(work)) return fail(TIO_ERR_INVALID_ARG, BAD_POINTER);
     if (!aligned(labels, 4) || !aligned(ref_logp, 4) || !aligned(seq_logp, 4) || !aligned(losses, 4) || !aligned(loss, 4))
         return fail(TIO_ERR_INVALID_ARG, "labels, sums and losses must be 4-byte aligned");
+    int64_t longest = 0;
+    for (int64_t i = 0; i < pairs; ++i) longest = std::max<int64_t>(longest, p.data[2 * i + 2] - p.data[2 * i]);
     const OnDeviceOf device((hipStream_t)stream);
     k::preference_loss((hipStream_t)stream, dtype,
-                       k::PreferenceArgs{p.rows, pairs, total_pairs ? total_pairs : pairs, V, ld, (const int32_t *)packing_dev, labels, logits, ref_logp, beta,
+                       k::PreferenceArgs{p.rows, pairs, total_pairs ? total_pairs : pairs, longest, V, ld, (const int32_t *)packing_dev, labels, logits, ref_logp, beta,
                                          smoothing, seq_logp, losses, loss, work, dlogits});
     return launched();
     TIO_OP_END

@@ -174,7 +174,7 @@ template <typename T> __device__ __forceinline__ float gelu(float x) { return x 
 template <typename T> __device__ __forceinline__ void gelu_both(float x, float &y, float &dy) {
     const float s = logistic<T>(GELU_A * (x + GELU_B * x * x * x));
     y = x * s;
-    dy = s + y * (1.0f - s) * GELU_A * (1.0f + 3.0f * GELU_B * x * x);
+    dy = s + y * (1.0f - s) * GELU_A * (1.0f + 3.0f * GELU_B * fminf(x * x, 1e4f));      // beyond |x| = 100 y (1 - s) is zero, and must not meet infinity
 }
 
 // y = act(gate[, up]) of the values as they come; the checkpoint keeps the inputs (SwiGLU: the gate half's checkpoint, then the up half's).

@@ -214,3 +214,29 @@ def test_activation_of_extreme_inputs():
             assert torch.isfinite(y[0]).all() and torch.isfinite(dg[0]).all()
             assert y[0, 1] == 0 and y[0, 5] == 0 and y[0, 0] == t[0, 0] and y[1, 40] == float("inf")
             assert torch.isnan(dg[1, 32:64]).all() and torch.isfinite(dg[1, :32]).all()
+
+
+@pytest.mark.parametrize("act", ["gelu", "swiglu"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_activation_of_inputs_whose_square_is_infinite(dtype, act):
+    """The gradients are the logistic function's ends there: 1 or 0 of a GELU's input and of a gate, the gate itself or 0 of the other half."""
+    import torch
+    import paper_2506_06472_amd as tio
+    import packedlib as pl
+    two, big = act == "swiglu", [1e20, -1e20, 3e38, -3e38, 2e19, -2e19]
+    x = np.zeros((1, 32 * len(big)), np.float32)
+    x[0, ::32] = big
+    n = x.shape[1]
+    t, ld = _padded(x, dtype, 0.0)
+    one, _ = _padded(np.ones_like(x), dtype, 0.0)
+    kept = torch.zeros(2 * tio.tio_ckpt8_bytes(1, n), device="cuda", dtype=torch.uint8)
+    y, dg, du = (torch.zeros_like(t) for _ in range(3))
+    tio.tio_op_act_ckpt8(0, dtype, act, 1, n, t.data_ptr(), one.data_ptr() if two else 0, ld, y.data_ptr(), ld, kept.data_ptr())
+    tio.tio_op_act_ckpt8_bwd(0, dtype, act, 1, n, kept.data_ptr(), one.data_ptr(), ld, dg.data_ptr(), du.data_ptr() if two else 0, ld)
+    torch.cuda.synchronize()
+    is_up = torch.from_numpy(x[0, ::32] > 0).cuda()
+    assert torch.equal(y[0, :n:32], torch.where(is_up, t[0, :n:32], 0.0))
+    assert torch.equal(dg[0, :n:32], is_up.to(dg.dtype)) and torch.isfinite(dg).all() and torch.isfinite(du).all()
+    if two:
+        k = torch.from_numpy(pl.kept_values(t[:1, :n].double().cpu().numpy())[0, ::32]).cuda().to(du.dtype)
+        assert torch.equal(du[0, :n:32], torch.where(is_up, k, 0.0).to(du.dtype))

@@ -419,7 +419,7 @@ int tio_op_attention_packed_bwd(void *stream, const tio_packing *packing, const 
  * gradient of loss[0], in rows like the logits', with zeros in rows that do not count and up to the next multiple of 16 bytes behind
  * V; it may be the logits' own buffer, and otherwise overlaps none.  beta > 0, 0 <= smoothing <= 1.  work: device memory of
  * tio_op_preference_loss_work bytes, contents of no interest before and after, used by one call at a time.  16-byte aligned: logits,
- * dlogits, work and the packing's copy.  At most 2^22 - 1 rows. */
+ * dlogits, work and the packing's copy.  At most 2^22 - 1 rows, and as many pairs. */
 int tio_op_preference_loss_work(const tio_packing *packing, uint64_t *out_bytes);
 int tio_op_preference_loss(void *stream, int32_t dtype, const tio_packing *packing, const void *packing_dev, int64_t V, const void *logits,
                            int64_t ld, const int32_t *labels, const float *ref_logp, float beta, float smoothing, int64_t total_pairs,

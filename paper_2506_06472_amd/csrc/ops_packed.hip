@@ -148,7 +148,7 @@ int tio_op_preference_loss(void *stream, int32_t dtype, const tio_packing *packi
     if (!(beta > 0.f) || !std::isfinite(beta)) return fail(TIO_ERR_INVALID_ARG, "beta must be positive");
     if (!(smoothing >= 0.f && smoothing <= 1.f)) return fail(TIO_ERR_INVALID_ARG, "label smoothing must be 0 to 1");
     const int64_t pairs = p.n_seqs / 2;
-    if (p.rows >= 1 << 22) return fail(TIO_ERR_INVALID_ARG, "at most 2^22 - 1 rows");
+    if (p.rows >= 1 << 22 || pairs >= 1 << 22) return fail(TIO_ERR_INVALID_ARG, "at most 2^22 - 1 rows, and pairs");
     if (total_pairs && total_pairs < pairs) return fail(TIO_ERR_INVALID_ARG, "fewer pairs in total than in this batch");
     if (!aligned(packing_dev) || !aligned(logits) || !aligned(dlogits) || !aligned(work)) return fail(TIO_ERR_INVALID_ARG, BAD_POINTER);
     if (!aligned(labels, 4) || !aligned(ref_logp, 4) || !aligned(seq_logp, 4) || !aligned(losses, 4) || !aligned(loss, 4))

@@ -136,6 +136,13 @@ def test_preference_batches_beyond_a_launch():
         tio.tio_op_preference_loss(0, "bf16", p, P, 8, P, 8, P, P, 0.1, 0.0, P, P, P, P, P)
 
 
+def test_preference_pairs_beyond_a_launch():
+    """Empty sequences: few rows do not mean few pairs."""
+    p = tio.tio_packing_build(np.zeros((1 << 23) + 1, np.int32))
+    with pytest.raises(tio.TioError, match="pairs"):
+        tio.tio_op_preference_loss(0, "bf16", p, P, 8, P, 8, P, P, 0.1, 0.0, P, P, P, P, P)
+
+
 @pytest.mark.parametrize("rows,cols,want", [(1, 1, 48), (1, 32, 48), (3, 33, 208), (128, 512, 128 * 512 + 128 * 16), (1021, 2730, (1021 * 86 * 33 + 15) // 16 * 16)])
 def test_checkpoint_bytes(rows, cols, want):
     assert tio.tio_ckpt8_bytes(rows, cols) == want

@@ -486,6 +486,28 @@ template <int KS> __device__ __forceinline__ float row_dot(const bf16x8 (&g)[KS]
     return p[0];
 }
 
+// GROUPED: delta of a sequence's first rows, from the probabilities instead of the rounded output.  A row's dO . O misses sum(P dP) by the rounding of O, which,
+// relative to the row's dS, falls with the square root of its number of keys; and the first rows have the largest gradients.  dQ of 4 heads
+// of 64, relative to the norm, with the output's throughout and like this: sequences of 34 and 2 rows 3.3e-3 / 2.5e-3, one of 1713 2.5e-3 / 2.4e-3, of
+// which the roundings of dS and of the result make 2.3e-3.  It costs what a few loads in a row take: 12 heads, sequences of up to 100 rows
+// 12.6 -> 13.3 us, 32 heads of 128 in 4 groups, up to 60 rows 20.6 -> 23.6, large batches less than 1 %; for eight rows instead of 16 half a
+// microsecond less where groups are large, and dQ up to 2.6e-3.  q, g: fragments of Q and dO of sixteen rows, a lane's row of the sequence `row`;
+// k, v: of its first sixteen keys.
+constexpr int EARLY = 16;
+template <int KS> __device__ __forceinline__ float early_delta(const bf16x8 (&q)[KS], const bf16x8 (&g)[KS], const bf16x8 (&k)[KS], const bf16x8 (&v)[KS],
+                                                               float c, float lse2, int row, int grp) {
+    floatx4 s = zero4(), dp = zero4();
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        mma(s, k[ks], q[ks]);
+        mma(dp, v[ks], g[ks]);
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) sum += 4 * grp + r <= row ? __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse2)) * dp[r] : 0.f;
+    return sum_halves(sum_neighbours(sum));
+}
+
 // Bound: the matrix cores and the vector ALU, which work for 57 and 48 % of the time at head size 128 (39 and 57 at 64) and for a fifth to a third
 // of the products' time together, and power; the tiles in front of the diagonal run through a loop of their own, without mask and
 // branch.  Three wavefronts per SIMD at head size 64, two at 128.  With fragments of the transposed K tile four ahead in registers, where
@@ -530,9 +552,24 @@ __device__ __forceinline__ void dq_rows(const QueryPlace &at, const uint16_t *__
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) of[ks] = buf_frag(rsO, atg + (ks * 32 + grp * 8) * 2);
             dl[u] = row_dot<KS>(gf[u], of);
-            if (q < Tn && grp == 0) delta[stat] = dl[u];
+            if (!GROUPED && q < Tn && grp == 0) delta[stat] = dl[u];
         } else {
             dl[u] = q < Tn ? delta[stat] : 0.f;
+        }
+    }
+    if (GROUPED && q0w / G < EARLY) {
+        const __amdgpu_buffer_rsrc_t rsK1 = head_rsrc(at.k, Tn, ld, DH), rsV1 = head_rsrc(at.v, Tn, ld, DH);
+        bf16x8 k1[KS], v1[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            k1[ks] = buf_frag(rsK1, (uint32_t)l16 * ldb + (ks * 32 + grp * 8) * 2);
+            v1[ks] = buf_frag(rsV1, (uint32_t)l16 * ldb + (ks * 32 + grp * 8) * 2);
+        }
+#pragma unroll
+        for (int u = 0; u < NG; ++u) {
+            const int q = (q0w + 16 * u + l16) / G;
+            const float early = early_delta<KS>(qf[u], gf[u], k1, v1, c, lse2[u], q, grp);
+            if (q < EARLY) dl[u] = early;
         }
     }
     floatx4 dq[DT][NG];
@@ -679,7 +716,7 @@ __device__ __forceinline__ void dkv_rows(const KeyPlace &at, const uint16_t *__r
     constexpr int KS = DH / 32, DT = DH / 16, TE = 64 * DH, RING = 4, TR = 4, KEYS = NW * 16 * NG;
     constexpr bool VLDS = dkv_v_in_lds<DH, NG>(), ONE_LOOP = DH == 64;
     constexpr int BUF = 2 * TE;                                          // Q tile | dO tile, filled as in the forward kernel
-    // [2 buffers][Q | dO], [KEYS][DH] V rows if VLDS, then [2][64 lse | 64 delta] floats
+    // [2 buffers][Q | dO], [KEYS][DH] V rows if VLDS, then [2][64 lse | 64 delta] floats; GROUPED: then delta of the first EARLY rows
     extern __shared__ __attribute__((aligned(1024))) uint16_t smem[];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l16 = lane & 15, grp = lane >> 4;
     const int64_t ld = at.ld;
@@ -748,11 +785,22 @@ __device__ __forceinline__ void dkv_rows(const KeyPlace &at, const uint16_t *__r
             }
         }
     };
-    auto store_stats = [&](int buf) {
-        if (wave < STATS) stats[buf * 128 + wave * 64 + lane_here()] = st * to_lds;
-        if (DELTA) {
-            const float sum = quad_dot<DELTA ? CH : 1>(go, oo);
+    // delta of row v of the tile at i0
+    auto delta_of = [&](float x, int v, int i0) __attribute__((always_inline)) {
+        const int e = i0 * G + v;
+        return v < per_tile * G && e < EARLY * G ? stats[256 + e] : x;
+    };
+    auto store_stats = [&](int buf, int i0) {
+        if (wave < STATS) {
             const int ln = lane_here();
+            float x = st * to_lds;
+            if (GROUPED && !DELTA && i0 < EARLY && wave == 1) x = delta_of(x, ln, i0);
+            stats[buf * 128 + wave * 64 + ln] = x;
+        }
+        if (DELTA) {
+            float sum = quad_dot<DELTA ? CH : 1>(go, oo);
+            const int ln = lane_here();
+            if (GROUPED && i0 < EARLY) sum = delta_of(sum, wave * 16 + (ln >> 2), i0);
             if ((ln & 3) == 0) stats[buf * 128 + 64 + wave * 16 + (ln >> 2)] = sum;
         }
     };
@@ -762,9 +810,32 @@ __device__ __forceinline__ void dkv_rows(const KeyPlace &at, const uint16_t *__r
         dmaG.load(rsG, (uint32_t)i0, ldg, at + TE * 2, wave);
     };
     int t = GROUPED ? at.t0 : 0;
+    if (GROUPED && kv0 + t * per_tile < EARLY) {
+        const __amdgpu_buffer_rsrc_t rsQ1 = head_rsrc(at.q, Tn, ld, DH * G);
+        bf16x8 k1[KS], v1[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            k1[ks] = buf_frag(rsK, (uint32_t)l16 * ldb + (ks * 32 + grp * 8) * 2);
+            v1[ks] = buf_frag(rsV, (uint32_t)l16 * ldb + (ks * 32 + grp * 8) * 2);
+        }
+        const int to = (ntiles * per_tile < EARLY ? ntiles * per_tile : EARLY) * G;         // of this workgroup's tiles
+        for (int v0 = t * per_tile * G + wave * 16; v0 < to; v0 += NW * 16) {
+            const int v = v0 + l16, r = v / G;
+            bf16x8 q1[KS], g1[KS];
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                q1[ks] = buf_frag(rsQ1, row_offset<GROUPED, DH>(v, G, ldb) + (ks * 32 + grp * 8) * 2);
+                g1[ks] = buf_frag(rsD, row_offset<GROUPED, DH>(v, G, ldg) + (ks * 32 + grp * 8) * 2);
+            }
+            const float lse2 = r < Tn ? lse[(v - r * G) * at.heads_ld + r] * LOG2E : 0.f;
+            const float early = early_delta<KS>(q1, g1, k1, v1, c, lse2, r, grp);
+            if (grp == 0 && v < EARLY * G) stats[256 + v] = early;
+        }
+        __syncthreads();
+    }
     load_tile(kv0 + t * per_tile, t & 1);
     load_stats(kv0 + t * per_tile);
-    store_stats(t & 1);
+    store_stats(t & 1, kv0 + t * per_tile);
     if (t + 1 < ntiles) load_stats(kv0 + (t + 1) * per_tile);
     __builtin_amdgcn_s_waitcnt(0x0F70);                 // vmcnt(0): this wavefront's part of tile 0 (and of V) has landed
     __syncthreads();
@@ -787,7 +858,7 @@ __device__ __forceinline__ void dkv_rows(const KeyPlace &at, const uint16_t *__r
             // The statistics fetched a tile ago go to LDS before the tile loads are issued: the write waits for every
             // outstanding vector memory operation of the wavefront, and behind the tile loads that would be their
             // whole latency, at the start of every tile.
-            store_stats((t + 1) & 1);
+            store_stats((t + 1) & 1, i0 + per_tile);
             load_tile(i0 + per_tile, (t + 1) & 1);
             if (t + 2 < ntiles) load_stats(i0 + 2 * per_tile);
         }

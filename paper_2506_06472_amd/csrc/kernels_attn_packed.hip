@@ -93,8 +93,8 @@ __global__ void __launch_bounds__(NW * 64) attn_packed_sums_k(const PackedRows w
 }
 
 template <int DH, int SPLIT> constexpr size_t fwd_smem() { return (size_t)3 * 2 * 32 * SPLIT * DH * 2; }      // three steps
-template <int DH, int NW, int NG> constexpr size_t dkv_smem() {         // tiles, V rows, then statistics
-    return (size_t)2 * 2 * 64 * DH * 2 + (dkv_v_in_lds<DH, NG>() ? (size_t)NW * 16 * NG * DH * 2 : 0) + 2 * 128 * 4;
+template <int DH, int NW, int NG> constexpr size_t dkv_smem(int group) {         // tiles, V rows, then statistics and the first rows' delta
+    return (size_t)2 * 2 * 64 * DH * 2 + (dkv_v_in_lds<DH, NG>() ? (size_t)NW * 16 * NG * DH * 2 : 0) + 2 * 128 * 4 + (size_t)EARLY * group * 4;
 }
 
 PackedRows rows_of(const Packing &p, const void *device, const ItemList &list, int words, const void *qkv, int64_t ld, int64_t ldg) {
@@ -117,7 +117,7 @@ template <int DH> void fwd(hipStream_t s, const Packing &p, const void *device, 
 }
 
 // The delta of short sequences is computed where it is needed, by every block of keys that a row meets, which saves a launch of 3 us (eight sequences of up
-// to 100 rows, 12 heads of 64: forward and backward 17.6 -> 15.6 us); the bound is that of the kernels of one length.
+// to 100 rows, 12 heads of 64 in 4 groups: forward and backward 19.6 -> 17.8 us); the bound is that of the kernels of one length.
 template <int DH, int NG> bool own_delta(const Packing &p) { return NG == 1 && (int64_t)p.max_len * p.group() * DH <= 65536; }
 
 // blocks of NW wavefronts of 16 NG keys or query rows
@@ -128,8 +128,8 @@ void both(hipStream_t s, const Packing &p, const void *device, const void *qkv, 
     const unsigned key_blocks = keys.places.grid();
     auto go = [&](auto DELTA, auto TAIL) {
         const auto kernel = attn_packed_both_mfma_k<DH, NW, NG, DELTA(), TAIL()>;
-        (void)hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)dkv_smem<DH, NW, NG>());
-        kernel<<<key_blocks + queries.places.grid(), NW * 64, dkv_smem<DH, NW, NG>(), s>>>(keys, queries, key_blocks, (const uint16_t *)dO, (const uint16_t *)o,
+        (void)hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)dkv_smem<DH, NW, NG>(64));
+        kernel<<<key_blocks + queries.places.grid(), NW * 64, dkv_smem<DH, NW, NG>(p.group()), s>>>(keys, queries, key_blocks, (const uint16_t *)dO, (const uint16_t *)o,
                                                                                           lse, delta, (uint16_t *)dqkv, partial, p.parts, scale);
     };
     auto with = [&](auto DELTA) {

@@ -19,7 +19,7 @@ def attention(lens, H, Hkv, dh, qkv, dO, u):
     """o, lse, dqkv of the definition, and bounds of o's and dqkv's errors, element by element.
 
     u: twice a rounding of the storage type.  The kernels round the probabilities P and the score gradients dS to it before the second
-    product and every result once, and take delta = rowsum(dO * O) from the stored O:
+    product and every result once, and take delta = rowsum(dO * O) from the stored O (in a sequence's first rows not even that):
       |O - ref| <= u (|O| + P|V|)        E_i = u sum_d |dO_id| (|O_id| + (P|V|)_id)        (error of delta_i)
       |dQ - ref| <= u |dQ| + (E (P|K|) + u |dS||K|) / sqrt(dh),  dK likewise with |Q|,  |dV - ref| <= u (|dV| + P^T |dO|)
     dK and dV are sums over the query heads of a group, and so are their bounds (|dK| once more for the sum's own rounding)."""

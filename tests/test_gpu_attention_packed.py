@@ -159,6 +159,30 @@ def test_gradients_of_keys_at_minus_infinity(H, Hkv, dh):
         assert ((a - b).norm() <= 3 * 2.0 ** -8 * b.norm()).item(), name
 
 
+@pytest.mark.parametrize("lens,H,Hkv,dh", [([34, 2, 3, 27], 8, 4, 64), ([17] * 4, 12, 12, 64), ([8, 1, 208, 14], 8, 2, 128), ([300, 9, 40], 10, 2, 128), ([60] * 5, 33, 1, 64),
+                                           ([1500, 40], 8, 2, 64), ([700, 650, 30, 512], 48, 8, 64), ([600, 555, 800], 40, 10, 128)])
+def test_short_rows_keep_their_precision(lens, H, Hkv, dh):
+    """dQ of the first sixteen rows of every sequence, and dQ and dK of short batches, are as far off as two roundings make them.
+
+    dS is rounded to bf16 and the result is, each an independent error of the same size relative to the norm, which is that of the definition's result
+    rounded once: together sqrt(2) of it.  P, of which dS is made, and delta are held to 32 bits here; half a rounding of delta in O would add 0.7 to 1 of
+    it in rows of few keys.  6 % for the sample: the few hundred roundings of dS that count."""
+    import torch
+    import packedlib as pl
+    print(f"precision lens={lens} H={H} Hkv={Hkv} dh={dh}", flush=True)
+    qkv, dO = _inputs(lens, H, Hkv, dh, "bf16")
+    d = pl.attention(lens, H, Hkv, dh, qkv, dO, 0.0)[2]
+    once = torch.from_numpy(d).to(torch.bfloat16).double().numpy()
+    got = pl.run_attention(lens, "bf16", H, Hkv, dh, qkv, dO)[2].double().cpu().numpy()
+    first = np.concatenate([a + np.arange(min(n, 16)) for a, n in zip(pl.offsets(lens), lens)])
+    parts = {"dq": (first, slice(0, H * dh))}
+    if max(lens) <= 300:
+        parts |= {"all dq": (slice(None), slice(0, H * dh)), "dk": (slice(None), slice(H * dh, (H + Hkv) * dh))}
+    for name, at in parts.items():
+        a, b = (np.linalg.norm(x[at] - d[at]) for x in (got, once))
+        assert a <= 1.5 * b, (name, a / b)
+
+
 @pytest.mark.parametrize("dtype,H,Hkv,dh", [("bf16", 4, 2, 64), ("bf16", 5, 1, 128), ("fp32", 4, 2, 32)])
 def test_gradients_against_differences(dtype, H, Hkv, dh):
     """Directional differences of the forward pass's own log-sum-exp and output in fp32-readable steps: the gradient of sum(w * o) along a random

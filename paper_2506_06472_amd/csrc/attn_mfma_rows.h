@@ -829,7 +829,8 @@ __device__ __forceinline__ void dkv_rows(const KeyPlace &at, const uint16_t *__r
             }
             const float lse2 = r < Tn ? lse[(v - r * G) * at.heads_ld + r] * LOG2E : 0.f;
             const float early = early_delta<KS>(q1, g1, k1, v1, c, lse2, r, grp);
-            if (grp == 0 && v < EARLY * G) stats[256 + v] = early;
+            // of a row past the sequence zero, like its Q, dO and statistics: with an infinite key its scores are not numbers, and p = 0 does not take that out
+            if (grp == 0 && v < EARLY * G) stats[256 + v] = r < Tn ? early : 0.f;
         }
         __syncthreads();
     }

@@ -268,3 +268,30 @@ def test_captured_and_replayed(dtype, H, Hkv, dh):
         eager = pl.run_attention(lens, dtype, H, Hkv, dh, a, b, packed=packed)
         for name, x, y in zip(("o", "lse", "dqkv"), (o, lse, dqkv), eager):
             assert torch.equal(x, y), (seed, name)
+
+
+@pytest.mark.parametrize("H,Hkv,dh", [(4, 2, 64), (3, 1, 64), (33, 1, 64), (8, 2, 128), (5, 1, 128), (4, 4, 128)])
+@pytest.mark.parametrize("more", [[], [700]], ids=["short", "beside a long one"])
+def test_gradients_of_keys_at_minus_infinity_in_short_sequences(H, Hkv, dh, more):
+    """Sequences of fewer than sixteen rows in which a key's scores are all -inf: it takes part in nothing, so dK and dV are the definition's, and so is
+    dQ but for the component in which the key is infinite (zero times infinity)."""
+    import packedlib as pl
+    lens = [5, 40, 9, 2, 15, 0, 3, 16, 17] + more
+    print(f"packed attention, infinite keys of short sequences lens={lens} H={H} Hkv={Hkv} dh={dh}", flush=True)
+    qkv, dO = _inputs(lens, H, Hkv, dh, "bf16")
+    x = qkv.reshape(-1, H + 2 * Hkv, dh)
+    x[:, :H, 5] = np.abs(x[:, :H, 5]) + 0.25
+    from synth import to_bf16_round
+    x = to_bf16_round(x)
+    for a, n in zip(pl.offsets(lens), lens):
+        if n > 1:
+            x[int(a) + max(1, n // 2), H:H + Hkv, 5] = -np.inf
+    qkv = x.reshape(len(x), -1)
+    with np.errstate(invalid="ignore"):
+        o, _, d, ob, db = pl.attention(lens, H, Hkv, dh, qkv, dO, 2.0 ** -8)
+    got = [t.double().cpu().numpy() for t in pl.run_attention(lens, "bf16", H, Hkv, dh, qkv, dO)]
+    assert np.all(np.abs(got[0] - o) <= ob + 1e-30)
+    there = np.ones(d.shape, bool)
+    there[:, :H * dh].reshape(len(d), H, dh)[:, :, 5] = False
+    assert np.isfinite(d[there]).all() and np.isfinite(db[there]).all() and np.isfinite(got[2][there]).all()
+    assert np.all(np.abs(got[2] - d)[there] <= db[there] + 1e-30)

@@ -397,8 +397,8 @@ void tio_packing_free(tio_packing *packing);
  * of v, dh elements each; query head h uses key head h / (H / Hkv).  o: rows of ld_o elements that begin with H heads; lse: fp32
  * [H, rows], the log-sum-exp of the scores scaled by 1/sqrt(dh).  Strides are multiples of 8 elements, device pointers 16-byte
  * aligned.  A sequence's rows, at the larger stride, must span less than 2 GiB (TIO_ERR_INVALID_ARG otherwise).  What stands between
- * the heads and the stride is not touched.  Scores of -inf or below -700000 (keys with
- * an infinite component, or one of the type's lowest value) are probabilities of zero as long as a row sees another one. */
+ * the heads and the stride is not touched.  Scores of -inf (keys with an infinite component) are probabilities of zero; a row that sees no
+ * other has an o that is not a number.  Finite scores, of whatever size, have their softmax. */
 int tio_op_attention_packed(void *stream, const tio_packing *packing, const void *packing_dev, const void *qkv, int64_t ld_qkv,
                             void *o, int64_t ld_o, float *lse);
 /* Gradients of all of q | k | v (dqkv: rows as those of qkv, same stride; its heads only) from dO (rows as those of o), the forward

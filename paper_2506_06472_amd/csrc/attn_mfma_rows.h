@@ -14,6 +14,7 @@ namespace {
 constexpr int NT = 256;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
+constexpr float FAR = 1048576.0f;       // forward pass, GROUPED: reference exponents beyond this one, of either sign, are taken apart
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -259,6 +260,7 @@ __global__ void __launch_bounds__(NT *SPLIT, SPLIT > 1 ? 2 : DH == 64 || NG == 1
     __builtin_amdgcn_s_waitcnt(0x0F70);                 // vmcnt(0): this wavefront's part of tile 0 has landed (and Q, which the compiler knows of)
     __builtin_amdgcn_s_barrier();
     int slot = 0;                                       // of step t in the ring
+    bool far = GROUPED;                                 // GROUPED: some row of the wavefront has a reference exponent beyond FAR (uniform)
     // Step t + 2 goes to the slot of step t - 1, free since the barrier that ended it; past the last step the loads lie outside the
     // descriptor and bring zeros that nobody reads.  They are issued one at a time between the score products: issued together
     // right after the barrier, the loads of all wavefronts of a compute unit queue up behind one another and every wavefront stalls.
@@ -325,40 +327,51 @@ __global__ void __launch_bounds__(NT *SPLIT, SPLIT > 1 ? 2 : DH == 64 || NG == 1
         // where key 0 is visible to every row) is the row maximum of the tile computed, m raised to it, everything
         // accumulated so far rescaled and the tile redone.  After the first keys that is rare, and the common
         // path has no maximum, no exchange between the lane groups and no rescale in it.
+        // GROUPED: a row's tiles may hold nothing but scores of -inf (keys that it does not see: a set's first tile), or scores so large that the product with
+        // c, rounded into m, is off by more than exp2 tolerates.  Where m is beyond FAR the probabilities are taken of rounded products, of which the largest
+        // is m itself, in every tile (a tile's question whether there is such a row: 0.5 to 0.8 % of the pass at head size 128).
         floatx4 p[2][NG];
         float psum[NG];
-        auto probabilities = [&](int u) __attribute__((always_inline)) {
+        auto probabilities = [&](int u, float by, float ref) __attribute__((always_inline)) {
             psum[u] = 0.f;
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    p[k][u][r] = __builtin_amdgcn_exp2f(fmaf(s[k][u][r], c, -m[u]));
+                    p[k][u][r] = __builtin_amdgcn_exp2f(fmaf(s[k][u][r], by, -ref));
                     psum[u] += p[k][u][r];
                 }
         };
 #pragma unroll
-        for (int u = 0; u < NG; ++u) probabilities(u);
-        if (__any(!(psum[0] < 65536.0f) || !(psum[NG - 1] < 65536.0f))) {
+        for (int u = 0; u < NG; ++u) probabilities(u, c, m[u]);
+        if (far || __any(!(psum[0] < 65536.0f) || !(psum[NG - 1] < 65536.0f))) {
 #pragma unroll
             for (int u = 0; u < NG; ++u) {
-                if (!__any(!(psum[u] < 65536.0f))) continue;       // by itself: the bits do not depend on the rows of a wavefront
+                if (!__any(!(psum[u] < 65536.0f) || (GROUPED && fabsf(m[u]) > FAR))) continue;       // by itself: the bits do not depend on the rows of a wavefront
                 float tmax = -INFINITY;
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) tmax = fmaxf(tmax, s[k][u][r]);
-                // GROUPED: m is never below -2^20, so that tiles with nothing but scores of -inf, or so low that m would lose what exp2 needs of them, add
-                // zeros to a row, whichever tile it begins with (a set's first may hold no key that a row sees)
-                const float mt = fmaxf(m[u], max_groups(tmax) * c), mn = GROUPED ? fmaxf(mt, -1048576.0f) : mt, corr = __builtin_amdgcn_exp2f(m[u] - mn);
+                const float mn = fmaxf(m[u], max_groups(tmax) * c), ref = GROUPED && mn == -INFINITY ? 0.f : mn, corr = __builtin_amdgcn_exp2f(m[u] - ref);
                 l[u] *= corr;
                 m[u] = mn;
 #pragma unroll
                 for (int i = 0; i < DT; ++i)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) oacc[i][u][r] *= corr;
-                probabilities(u);
+                float cc = c;
+                if (GROUPED) {
+                    const bool rounded = fabsf(mn) > FAR;
+                    cc = rounded ? 1.f : c;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[k][u][r] = rounded ? s[k][u][r] * c : s[k][u][r];
+                }
+                probabilities(u, cc, ref);
             }
+            if (GROUPED) far = __any(fmaxf(fabsf(m[0]), fabsf(m[NG - 1])) > FAR);
         }
         __builtin_amdgcn_sched_barrier(0);
         bf16x8 pk[NG];

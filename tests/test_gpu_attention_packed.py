@@ -295,3 +295,52 @@ def test_gradients_of_keys_at_minus_infinity_in_short_sequences(H, Hkv, dh, more
     there[:, :H * dh].reshape(len(d), H, dh)[:, :, 5] = False
     assert np.isfinite(d[there]).all() and np.isfinite(db[there]).all() and np.isfinite(got[2][there]).all()
     assert np.all(np.abs(got[2] - d)[there] <= db[there] + 1e-30)
+
+
+# batches of both sizes of forward blocks, with one set and two of wavefronts; keys in the first seventy rows of the second sequence
+LOW_BATCHES = [("bf16", [20, 400, 5], 4, 2, 64), ("bf16", [20, 400, 5], 3, 1, 64), ("bf16", [20, 400, 5], 5, 1, 128), ("bf16", [20, 400, 5], 33, 1, 64),
+               ("bf16", [300, 400, 340], 32, 8, 128), ("bf16", [300, 400, 340], 48, 16, 64), ("bf16", [700, 650, 600, 580], 64, 8, 64),
+               ("bf16", [500, 400, 340, 600, 700], 32, 8, 128), ("fp32", [20, 400, 5], 4, 2, 32), ("fp32", [20, 400, 5], 2, 1, 64), ("bf16", [20, 400, 5], 4, 1, 32)]
+
+
+def _low_scores(dtype, lens, H, Hkv, dh, how, power, sign=-1, low=70):
+    """The first `low` keys of the second sequence have scores of -1.0625 2^power and less (sign = 1: that and more), each an exact product (and of a size at
+    which exp2(score - log-sum-exp), of two rounded numbers, is infinite).  Its rows, the definition's values for them, and the library's for the batch."""
+    import packedlib as pl
+    print(f"packed attention, low scores {dtype} lens={lens} H={H} Hkv={Hkv} dh={dh} {how} {sign} 2^{power}", flush=True)
+    second, n = lens[0], lens[1]
+    qkv, dO = _inputs(lens, H, Hkv, dh, dtype)
+    x = qkv.reshape(-1, H + 2 * Hkv, dh)
+    x[:, :H, 5] = 1.0
+    x[second:second + low, H:H + Hkv] = 0.0
+    at = {"equal": np.full(low, power), "falling": power + np.arange(low) // 4, "rising": power + (low - np.arange(low)) // 4}[how]
+    x[second:second + low, H:H + Hkv, 5] = sign * 1.0625 * np.exp2(np.minimum(at, 120).astype(float))[:, None]
+    qkv = x.reshape(len(x), -1)
+    rows = slice(second, second + n)
+    want = pl.attention([n], H, Hkv, dh, qkv[rows], dO[rows], 2.0 ** -8 if dtype == "bf16" else 1e-5)
+    return rows, want, [t.double().cpu().numpy() for t in pl.run_attention(lens, dtype, H, Hkv, dh, qkv, dO)]
+
+
+@pytest.mark.parametrize("dtype,lens,H,Hkv,dh", LOW_BATCHES)
+@pytest.mark.parametrize("how", ["equal", "falling", "rising"])
+@pytest.mark.parametrize("power", [23, 40, 100])
+def test_rows_that_see_only_very_low_scores(dtype, lens, H, Hkv, dh, how, power):
+    """Such rows have the softmax of what they see (all alike; the first, or the latest, of keys far apart), the rows behind them that of the other keys."""
+    low = 70
+    rows, (o, lse, _, ob, _), got = _low_scores(dtype, lens, H, Hkv, dh, how, power)
+    assert np.all(np.abs(got[0][rows] - o) <= ob + 1e-30)
+    # of a low row: the scale, the product and the sum with log l, each 2^-24 of it
+    err = np.abs(got[1][:, rows] - lse)
+    assert np.all(err[:, :low] <= 2.0 ** -21 * np.abs(lse[:, :low])) and err[:, low:].max() <= 2e-5 * (1 + np.abs(lse[:, low:]).max())
+    assert np.isfinite(got[0]).all() and np.isfinite(got[1]).all()
+
+
+@pytest.mark.parametrize("dtype,lens,H,Hkv,dh", LOW_BATCHES)
+@pytest.mark.parametrize("how", ["equal", "falling", "rising"])
+@pytest.mark.parametrize("power", [23, 40, 100])
+def test_rows_that_see_very_high_scores(dtype, lens, H, Hkv, dh, how, power):
+    """The rows behind them too have the softmax of these keys alone."""
+    rows, (o, lse, _, ob, _), got = _low_scores(dtype, lens, H, Hkv, dh, how, power, 1)
+    assert np.all(np.abs(got[0][rows] - o) <= ob + 1e-30)
+    assert np.all(np.abs(got[1][:, rows] - lse) <= 2.0 ** -21 * np.abs(lse))
+    assert np.isfinite(got[0]).all() and np.isfinite(got[1]).all()

@@ -505,7 +505,8 @@ template <int KS> __device__ __forceinline__ float row_dot(const bf16x8 (&g)[KS]
 // which the roundings of dS and of the result make 2.3e-3.  It costs what a few loads in a row take: 12 heads, sequences of up to 100 rows
 // 12.6 -> 13.3 us, 32 heads of 128 in 4 groups, up to 60 rows 20.6 -> 23.6, large batches less than 1 %; for eight rows instead of 16 half a
 // microsecond less where groups are large, and dQ up to 2.6e-3.  q, g: fragments of Q and dO of sixteen rows, a lane's row of the sequence `row`;
-// k, v: of its first sixteen keys.
+// k, v: of its first sixteen keys.  A row whose scores are so large that its log-sum-exp, rounded, leaves infinite probabilities keeps the output's delta: its own
+// gradients are lost, but delta meets the keys that it does not see too, times a probability of zero.
 constexpr int EARLY = 16;
 template <int KS> __device__ __forceinline__ float early_delta(const bf16x8 (&q)[KS], const bf16x8 (&g)[KS], const bf16x8 (&k)[KS], const bf16x8 (&v)[KS],
                                                                float c, float lse2, int row, int grp) {
@@ -582,7 +583,7 @@ __device__ __forceinline__ void dq_rows(const QueryPlace &at, const uint16_t *__
         for (int u = 0; u < NG; ++u) {
             const int q = (q0w + 16 * u + l16) / G;
             const float early = early_delta<KS>(qf[u], gf[u], k1, v1, c, lse2[u], q, grp);
-            if (q < EARLY) dl[u] = early;
+            if (q < EARLY && fabsf(early) < INFINITY) dl[u] = early;
         }
     }
     floatx4 dq[DT][NG];
@@ -801,7 +802,7 @@ __device__ __forceinline__ void dkv_rows(const KeyPlace &at, const uint16_t *__r
     // delta of row v of the tile at i0
     auto delta_of = [&](float x, int v, int i0) __attribute__((always_inline)) {
         const int e = i0 * G + v;
-        return v < per_tile * G && e < EARLY * G ? stats[256 + e] : x;
+        return v < per_tile * G && e < EARLY * G && fabsf(stats[256 + e]) < INFINITY ? stats[256 + e] : x;
     };
     auto store_stats = [&](int buf, int i0) {
         if (wave < STATS) {

@@ -344,3 +344,15 @@ def test_rows_that_see_very_high_scores(dtype, lens, H, Hkv, dh, how, power):
     assert np.all(np.abs(got[0][rows] - o) <= ob + 1e-30)
     assert np.all(np.abs(got[1][:, rows] - lse) <= 2.0 ** -21 * np.abs(lse))
     assert np.isfinite(got[0]).all() and np.isfinite(got[1]).all()
+
+
+@pytest.mark.parametrize("dtype,lens,H,Hkv,dh", LOW_BATCHES)
+@pytest.mark.parametrize("how", ["equal", "falling", "rising"])
+@pytest.mark.parametrize("power", [23, 40, 100])
+@pytest.mark.parametrize("low", [9, 70])
+def test_gradients_beside_rows_of_very_low_scores(dtype, lens, H, Hkv, dh, how, power, low):
+    """Gradients of the rows and keys behind them are the definition's: neither those keys nor the rows that see only them count there, in the blocks that
+    they share with them either."""
+    rows, (_, _, d, _, db), got = _low_scores(dtype, lens, H, Hkv, dh, how, power, low=low)
+    assert np.all(np.abs(got[2][rows] - d)[low:] <= db[low:] + 1e-30)
+    assert np.isfinite(got[2][:rows.start]).all() and np.isfinite(got[2][rows.stop:]).all()

@@ -61,6 +61,73 @@ def attention(lens, H, Hkv, dh, qkv, dO, u):
     return o.reshape(rows, -1), lse, d.reshape(rows, -1), ob.reshape(rows, -1), db.reshape(rows, -1)
 
 
+def attention_on(device, lens, H, Hkv, dh, qkv, dO, u):
+    """attention() by torch in 64 bits on `device`, for batches that the host would take long over; the same values and bounds as numpy arrays."""
+    import torch
+    G, rows = H // Hkv, int(np.sum(lens))
+    x = torch.from_numpy(np.ascontiguousarray(qkv)).to(device).double().view(rows, H + 2 * Hkv, dh)
+    g = torch.from_numpy(np.ascontiguousarray(dO)).to(device).double().view(rows, H, dh)
+    rs = 1.0 / np.sqrt(dh)
+    o, lse, ob = torch.zeros_like(g), torch.zeros((H, rows), device=device, dtype=torch.float64), torch.zeros_like(g)
+    d, db = torch.zeros_like(x), torch.zeros_like(x)
+    first = 0
+    for n in lens:
+        r = slice(first, first + n)
+        first += n
+        if n == 0:
+            continue
+        hidden = torch.ones((n, n), device=device, dtype=torch.bool).triu(1)
+        for h in range(H):
+            ik, iv = H + h // G, H + Hkv + h // G
+            q, k, v, go = (t.contiguous() for t in (x[r, h], x[r, ik], x[r, iv], g[r, h]))
+            s = (q @ k.t().contiguous() * rs).masked_fill(hidden, -torch.inf)
+            l = torch.logsumexp(s, 1, keepdim=True)
+            p = torch.exp(s - l)
+            pt = p.t().contiguous()
+            out, pv = p @ v, p @ v.abs()
+            o[r, h], lse[h, r], ob[r, h] = out, l[:, 0], u * (out.abs() + pv)
+            dS = p * (go @ v.t().contiguous() - (go * out).sum(1, keepdim=True))
+            dst = dS.t().contiguous()
+            dq, dk, dv = dS @ k * rs, dst @ q * rs, pt @ go
+            d[r, h] = dq
+            d[r, ik] += dk
+            d[r, iv] += dv
+            E = u * (go.abs() * (out.abs() + pv)).sum(1, keepdim=True)
+            aS = u * dS.abs() + p * E
+            db[r, h] = u * dq.abs() + aS @ k.abs() * rs
+            db[r, ik] += u * dk.abs() + aS.t().contiguous() @ q.abs() * rs
+            db[r, iv] += u * (dv.abs() + pt @ go.abs())
+    return tuple(t.reshape(t.shape[0], -1).cpu().numpy() for t in (o, lse, d, ob, db))
+
+
+def blocks(lens, H, Hkv, dh):
+    """(rows of a forward block, keys of a backward block, blocks of keys that are cut) of a bf16 packing with head size 64 or 128, from its lists: each
+    query list covers the batch once in blocks of its size, the list of keys in its."""
+    off, G = offsets(lens), H // Hkv
+    data = tio.tio_packing_build(off, "bf16", H, Hkv, dh).export()["data"]
+    data = data[(len(off) + 3) // 4 * 4:]
+    at = [(int(a), n) for a, n in zip(off, lens) if n]
+
+    def queries(i, rows):
+        """where the list that starts at word i ends, None if it is not one of blocks of `rows`"""
+        want = {(a, n, v) for a, n in at for v in range(0, n * G, rows)}
+        got = data[i:i + 4 * len(want)]
+        return i + len(got) if len(got) == 4 * len(want) and {tuple(map(int, w[:3])) for w in got.reshape(-1, 4)} == want else None
+    found = set()
+    for fwd in (64, 128):
+        for keys in (64, 128 if dh == 64 else 256):
+            end = queries(0, fwd)
+            if end is not None and keys != fwd:
+                end = queries(end, keys)
+            if end is None or (len(data) - end) % 8:
+                continue
+            rest = data[end:].reshape(-1, 8)
+            if {tuple(map(int, w[:3])) for w in rest[rest[:, 6] == 0]} == {(a, n, k) for a, n in at for k in range(0, n, keys)}:
+                found.add((fwd, keys, int((rest[:, 6] > 0).sum())))
+    assert len(found) == 1, found
+    return found.pop()
+
+
 def run_attention(lens, dtype, H, Hkv, dh, qkv, dO, extra_rows=0, pad=0, pad_o=0, stream=0, packed=None):
     """o, lse, dqkv as torch tensors with everything that is not to be written set to 7: extra rows behind the batch, pad columns."""
     import torch

@@ -356,3 +356,33 @@ def test_gradients_beside_rows_of_very_low_scores(dtype, lens, H, Hkv, dh, how, 
     rows, (_, _, d, _, db), got = _low_scores(dtype, lens, H, Hkv, dh, how, power, low=low)
     assert np.all(np.abs(got[2][rows] - d)[low:] <= db[low:] + 1e-30)
     assert np.isfinite(got[2][:rows.start]).all() and np.isfinite(got[2][rows.stop:]).all()
+
+
+# (rows of a forward block, keys of a backward block, whether blocks of keys are cut) of each batch: the kernels of large batches
+@pytest.mark.parametrize("lens,H,Hkv,dh,want", [
+    ([900, 11], 66, 2, 64, (64, 128, True)), ([900, 800, 14], 64, 16, 64, (64, 128, True)), ([1100, 9, 64], 64, 4, 64, (64, 128, True)),
+    ([800, 780, 300, 31, 1, 7], 64, 64, 64, (128, 128, False)), ([1000, 900, 9], 64, 32, 64, (128, 128, False)),
+    ([700, 690, 640, 513, 0, 9], 48, 8, 64, (128, 128, True)), ([700, 650, 600, 580, 12], 64, 8, 64, (128, 128, True)),
+    ([1500, 13], 40, 8, 128, (64, 256, True)), ([1500, 200, 9, 1], 32, 8, 128, (64, 256, True)), ([1500, 9], 32, 32, 128, (64, 256, False)),
+    ([1200, 9], 64, 8, 128, (128, 256, True)), ([1300, 3], 64, 2, 128, (128, 256, True)), ([1400, 11], 66, 2, 128, (128, 256, True)),
+    ([1000, 700, 0, 300, 15], 64, 64, 128, (128, 64, False))])
+def test_blocks_of_large_batches(lens, H, Hkv, dh, want):
+    """Values, and the precision of the first sixteen rows' dQ (see test_short_rows_keep_their_precision), where two groups of sixteen keys or query rows
+    belong to a wavefront: groups of heads that divide a tile and groups that do not, blocks of keys in one piece and in several."""
+    import torch
+    import packedlib as pl
+    fwd, keys, cut = pl.blocks(lens, H, Hkv, dh)
+    assert (fwd, keys, cut > 0) == want
+    print(f"packed attention in blocks of {fwd} rows and {keys} keys, {cut} cut: lens={lens} H={H} Hkv={Hkv} dh={dh}", flush=True)
+    qkv, dO = _inputs(lens, H, Hkv, dh, "bf16")
+    o, lse, d, ob, db = pl.attention_on("cuda", lens, H, Hkv, dh, qkv, dO, 2.0 ** -8)
+    got = [t.double().cpu().numpy() for t in pl.run_attention(lens, "bf16", H, Hkv, dh, qkv, dO)]
+    err = np.abs(got[0] - o)
+    assert np.all(err <= ob + 1e-30), ("o", float((err / (ob + 1e-30)).max()))
+    assert np.abs(got[1] - lse).max() <= 2e-5 * (1 + np.abs(lse).max())
+    err = np.abs(got[2] - d)
+    assert np.all(err <= db + 1e-30), ("dqkv", float((err / (db + 1e-30)).max()))
+    first = np.concatenate([a + np.arange(min(n, 16)) for a, n in zip(pl.offsets(lens), lens)])
+    once = torch.from_numpy(d).to(torch.bfloat16).double().numpy()
+    a, b = (np.linalg.norm(x[first, :H * dh] - d[first, :H * dh]) for x in (got[2], once))
+    assert a <= 1.5 * b, a / b

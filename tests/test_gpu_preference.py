@@ -240,3 +240,65 @@ def test_captured_and_replayed(dtype, lens):
         eager = _run(lens, dtype, a, b, c, 0.1, 0.0, V)
         for name, u, v in zip(("seq", "losses", "loss", "dlogits"), (seq, losses, loss, d), eager):
             assert torch.equal(u, v), (seed, name)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("V,masked", [(300, slice(100, 251)), (64, slice(0, 64)), (9000, slice(0, 8200)), (50257, slice(300, 50257))])
+@pytest.mark.parametrize("lens", [[4, 5, 3, 2], [4, 5, 3, 2] * 5], ids=["few", "many"])
+def test_logits_of_the_types_lowest_and_largest_value(dtype, V, masked, lens):
+    """Tokens taken out with the type's lowest value, all of a row's too, and the largest value, which times log2(e) are beyond 32 bits."""
+    import torch
+    print(f"preference, lowest and largest values {dtype} V={V} masked={masked} {len(lens)} sequences", flush=True)
+    x, y, ref = _inputs(lens, V, dtype, 0.0)
+    low = np.float32(torch.finfo(torch.bfloat16 if dtype == "bf16" else torch.float32).min)
+    x[:, masked] = low
+    x[1] = low                                             # every token as likely as every other
+    x[2] = low
+    x[2, :3] = [1.0, 2.0, 3.0]
+    y[2] = 1
+    x[5, :] = 0.0                                          # one token certain
+    x[5, 7] = -low
+    y[5] = 7
+    x[6, :] = low                                          # the same beside the lowest
+    x[6, 9] = -low
+    y[6] = 9
+    x[10, :] = 0.5 * low                                   # the row's largest is near the end of the range, and not alone
+    x[10, ::2] = 0.75 * low
+    y[10] = 11
+    at = np.arange(len(y))
+    assert x.shape[1] == V and (np.isfinite(x)).all()
+    keep = np.isin(at, (1, 2, 5, 6, 10))
+    x[~keep, y[~keep]] = 2.0                               # the label is possible
+    # the definition of logits less their row's largest, which is the same: of -3.4e38 + log V 64 bits lose log V
+    shifted = x.astype(np.float64) - x.max(1, keepdims=True).astype(np.float64)
+    seq, losses, loss, d, w, p = _definition(lens, shifted, y, ref, 0.1, 0.1, len(lens) // 2)
+    assert np.isfinite(seq).all() and np.isfinite(d).all()
+    got = [t.double().cpu().numpy() for t in _run(lens, dtype, x, y, ref, 0.1, 0.1, V)]
+    # the bounds of _check, where no row's largest logit is more than a few apart from those that count
+    row = 2.0 ** -17 * 2
+    of_seq = row * np.array(lens)
+    assert np.all(np.abs(got[0] - seq) <= of_seq + 2.0 ** -24 * np.abs(seq))
+    of_z = 0.1 * of_seq.reshape(-1, 2).sum(1)
+    h = seq - ref.astype(np.float64)
+    of_loss = 2.0 ** -24 * np.abs(0.1 * (h[0::2] - h[1::2])) + 2.0 ** -20 * np.abs(losses)
+    assert np.all(np.abs(got[1] - losses) <= of_z + of_loss + 1e-12)
+    assert abs(got[2][0] - loss) <= of_z.mean() + 2.0 ** -20 * abs(loss)
+    half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -23
+    onehot = np.zeros_like(p)
+    onehot[at, y] = 1
+    lim = half * np.abs(d) + (np.repeat(np.repeat(of_z, 2), lens)[:, None] + 4 * row) * np.abs(w)[:, None] * (p + onehot) + 2.0 ** -126
+    assert np.all(np.abs(got[3] - d) <= lim)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_label_of_the_types_lowest_value(dtype):
+    """The label of a preferred answer's row is as good as impossible: its pair's loss is -beta times the lowest value, nobody else's."""
+    import torch
+    lens, V = [2, 3, 2, 2], 100
+    x, y, ref = _inputs(lens, V, dtype, 0.0)
+    low = torch.finfo(torch.bfloat16 if dtype == "bf16" else torch.float32).min
+    x[1, y[1]] = low
+    seq, losses, loss, d, _, _ = _definition(lens, x, y, ref, 0.1, 0.0, 2)
+    got = [t.double().cpu().numpy() for t in _run(lens, dtype, x, y, ref, 0.1, 0.0, V)]
+    for g, want in zip(got, (seq, losses, np.array([loss]), d)):
+        assert np.isfinite(g).all() and np.all(np.abs(g - want) <= 2.0 ** -8 * np.abs(want) + 1e-4)

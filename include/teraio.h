@@ -406,7 +406,8 @@ int tio_op_attention_packed(void *stream, const tio_packing *packing, const void
  * by one call at a time.  dqkv overlaps none of the other buffers.  Where a key is infinite, the gradients of the queries that see it, and of
  * some before it, are not numbers in that component (zero times infinity).  The probabilities are taken from lse, whose rounding, 2^-24 of it, is their
  * relative error: a row whose scores are all beyond 1e5 in magnitude loses its own gradients and its share in those of the keys it sees, no others.
- * A row that sees nothing but scores of -inf makes gradients of its sequence not numbers. */
+ * A row that sees nothing but scores of -inf makes gradients of its sequence not numbers.  rows * H * dh stays below 2^35 - 2^11
+ * (TIO_ERR_INVALID_ARG otherwise; batches whose longest sequence is short go further). */
 int tio_op_attention_packed_work(const tio_packing *packing, uint64_t *out_bytes);
 int tio_op_attention_packed_bwd(void *stream, const tio_packing *packing, const void *packing_dev, const void *qkv, int64_t ld_qkv,
                                 const void *o, const void *dO, int64_t ld_o, const float *lse, void *work, void *dqkv);

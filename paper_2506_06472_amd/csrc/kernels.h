@@ -102,6 +102,7 @@ void attn_packed_bwd(hipStream_t s, const Packing &p, const void *device, const 
 // bytes of the backward pass's work; whether the longest sequence's rows are within the offsets the kernels use (host only)
 int64_t attn_packed_work(const Packing &p);
 bool attn_packed_fits(const Packing &p, int64_t ld, int64_t ldo);
+bool attn_packed_bwd_fits(const Packing &p);     // whether the backward pass's launches are within a grid
 // delta[h][row] = dO . o over a head
 void attn_packed_pre(hipStream_t s, int dtype, const void *dO, const void *o, int64_t ldo, float *delta, int64_t rows, int64_t H, int64_t dh);
 // in fp32 arithmetic (kernels_attn.hip)

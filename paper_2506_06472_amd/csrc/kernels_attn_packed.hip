@@ -117,8 +117,9 @@ template <int DH> void fwd(hipStream_t s, const Packing &p, const void *device, 
 }
 
 // The delta of short sequences is computed where it is needed, by every block of keys that a row meets, which saves a launch of 3 us (eight sequences of up
-// to 100 rows, 12 heads of 64 in 4 groups: forward and backward 19.6 -> 17.8 us); the bound is that of the kernels of one length.
-template <int DH, int NG> bool own_delta(const Packing &p) { return NG == 1 && (int64_t)p.max_len * p.group() * DH <= 65536; }
+// to 100 rows, 12 heads of 64 in 4 groups: forward and backward 19.6 -> 17.8 us); the bound is that of the kernels of one length.  In fp32 arithmetic
+// at head size 32.
+bool own_delta(const Packing &p) { return p.mfma ? p.keys == 64 && (int64_t)p.max_len * p.group() * p.dh <= 65536 : p.dh == 32; }
 
 // blocks of NW wavefronts of 16 NG keys or query rows
 template <int DH, int NW, int NG>
@@ -136,7 +137,7 @@ void both(hipStream_t s, const Packing &p, const void *device, const void *qkv, 
         if (rows_between_loads<DH, NW>() % p.group()) go(DELTA, std::true_type{});
         else go(DELTA, std::false_type{});
     };
-    if (own_delta<DH, NG>(p)) {
+    if (NG == 1 && own_delta(p)) {
         with(std::bool_constant<NG == 1>{});
     } else {
         attn_packed_pre(s, TIO_PREC_BF16, dO, o, ldo, delta, p.rows, p.H, DH);
@@ -169,6 +170,12 @@ bool attn_packed_fits(const Packing &p, int64_t ld, int64_t ldo) {
     constexpr int64_t PAST = 512;
     const int64_t most = ld > ldo ? ld : ldo;
     return most < ((int64_t)1 << 24) && (!p.mfma || ((int64_t)p.max_len + PAST) * most * 2 < ((int64_t)1 << 31));
+}
+
+// The launch over all rows and heads for delta, where it is not the gradients' own: a grid has fewer than 2^32 threads.
+bool attn_packed_bwd_fits(const Packing &p) {
+    const int64_t lanes = p.dh / (p.dtype == TIO_PREC_BF16 ? 8 : 4);
+    return own_delta(p) || (int64_t)p.rows * p.H * lanes < ((int64_t)1 << 32) - NT;
 }
 
 void attn_packed_fwd(hipStream_t s, const Packing &p, const void *device, const void *qkv, int64_t ld, void *o, int64_t ldo, float *lse) {

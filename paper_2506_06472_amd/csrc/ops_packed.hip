@@ -120,6 +120,7 @@ int tio_op_attention_packed_bwd(void *stream, const tio_packing *packing, const 
     if (const char *wrong = attention_args(packing, packing_dev, qkv, ld_qkv, o, ld_o, lse)) return fail(TIO_ERR_INVALID_ARG, wrong);
     if (!dO || !work || !dqkv) return fail(TIO_ERR_INVALID_ARG, "null argument");
     if (!aligned(dO) || !aligned(work) || !aligned(dqkv)) return fail(TIO_ERR_INVALID_ARG, BAD_POINTER);
+    if (!k::attn_packed_bwd_fits(packing->p)) return fail(TIO_ERR_INVALID_ARG, "too many rows times heads for the backward pass: cut the batch");
     if (!packing->p.rows) return TIO_OK;
     const OnDeviceOf device((hipStream_t)stream);
     k::attn_packed_bwd((hipStream_t)stream, packing->p, packing_dev, qkv, ld_qkv, o, dO, ld_o, lse, work, dqkv);

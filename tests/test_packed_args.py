@@ -176,3 +176,13 @@ def test_activation_refusals(bad):
             tio.tio_op_act_ckpt8_bwd(0, "bf16", a["act"], a["rows"], a["f"], a["kept"], P, 104, a["gate"], a["up"], a["ldu"], a["y"], a["ldy"])
     with pytest.raises(tio.TioError):
         tio.tio_op_act_ckpt8_bwd(0, "bf16", "swiglu", 4, 100, P, 0, 104, P, P, 104)
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,dh,rows", [("bf16", 64, 1, 128, 1 << 22), ("bf16", 64, 1, 64, 1 << 23), ("bf16", 7, 7, 128, 38400000)])
+def test_backward_passes_beyond_a_launch(dtype, H, Hkv, dh, rows):
+    """The launch for delta has a thread for every 16 bytes of dO, and a grid fewer than 2^32: refused before anything is launched."""
+    p = tio.tio_packing_build(np.arange(0, rows + 1, 12800 if rows % 12800 == 0 else 1 << 14), dtype, H, Hkv, dh)
+    ld, ldo = (H + 2 * Hkv) * dh, H * dh
+    with pytest.raises(tio.TioError, match="backward") as e:
+        tio.tio_op_attention_packed_bwd(0, p, P, P, ld, P, P, ldo, P, P, P)
+    assert e.value.code == -1

@@ -378,7 +378,7 @@ int tio_op_attention(void *stream, int32_t dtype, int64_t B, int64_t T, int64_t 
  * has rows offsets[s] .. offsets[s+1]-1.  tio_packing_build (pure CPU) checks the host array of n_seqs + 1 offsets (the first 0, never
  * smaller than the one before) and decides how the batch is cut into workgroups for attention with H query heads in
  * groups that share one of Hkv key heads (H a multiple of Hkv, at most 64 to a key head; dh 32, 64 or 128; rows * H < 2^31), in
- * element type dtype.  H = Hkv = dh = 0: without attention (the preference loss needs none).  The caller copies the
+ * element type dtype.  n_seqs stays below 2^28, and a batch of more blocks of rows than a launch holds is refused (TIO_ERR_INVALID_ARG).  H = Hkv = dh = 0: without attention (the preference loss needs none).  The caller copies the
  * view's `data` (`bytes` bytes) to device memory, 16-byte aligned, before the first call that takes it, and passes handle and
  * copy together; one packing serves all layers of a step, on any stream.  The calls below are asynchronous on `stream`, allocate
  * nothing, keep nothing between calls, and may be captured into a graph (which then holds this packing).  Rows behind the

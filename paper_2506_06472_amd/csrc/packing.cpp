@@ -51,21 +51,28 @@ void key_items(Packing &p, const int32_t *offsets, int keys, int per_tile, int64
     std::vector<std::pair<int64_t, KeyItem>> items, sums;
     for (int s = 0; s < p.n_seqs; ++s) {
         const int32_t first = offsets[s], len = offsets[s + 1] - first;
-        for (int32_t kv0 = 0; kv0 < len; kv0 += keys) {
-            const int64_t tiles = ((int64_t)len - kv0 + per_tile - 1) / per_tile, pieces = pieces_of(tiles, piece);
+        for (int64_t kv0 = 0; kv0 < len; kv0 += keys) {
+            const int64_t tiles = (len - kv0 + per_tile - 1) / per_tile, pieces = pieces_of(tiles, piece);
             if (pieces == 1) {
-                items.push_back({tiles, KeyItem{first, len, kv0, 0, (int32_t)tiles, -1, 0, 0}});
+                items.push_back({tiles, KeyItem{first, len, (int32_t)kv0, 0, (int32_t)tiles, -1, 0, 0}});
                 continue;
             }
-            sums.push_back({pieces, KeyItem{first, len, kv0, 0, 0, p.parts, (int32_t)pieces, 0}});
+            sums.push_back({pieces, KeyItem{first, len, (int32_t)kv0, 0, 0, p.parts, (int32_t)pieces, 0}});
             for (int64_t i = 0; i < pieces; ++i) {
                 const int64_t t0 = tiles * i / pieces, t1 = tiles * (i + 1) / pieces;
-                items.push_back({t1 - t0, KeyItem{first, len, kv0, (int32_t)t0, (int32_t)t1, p.parts++, 0, 0}});
+                items.push_back({t1 - t0, KeyItem{first, len, (int32_t)kv0, (int32_t)t0, (int32_t)t1, p.parts++, 0, 0}});
             }
         }
     }
     p.key = append(p, items);
     p.sums = append(p, sums);
+}
+
+int64_t key_blocks(const Packing &p, const int32_t *offsets, int keys, int per_tile, int64_t piece) {
+    int64_t n = 0;
+    for (int s = 0; s < p.n_seqs; ++s)
+        for (int64_t left = offsets[s + 1] - offsets[s]; left > 0; left -= keys) n += pieces_of((left + per_tile - 1) / per_tile, piece);
+    return n;
 }
 
 // How the backward pass is cut: the keys of a block (64 of four wavefronts with 16 keys each; or 128 of four, head size 64, and 256 of eight,
@@ -122,9 +129,10 @@ int64_t cut_backward(Packing &p, const int32_t *offsets, int per_tile) {
     return best_piece;
 }
 
-// a grid has fewer than 2^32 threads, of which a workgroup here has at most 512 (and the kernels in fp32 arithmetic one for every query head)
-void check_grids(const Packing &p) {
-    const int64_t heads = p.mfma ? p.Hkv : p.H, items = std::max<int64_t>(p.fwd.n, (int64_t)p.dq.n + p.key.n) + 32;
+// A grid has fewer than 2^32 threads, of which a workgroup here has at most 512 (and the kernels in fp32 arithmetic one for every query head).  Asked before the
+// lists are built: those of a batch that is refused could be larger than the host's memory.
+void check_grids(const Packing &p, int64_t fwd, int64_t dq, int64_t key) {
+    const int64_t heads = p.mfma ? p.Hkv : p.H, items = std::max(fwd, dq + key) + 32;
     if (items * heads >= ((int64_t)1 << 23)) throw std::invalid_argument("too many blocks of rows: cut the batch");
 }
 
@@ -132,6 +140,7 @@ void check_grids(const Packing &p) {
 
 Packing build_packing(const int32_t *offsets, int32_t n_seqs, int32_t dtype, int64_t H, int64_t Hkv, int64_t dh) {
     if (n_seqs < 1) throw std::invalid_argument("a packing needs at least one sequence");
+    if (n_seqs >= 1 << 28) throw std::invalid_argument("too many sequences");
     if (offsets[0] != 0) throw std::invalid_argument("the first offset must be 0");
     Packing p;
     p.n_seqs = n_seqs;
@@ -155,9 +164,10 @@ Packing build_packing(const int32_t *offsets, int32_t n_seqs, int32_t dtype, int
     const int group = p.group();
     if (!p.mfma) {                                   // every query head by itself
         p.fwd_rows = p.dq_rows = p.keys = 32;
+        const int64_t n = query_blocks(p, offsets, 32, 1);             // of keys as many
+        check_grids(p, n, n, n);
         p.fwd = p.dq = query_items(p, offsets, 32, 1);
         key_items(p, offsets, 32, 32, WHOLE);
-        check_grids(p);
         return p;
     }
     // Forward pass: sixteen rows to a wavefront while there are few blocks of 64 rows, and two sets of wavefronts to a block, which take every other tile of
@@ -170,12 +180,13 @@ Packing build_packing(const int32_t *offsets, int32_t n_seqs, int32_t dtype, int
     p.fwd_rows = blocks <= (dh == 64 ? 1800 : 1024) ? 64 : 128;
     p.fwd_sets = blocks <= (dh == 64 ? 512 : p.max_len >= 700 ? 400 : 256) ? 2 : 1;
     const int per_tile = rows_per_tile(true, group);
+    check_grids(p, 0, query_blocks(p, offsets, 256, group), query_blocks(p, offsets, 256, 1));           // the fewest there may be
     const int64_t piece = cut_backward(p, offsets, per_tile);
     p.dq_rows = p.keys;
+    check_grids(p, query_blocks(p, offsets, p.fwd_rows, group), query_blocks(p, offsets, p.dq_rows, group), key_blocks(p, offsets, p.keys, per_tile, piece));
     p.fwd = query_items(p, offsets, p.fwd_rows, group);
     p.dq = p.fwd_rows == p.dq_rows ? p.fwd : query_items(p, offsets, p.dq_rows, group);
     key_items(p, offsets, p.keys, per_tile, piece);
-    check_grids(p);
     return p;
 }
 

@@ -186,3 +186,23 @@ def test_backward_passes_beyond_a_launch(dtype, H, Hkv, dh, rows):
     with pytest.raises(tio.TioError, match="backward") as e:
         tio.tio_op_attention_packed_bwd(0, p, P, P, ld, P, P, ldo, P, P, P)
     assert e.value.code == -1
+
+
+@pytest.mark.parametrize("heads", [("fp32", 1, 1, 32), ("bf16", 1, 1, 32), ("bf16", 1, 1, 64), ("bf16", 1, 1, 128)])
+@pytest.mark.parametrize("rows", [(1 << 31) - 1, (1 << 31) - 200, (1 << 30) + 77])
+def test_one_sequence_of_nearly_all_rows_is_refused(heads, rows):
+    """Before any list is built: the lists of such a batch would take gigabytes, and its last block ends past 32 bits."""
+    import resource
+    before = resource.getrusage(resource.RUSAGE_SELF).ru_maxrss
+    with pytest.raises(tio.TioError, match="cut the batch") as e:
+        tio.tio_packing_build([0, rows], *heads)
+    assert e.value.code == -1
+    assert resource.getrusage(resource.RUSAGE_SELF).ru_maxrss - before < 1 << 16          # KiB
+
+
+def test_more_sequences_than_words_are_refused():
+    """By their number: no offset is looked at."""
+    import ctypes as C
+    off, out = (C.c_int32 * 1)(0), C.c_void_p()
+    for n in (1 << 28, (1 << 31) - 1):
+        assert tio.binding.lib().tio_packing_build(off, C.c_int32(n), 1, C.c_int64(0), C.c_int64(0), C.c_int64(0), C.byref(out)) == -1

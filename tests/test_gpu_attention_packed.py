@@ -386,3 +386,27 @@ def test_blocks_of_large_batches(lens, H, Hkv, dh, want):
     once = torch.from_numpy(d).to(torch.bfloat16).double().numpy()
     a, b = (np.linalg.norm(x[first, :H * dh] - d[first, :H * dh]) for x in (got[2], once))
     assert a <= 1.5 * b, a / b
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,dh", [("bf16", 4, 2, 64), ("bf16", 8, 8, 64), ("bf16", 5, 1, 128), ("fp32", 4, 2, 32)])
+@pytest.mark.parametrize("part", ["q", "k", "v"])
+def test_gradients_of_each_part_against_differences(dtype, H, Hkv, dh, part):
+    """sum(w * o) of the definition in 64 bits, a step either way in one of q, k and v, against the kernel's gradient along that direction.  The direction
+    is near the gradient's own, so that the derivative is large beside what the element-wise bounds allow: a gradient that is zero, half as large or
+    of the other sign does not pass.  Differences in 64 bits with a step of 1e-3 of norm 1: their error is of the step's square, 1e-6 of the third
+    derivative, which is of the derivative's size."""
+    import packedlib as pl
+    lens = [40, 1, 77]
+    qkv, dO = _inputs(lens, H, Hkv, dh, dtype)
+    _, _, d, _, db = pl.attention(lens, H, Hkv, dh, qkv, dO, 2.0 ** -8 if dtype == "bf16" else 1e-5)
+    first = {"q": 0, "k": H, "v": H + Hkv}[part]
+    cols = slice(first * dh, (first + (H if part == "q" else Hkv)) * dh)
+    v = np.zeros_like(d)
+    v[:, cols] = d[:, cols] * np.random.default_rng(7).uniform(0.5, 1.5, d[:, cols].shape)
+    v /= np.linalg.norm(v)
+    t = 1e-3
+    f = [float((pl.attention(lens, H, Hkv, dh, qkv.astype(np.float64) + s * t * v, dO, 0.0)[0] * dO).sum()) for s in (1, -1)]
+    slope, limit = (f[0] - f[1]) / (2 * t), float((db * np.abs(v)).sum())
+    assert limit < slope / 2.5
+    got = pl.run_attention(lens, dtype, H, Hkv, dh, qkv, dO)[2].double().cpu().numpy()
+    assert abs(slope - (got * v).sum()) <= limit + 1e-5 * slope

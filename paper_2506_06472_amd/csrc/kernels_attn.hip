@@ -502,10 +502,15 @@ void launch_bwd(hipStream_t s, const BwdArgs<T, W> &a, unsigned key_blocks, unsi
     }
     if constexpr (own_delta<DH>()) {
         const bool eight = eight_wavefronts((int64_t)key_blocks + query_blocks, longest, DH);
-        if (a.O && eight) launch_both<Rows, T, DH, 8, true>(s, a, key_blocks, query_blocks);
-        else if (a.O) launch_both<Rows, T, DH, 4, true>(s, a, key_blocks, query_blocks);
-        else if (eight) launch_both<Rows, T, DH, 8, false>(s, a, key_blocks, query_blocks);
-        else launch_both<Rows, T, DH, 4, false>(s, a, key_blocks, query_blocks);
+        if constexpr (!W::GROUPED) {                       // a packed batch's calls have O
+            if (!a.O) {
+                if (eight) launch_both<Rows, T, DH, 8, false>(s, a, key_blocks, query_blocks);
+                else launch_both<Rows, T, DH, 4, false>(s, a, key_blocks, query_blocks);
+                return;
+            }
+        }
+        if (eight) launch_both<Rows, T, DH, 8, true>(s, a, key_blocks, query_blocks);
+        else launch_both<Rows, T, DH, 4, true>(s, a, key_blocks, query_blocks);
     } else {
         launch_both<Rows, T, DH, 4, false>(s, a, key_blocks, query_blocks);
     }
@@ -522,6 +527,8 @@ void launch_fwd(hipStream_t s, const W &where, unsigned grid, T *o, float *lse, 
     if (eight_wavefronts(grid, longest, DH)) attn_fwd_k<Rows, T, DH, MANY><<<grid, MANY * 64, 0, s>>>(where, o, lse, scale);
     else attn_fwd_k<Rows, T, DH, 4><<<grid, 256, 0, s>>>(where, o, lse, scale);
 }
+// whether a packed batch comes here: in bf16 the other head sizes have kernels_attn_packed.hip
+template <typename T, int DH> constexpr bool packed_f32() { return sizeof(T) == 4 || DH == 32; }
 template <typename T> PackedBlocks<T> packed_blocks(const Packing &p, const void *device, const void *qkv, int64_t ld, int64_t ldg) {
     return PackedBlocks<T>{(const T *)qkv, ld, ldg, p.H, p.Hkv, packed_places(p, device, p.fwd, sizeof(QueryItem) / 4, p.H),
                            packed_places(p, device, p.key, sizeof(KeyItem) / 4, p.Hkv)};
@@ -580,8 +587,10 @@ void attn_bwd(hipStream_t s, int dtype, const void *dO, const void *qkv, const v
 
 void attn_packed_fwd_f32(hipStream_t s, const Packing &p, const void *device, const void *qkv, int64_t ld, void *o, int64_t ldo, float *lse, float scale) {
     TIO_ATTN_DISPATCH(p.dtype, p.dh, {
-        const PackedBlocks<T> where = packed_blocks<T>(p, device, qkv, ld, ldo);
-        launch_fwd<T, DH>(s, where, where.query.grid(), (T *)o, lse, scale, p.max_len, false);
+        if constexpr (packed_f32<T, DH>()) {
+            const PackedBlocks<T> where = packed_blocks<T>(p, device, qkv, ld, ldo);
+            launch_fwd<T, DH>(s, where, where.query.grid(), (T *)o, lse, scale, p.max_len, false);
+        }
     });
 }
 
@@ -620,9 +629,11 @@ void attn_packed_bwd_f32(hipStream_t s, const Packing &p, const void *device, co
     const bool own = p.dh == 32;
     if (!own) attn_packed_pre(s, p.dtype, dO, o, ldo, delta, p.rows, p.H, p.dh);
     TIO_ATTN_DISPATCH(p.dtype, p.dh, {
-        const PackedBlocks<T> where = packed_blocks<T>(p, device, qkv, ld, ldo);
-        const BwdArgs<T, PackedBlocks<T>> a{where, (const T *)dO, own ? (const T *)o : nullptr, lse, delta, (T *)dqkv, scale};
-        launch_bwd<T, DH>(s, a, where.key.grid(), where.query.grid(), p.max_len, false);
+        if constexpr (packed_f32<T, DH>()) {
+            const PackedBlocks<T> where = packed_blocks<T>(p, device, qkv, ld, ldo);
+            const BwdArgs<T, PackedBlocks<T>> a{where, (const T *)dO, own ? (const T *)o : nullptr, lse, delta, (T *)dqkv, scale};
+            launch_bwd<T, DH>(s, a, where.key.grid(), where.query.grid(), p.max_len, false);
+        }
     });
 }
 

@@ -240,3 +240,43 @@ def test_activation_of_inputs_whose_square_is_infinite(dtype, act):
     if two:
         k = torch.from_numpy(pl.kept_values(t[:1, :n].double().cpu().numpy())[0, ::32]).cuda().to(du.dtype)
         assert torch.equal(du[0, :n:32], torch.where(is_up, k, 0.0).to(du.dtype))
+
+
+@pytest.mark.parametrize("dtype,act,rows,cols", [("bf16", "none", 16400, 8250), ("fp32", "none", 16400, 8250), ("bf16", "gelu", 16400, 8250),
+                                                 ("fp32", "gelu", 16400, 8250), ("bf16", "swiglu", 8200, 8250), ("fp32", "swiglu", 8200, 8250)])
+def test_large_checkpoints_are_those_of_their_parts(dtype, act, rows, cols):
+    """A checkpoint of more than 128 MiB (which goes past the caches) has the bytes, outputs and gradients that its rows have in parts."""
+    import torch
+    import paper_2506_06472_amd as tio
+    print(f"large checkpoint {dtype} {act} {rows} x {cols}", flush=True)
+    t, halves, ld = _types(dtype), 2 if act == "swiglu" else 1, (cols + 7) // 8 * 8
+    blocks, need = (cols + 31) // 32, tio.tio_ckpt8_bytes(rows, cols)
+    assert halves * need > 128 << 20
+    g = torch.Generator(device="cuda").manual_seed(rows + cols)
+    x = torch.randn((halves, rows, ld), device="cuda", generator=g).to(t)
+    dy = torch.randn((rows, ld), device="cuda", generator=g).to(t)
+
+    def run(first, n):
+        size = tio.tio_ckpt8_bytes(n, cols)
+        kept = torch.zeros(halves * size, device="cuda", dtype=torch.uint8)
+        y, again, dx = torch.zeros((n, ld), device="cuda", dtype=t), torch.zeros((n, ld), device="cuda", dtype=t), torch.zeros((halves, n, ld), device="cuda", dtype=t)
+        at = [x[i, first:first + n].data_ptr() for i in range(halves)]
+        if act == "none":
+            tio.tio_op_ckpt8_store(0, dtype, n, cols, at[0], ld, kept.data_ptr())
+            tio.tio_op_ckpt8_load(0, dtype, n, cols, kept.data_ptr(), dx.data_ptr(), ld)
+        else:
+            two = halves == 2
+            tio.tio_op_act_ckpt8(0, dtype, act, n, cols, at[0], at[1] if two else 0, ld, y.data_ptr(), ld, kept.data_ptr())
+            tio.tio_op_act_ckpt8_bwd(0, dtype, act, n, cols, kept.data_ptr(), dy[first:first + n].data_ptr(), ld, dx.data_ptr(), dx[1].data_ptr() if two else 0, ld,
+                                     again.data_ptr(), ld)
+        torch.cuda.synchronize()
+        half = [kept[i * size:(i + 1) * size] for i in range(halves)]
+        return y, again, dx, [h[:n * blocks * 32].view(n, -1) for h in half], [h[n * blocks * 32:n * blocks * 33].view(n, -1) for h in half]
+    torch.cuda.synchronize()
+    whole = run(0, rows)
+    for first in range(0, rows, 4100):
+        n = min(4100, rows - first)
+        part, r = run(first, n), slice(first, first + n)
+        assert torch.equal(whole[0][r], part[0]) and torch.equal(whole[1][r], part[1]) and torch.equal(whole[2][:, r], part[2])
+        for i in range(halves):
+            assert torch.equal(whole[3][i][r], part[3][i]) and torch.equal(whole[4][i][r], part[4][i])

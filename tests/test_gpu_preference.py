@@ -302,3 +302,10 @@ def test_label_of_the_types_lowest_value(dtype):
     got = [t.double().cpu().numpy() for t in _run(lens, dtype, x, y, ref, 0.1, 0.0, V)]
     for g, want in zip(got, (seq, losses, np.array([loss]), d)):
         assert np.isfinite(g).all() and np.all(np.abs(g - want) <= 2.0 ** -8 * np.abs(want) + 1e-4)
+
+
+@pytest.mark.parametrize("dtype,lens,V", [("bf16", [40000, 30000, 5, 3], 40), ("fp32", [65535, 1, 65536, 2], 17), ("bf16", [1, 2] * 6000, 24)])
+@pytest.mark.parametrize("grad", ["apart", "in place"])
+def test_more_rows_than_a_launch_of_the_gradient(dtype, lens, V, grad):
+    """Rows past 65535, whose gradient takes several launches, and thousands of pairs."""
+    _check(lens, V, dtype, grad=grad, s=0.1)

@@ -410,3 +410,19 @@ def test_gradients_of_each_part_against_differences(dtype, H, Hkv, dh, part):
     assert limit < slope / 2.5
     got = pl.run_attention(lens, dtype, H, Hkv, dh, qkv, dO)[2].double().cpu().numpy()
     assert abs(slope - (got * v).sum()) <= limit + 1e-5 * slope
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,dh,ld", [("bf16", 4, 2, 64, 1 << 20), ("bf16", 5, 1, 128, 1 << 20), ("fp32", 4, 2, 64, 1 << 19), ("bf16", 4, 2, 32, 1 << 20)])
+def test_rows_beyond_4_gib(dtype, H, Hkv, dh, ld):
+    """Buffers whose later sequences lie past 32-bit offsets: the bits of rows side by side."""
+    import torch
+    import packedlib as pl
+    lens = [511] * 5 + [31, 257]                           # (511 + 512) 2^21 bytes: the longest that a stride of 2^20 bf16 elements allows
+    print(f"packed attention in rows of {ld} elements {dtype} H={H} Hkv={Hkv} dh={dh}", flush=True)
+    qkv, dO = _inputs(lens, H, Hkv, dh, dtype)
+    assert sum(lens[:-1]) * ld * (2 if dtype == "bf16" else 4) > 1 << 32
+    near = pl.run_attention(lens, dtype, H, Hkv, dh, qkv, dO)
+    far = pl.run_attention(lens, dtype, H, Hkv, dh, qkv, dO, pad=ld - (H + 2 * Hkv) * dh, pad_o=ld - H * dh)
+    assert all(torch.equal(a, b) for a, b in zip(near, far))
+    del far
+    torch.cuda.empty_cache()

@@ -280,3 +280,37 @@ def test_large_checkpoints_are_those_of_their_parts(dtype, act, rows, cols):
         assert torch.equal(whole[0][r], part[0]) and torch.equal(whole[1][r], part[1]) and torch.equal(whole[2][:, r], part[2])
         for i in range(halves):
             assert torch.equal(whole[3][i][r], part[3][i]) and torch.equal(whole[4][i][r], part[4][i])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rows_beyond_4_gib(dtype):
+    """Strides that take the later rows past 32-bit offsets: the values of rows side by side."""
+    import torch
+    import paper_2506_06472_amd as tio
+    import packedlib as pl
+    rows, cols, ld = 2500, 100, 1 << 20
+    x = _values(rows, cols, dtype)
+    t = torch.full((rows, ld), float("nan"), device="cuda", dtype=_types(dtype))
+    t[:, :cols] = torch.from_numpy(x).cuda().to(t.dtype)
+    kept = torch.zeros(2 * tio.tio_ckpt8_bytes(rows, cols), device="cuda", dtype=torch.uint8)
+    tio.tio_op_ckpt8_store(0, dtype, rows, cols, t.data_ptr(), ld, kept.data_ptr())
+    t.fill_(7.0)
+    tio.tio_op_ckpt8_load(0, dtype, rows, cols, kept.data_ptr(), t.data_ptr(), ld)
+    torch.cuda.synchronize()
+    want = pl.kept_values(x)
+    assert np.array_equal(t[:, :cols].double().cpu().numpy(), want) and (t[:, 104:] == 7.0).all()
+    # an activation of two halves of one matrix, and its gradients, against its rows side by side
+    t[:, :cols] = torch.from_numpy(x).cuda().to(t.dtype)
+    t[:, 128:128 + cols] = t[:, :cols].flip(0)
+    near = t[:, :232].contiguous()
+    got = []
+    for src, n in ((t, ld), (near, 232)):
+        y, dg, du = (torch.zeros_like(src) for _ in range(3))
+        tio.tio_op_act_ckpt8(0, dtype, "swiglu", rows, cols, src.data_ptr(), src[:, 128:].data_ptr(), n, y.data_ptr(), n, kept.data_ptr())
+        tio.tio_op_act_ckpt8_bwd(0, dtype, "swiglu", rows, cols, kept.data_ptr(), y.data_ptr(), n, dg.data_ptr(), du.data_ptr(), n)
+        torch.cuda.synchronize()
+        got.append([a[:, :cols].clone() for a in (y, dg, du)])
+        del y, dg, du
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    del t
+    torch.cuda.empty_cache()

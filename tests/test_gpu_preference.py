@@ -309,3 +309,18 @@ def test_label_of_the_types_lowest_value(dtype):
 def test_more_rows_than_a_launch_of_the_gradient(dtype, lens, V, grad):
     """Rows past 65535, whose gradient takes several launches, and thousands of pairs."""
     _check(lens, V, dtype, grad=grad, s=0.1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lens", [[40, 33, 5, 20], [1200, 700, 300, 200, 3, 1]], ids=["few", "many"])
+def test_rows_beyond_4_gib(dtype, lens):
+    """Strides that take the later rows past 32-bit offsets: the bits of rows side by side."""
+    import torch
+    V, rows = 4100, sum(lens)
+    x, y, ref = _inputs(lens, V, dtype, 0.3)
+    near = _run(lens, dtype, x, y, ref, 0.1, 0.1, V)
+    ld = (5 << 30) // (rows * (2 if dtype == "bf16" else 4)) // 8 * 8
+    far = _run(lens, dtype, x, y, ref, 0.1, 0.1, V, pad=ld - (V + 7) // 8 * 8)
+    assert all(torch.equal(a, b) for a, b in zip(near, far))
+    del far
+    torch.cuda.empty_cache()

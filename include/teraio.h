@@ -435,7 +435,7 @@ int tio_op_preference_loss(void *stream, int32_t dtype, const tio_packing *packi
  * stands for NaNs.  A checkpoint of [rows, cols] is tio_ckpt8_bytes bytes (a multiple of 16; 33 for each block) of one buffer, to be
  * moved as a whole; its layout is the library's.  Matrices are rows of ld elements, a multiple of 8 and at least cols rounded up to 8;
  * the padding up to there is not used where a matrix is read, and gets zeros where one is written.  Pointers are 16-byte aligned, buffers
- * do not overlap, rows * cols (rounded up to 32) stays below 2^34. */
+ * do not overlap, rows and cols are at most 2^31 - 2^10 and rows * cols (rounded up to 32) at most 2^34 - 2^13. */
 enum { TIO_ACT_GELU = 0, TIO_ACT_SWIGLU = 1 };
 int tio_ckpt8_bytes(int64_t rows, int64_t cols, uint64_t *out_bytes);
 int tio_op_ckpt8_store(void *stream, int32_t dtype, int64_t rows, int64_t cols, const void *x, int64_t ldx, void *ckpt);

@@ -63,7 +63,7 @@ const char *attention_args(const tio_packing *packing, const void *device, const
 const char *matrix_args(int32_t dtype, int64_t rows, int64_t cols) {
     if (!known_type(dtype)) return "unknown element type";
     if (rows < 1 || cols < 1) return "non-positive dimension";
-    if (!k::ckpt8_fits(rows, cols)) return "rows times columns must stay below 2^34";
+    if (!k::ckpt8_fits(rows, cols)) return "rows and columns must be at most 2^31 - 2^10, their product (rounded up to 32 columns) at most 2^34 - 2^13";
     return nullptr;
 }
 bool stride_ok(int64_t ld, int64_t cols) { return ld % 8 == 0 && ld >= (cols + 7) / 8 * 8; }

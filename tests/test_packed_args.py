@@ -206,3 +206,15 @@ def test_more_sequences_than_words_are_refused():
     off, out = (C.c_int32 * 1)(0), C.c_void_p()
     for n in (1 << 28, (1 << 31) - 1):
         assert tio.binding.lib().tio_packing_build(off, C.c_int32(n), 1, C.c_int64(0), C.c_int64(0), C.c_int64(0), C.byref(out)) == -1
+
+
+@pytest.mark.parametrize("rows,cols,fits", [(8, (1 << 31) - 1024, True), (8, (1 << 31) - 1023, False), (9, (1 << 31) - 1024, False), ((1 << 29) - 256, 32, True),
+                                            ((1 << 29) - 256, 33, False), ((1 << 29) - 255, 32, False), ((1 << 28) - 128, 64, True), ((1 << 31) - 1024, 1, False)])
+def test_largest_checkpoints(rows, cols, fits):
+    """The limits that the header gives: 2^34 - 2^13 values in whole blocks of 32."""
+    assert fits == (rows * ((cols + 31) // 32 * 32) <= (1 << 34) - (1 << 13) and max(rows, cols) <= (1 << 31) - 1024)
+    if fits:
+        assert tio.tio_ckpt8_bytes(rows, cols) == (rows * ((cols + 31) // 32) * 33 + 15) // 16 * 16
+    else:
+        with pytest.raises(tio.TioError, match="2.34"):
+            tio.tio_ckpt8_bytes(rows, cols)

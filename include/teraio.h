@@ -377,12 +377,13 @@ int tio_op_attention(void *stream, int32_t dtype, int64_t B, int64_t T, int64_t 
  * A packed batch is n_seqs sequences of different lengths (zero among them) one behind the other, without padding: sequence s
  * has rows offsets[s] .. offsets[s+1]-1.  tio_packing_build (pure CPU) checks the host array of n_seqs + 1 offsets (the first 0, never
  * smaller than the one before) and decides how the batch is cut into workgroups for attention with H query heads in
- * groups that share one of Hkv key heads (H a multiple of Hkv, at most 64 to a key head; dh 32, 64 or 128; rows * H < 2^31), in
- * element type dtype.  n_seqs stays below 2^28, and a batch of more blocks of rows than a launch holds is refused (TIO_ERR_INVALID_ARG).  H = Hkv = dh = 0: without attention (the preference loss needs none).  The caller copies the
- * view's `data` (`bytes` bytes) to device memory, 16-byte aligned, before the first call that takes it, and passes handle and
- * copy together; one packing serves all layers of a step, on any stream.  The calls below are asynchronous on `stream`, allocate
- * nothing, keep nothing between calls, and may be captured into a graph (which then holds this packing).  Rows behind the
- * last sequence are neither read nor written. */
+ * groups that share one of Hkv key heads (H a multiple of Hkv, at most 65536, at most 64 to a key head; dh 32, 64 or 128;
+ * rows * H < 2^31), in element type dtype.  n_seqs stays below 2^28, and a batch of more blocks of rows than a launch holds is refused
+ * (TIO_ERR_INVALID_ARG).  H = Hkv = dh = 0: without attention (the preference loss needs none).  The caller copies the view's `data`
+ * (`bytes` bytes) to device memory, 16-byte aligned, before the first call that takes it, and passes handle and copy together; one
+ * packing serves all layers of a step, on any stream.  The calls below are asynchronous on `stream`, allocate nothing, keep nothing
+ * between calls, and may be captured into a graph (which then holds this packing).  Rows behind the last sequence are neither read nor
+ * written. */
 typedef struct tio_packing tio_packing;
 typedef struct tio_packing_view {
     int32_t n_seqs, rows, max_len, reserved;
@@ -395,19 +396,24 @@ void tio_packing_free(tio_packing *packing);
 
 /* Causal self-attention of every sequence over itself.  qkv: rows of ld_qkv elements that begin with H heads of q, Hkv of k and Hkv
  * of v, dh elements each; query head h uses key head h / (H / Hkv).  o: rows of ld_o elements that begin with H heads; lse: fp32
- * [H, rows], the log-sum-exp of the scores scaled by 1/sqrt(dh).  Strides are multiples of 8 elements, device pointers 16-byte
- * aligned.  A sequence's rows, at the larger stride, must span less than 2 GiB (TIO_ERR_INVALID_ARG otherwise).  What stands between
- * the heads and the stride is not touched.  Scores of -inf (keys with an infinite component) are probabilities of zero; a row that sees no
- * other has an o that is not a number.  Finite scores, of whatever size, have their softmax. */
+ * [H, rows], the log-sum-exp of the scores scaled by 1/sqrt(dh).  Strides are multiples of 8 elements below 2^24, device pointers
+ * 16-byte aligned.  bf16 with dh 64 or 128: the longest sequence's rows and 512 more, at the larger stride, span less than 2 GiB
+ * (TIO_ERR_INVALID_ARG otherwise).  What stands between the heads and the stride is not touched.  Scores of -inf (keys with an infinite
+ * component) are probabilities of zero; a row that sees no other has an o that is not a number.  Finite scores, of whatever size, have
+ * their softmax.  Any other infinity or NaN in a sequence may reach all results of that sequence, and none of another's.
+ * Scores, softmax and sums are in 32 bits.  bf16 with dh 64 or 128: the probabilities, and in the backward pass the scores' gradients,
+ * are rounded to bf16 for the products that follow, beside the rounding of the results
+ * (norm of the error against the result's, on normal values: o 2.1e-3 where one rounding leaves 1.6e-3, gradients 2.4e-3 and 1.7e-3). */
 int tio_op_attention_packed(void *stream, const tio_packing *packing, const void *packing_dev, const void *qkv, int64_t ld_qkv,
                             void *o, int64_t ld_o, float *lse);
 /* Gradients of all of q | k | v (dqkv: rows as those of qkv, same stride; its heads only) from dO (rows as those of o), the forward
  * pass's o and lse, and `work`: device memory of tio_op_attention_packed_work bytes, contents of no interest before and after, used
- * by one call at a time.  dqkv overlaps none of the other buffers.  Where a key is infinite, the gradients of the queries that see it, and of
- * some before it, are not numbers in that component (zero times infinity).  The probabilities are taken from lse, whose rounding, 2^-24 of it, is their
- * relative error: a row whose scores are all beyond 1e5 in magnitude loses its own gradients and its share in those of the keys it sees, no others.
- * A row that sees nothing but scores of -inf makes gradients of its sequence not numbers.  rows * H * dh stays below 2^35 - 2^11
- * (TIO_ERR_INVALID_ARG otherwise; batches whose longest sequence is short go further). */
+ * by one call at a time.  dqkv overlaps none of the other buffers.  Where a key is infinite, the gradients of the queries that see it,
+ * and of some before it, are not numbers in that component (zero times infinity).  The probabilities are taken from lse, whose rounding
+ * makes them off by 2^-23 |lse| of their size: a row whose scores are all beyond 1e5 in magnitude has gradients off by a per cent, one beyond
+ * 1e7 loses its own and its share in those of the keys it sees, no others.  A row that sees nothing but scores of -inf makes gradients of its
+ * sequence not numbers.
+ * rows * H * dh stays below 2^35 - 2^11 (TIO_ERR_INVALID_ARG otherwise; batches whose longest sequence is short go further). */
 int tio_op_attention_packed_work(const tio_packing *packing, uint64_t *out_bytes);
 int tio_op_attention_packed_bwd(void *stream, const tio_packing *packing, const void *packing_dev, const void *qkv, int64_t ld_qkv,
                                 const void *o, const void *dO, int64_t ld_o, const float *lse, void *work, void *dqkv);
@@ -422,14 +428,16 @@ int tio_op_attention_packed_bwd(void *stream, const tio_packing *packing, const 
  * gradient of loss[0], in rows like the logits', with zeros in rows that do not count and up to the next multiple of 16 bytes behind
  * V; it may be the logits' own buffer, and otherwise overlaps none.  beta > 0, 0 <= smoothing <= 1.  work: device memory of
  * tio_op_preference_loss_work bytes, contents of no interest before and after, used by one call at a time.  16-byte aligned: logits,
- * dlogits, work and the packing's copy.  At most 2^22 - 1 rows, and as many pairs. */
+ * dlogits, work and the packing's copy.  At most 2^22 - 1 rows, and as many pairs; V at most 2^28.  Logits may have any value of their type;
+ * -inf is a probability of zero, and a row of nothing else, an infinity or a NaN spoils its pair.  Log probabilities are summed in 64 bits, a
+ * row's exponentials and a pair's loss and weight are in 32. */
 int tio_op_preference_loss_work(const tio_packing *packing, uint64_t *out_bytes);
 int tio_op_preference_loss(void *stream, int32_t dtype, const tio_packing *packing, const void *packing_dev, int64_t V, const void *logits,
                            int64_t ld, const int32_t *labels, const float *ref_logp, float beta, float smoothing, int64_t total_pairs,
                            float *seq_logp, float *losses, float *loss, void *work, void *dlogits);
 
-/* Activations kept in 8 bits between the forward and the backward pass (half the bytes of bf16 to hold, or to move to a slow tier and
- * back).  Blocks of 32 neighbours of a row share a power of two: with a the block's largest magnitude and e = max(floor(log2 a), -120),
+/* Activations kept in 8 bits between the forward and the backward pass: half the bytes of bf16 to hold, or for a caller to move to a slower
+ * memory and back (the plans and the runtime above move their own tensors only, and have no checkpoints among them).  Blocks of 32 neighbours of a row share a power of two: with a the block's largest magnitude and e = max(floor(log2 a), -120),
  * an element x becomes q = clamp(round(x 2^(6-e)), -127, 127), ties to even, and stands for q 2^(e-6).  These values are exact in bf16 and in
  * fp32; they are at most half a step 2^(e-6) from x (a whole one where the clamp takes part).  A block with an infinity or a NaN
  * stands for NaNs.  A checkpoint of [rows, cols] is tio_ckpt8_bytes bytes (a multiple of 16; 33 for each block) of one buffer, to be

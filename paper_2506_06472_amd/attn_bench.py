@@ -5,9 +5,10 @@
 Forward alone, and forward plus backward (row-sum pre-pass, dQ launch, dK/dV launches): operands resident in device
 memory, standard normal values, the average over --reps back-to-back calls between two HIP events on the launch
 stream.  The rates count the algorithmic flops of causal attention: 4 B H T^2 dh / 2 forward, 2.5 times that backward
-(what the kernels execute is more: the backward launches recompute the scores, and tiles on the diagonal whole).  --packed times tio_op_attention_packed on batches of sequences of different lengths with grouped heads, the packing
-built outside the timed region.  --vendor times torch's scaled_dot_product_attention (the vendor's fused attention) on the same shapes instead,
-on contiguous [B, H, T, dh] operands made outside the timed region: a yardstick, nothing the library or its tests use.
+(what the kernels execute is more: the backward launches recompute the scores, and tiles on the diagonal are computed
+whole).  --packed times tio_op_attention_packed on batches of sequences of different lengths with grouped heads, the
+packing built outside the timed region.  --vendor times torch's scaled_dot_product_attention (the vendor's fused
+attention) on the same shapes instead, on contiguous [B, H, T, dh] operands made outside the timed region: a yardstick, nothing the library or its tests use.
 """
 import argparse
 

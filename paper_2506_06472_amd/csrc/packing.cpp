@@ -79,9 +79,9 @@ int64_t key_blocks(const Packing &p, const int32_t *offsets, int keys, int per_t
 // head size 128, with 32 each, which do a product for half the reads but are fewer and take longer for a tile) and the tiles of a piece.
 // The time is estimated as that of the tiles, dealt evenly, or of the longest chain of them if that is longer, a quarter of the shorter of the two, and
 // the partial sums' way to memory and back.  us; fitted to 480 ways to cut 30 batches (2 to 52 heads, groups of 1 to 13, 370 to 8192 rows), of which
-// it picks the fastest or one within 6 %, 0.6 % behind on average.  12 heads in 4 groups, 64, 8192 rows of 17 sequences: 256 x 1 piece 98 us,
-// 64 x 1 piece 77, 128 x 16 tiles 59; 32 heads in 8 groups, 128, 8192 rows of 8: 396 whole, 365 in pieces of 64, 410 with 64 keys; 7 heads, 128, 2600
-// rows of two: 514 whole, 75 in pieces of 16, 53 with 64 keys.
+// it picks the fastest or one within 6 %, 0.6 % behind on average.  Backward, us: 12 heads in 4 groups, 64, 8192 rows of 17 sequences: 128 keys whole 101,
+// in pieces of 16 tiles 61, 64 keys whole 80, in pieces of 16 61; 32 heads in 8 groups, 128, 8192 rows of 8: 256 keys whole 398, in pieces of 64 364, 64 keys
+// whole 421; 7 heads, 128, 2600 rows of two: 256 keys whole 524, in pieces of 16 73, 64 keys whole 265, in pieces of 16 52.
 struct Way {
     int keys;
     double tile, chain, fixed;                       // a tile among others (per compute unit), a tile of a chain, the rest

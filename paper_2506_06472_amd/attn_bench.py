@@ -8,7 +8,8 @@ stream.  The rates count the algorithmic flops of causal attention: 4 B H T^2 dh
 (what the kernels execute is more: the backward launches recompute the scores, and tiles on the diagonal are computed
 whole).  --packed times tio_op_attention_packed on batches of sequences of different lengths with grouped heads, the
 packing built outside the timed region.  --vendor times torch's scaled_dot_product_attention (the vendor's fused
-attention) on the same shapes instead, on contiguous [B, H, T, dh] operands made outside the timed region: a yardstick, nothing the library or its tests use.
+attention) on the same shapes instead, on contiguous [B, H, T, dh] operands made outside the timed region: a
+yardstick, nothing the library or its tests use.
 """
 import argparse
 

@@ -459,6 +459,77 @@ int tio_op_act_ckpt8(void *stream, int32_t dtype, int32_t act, int64_t rows, int
 int tio_op_act_ckpt8_bwd(void *stream, int32_t dtype, int32_t act, int64_t rows, int64_t f, const void *ckpt, const void *dy,
                          int64_t lddy, void *dgate, void *dup, int64_t ldu, void *y, int64_t ldy);
 
+/* ---- a decoder layer trained in 8-bit floating point: single operators on caller-provided device buffers --------------------
+ * They are asynchronous on `stream`, allocate nothing, keep nothing between calls, and may be captured into a graph.  Matrices are rows of
+ * ld elements, a multiple of 8 and at least the columns rounded up to 8; the columns up to there are not used where a matrix is read, and get
+ * zeros where one is written.  Device pointers, 16-byte aligned; buffers do not overlap but where said.
+ *
+ * Matrices stored in 8 bits.  Blocks of 128 neighbours of a row (tiles = 1: of 128 x 128 elements) share a power of two: with a the block's
+ * largest magnitude and M = 448 (e4m3) or 57344 (e5m2), e = max(the smallest e with a <= M 2^e, -110); an element x becomes the
+ * nearest code of x 2^-e, ties to even, and stands for code 2^e, a number that bf16 and fp32 hold exactly (but for magnitudes of 1.9375 2^127 and
+ * above, which become infinite, as they may in a rounding to bf16).  A block with an infinity or a NaN stands for NaNs.  tio_op_fp8_store writes
+ * the matrix (out, NULL for none) and, from the same pass, its transposed one (out_t, NULL for none), in blocks along ITS rows, for the products of
+ * the backward pass; each takes tio_fp8_bytes(rows, cols) of its own rows and columns (a multiple of 64).  The layout is the library's, made for the
+ * matrix cores; a stored matrix is moved as a whole.  rows and cols are at most 2^22, their product (rounded up to 16 and 128) at most 2^36. */
+enum { TIO_FP8_E4M3 = 0, TIO_FP8_E5M2 = 1 };
+int tio_fp8_bytes(int64_t rows, int64_t cols, uint64_t *out_bytes);
+int tio_op_fp8_store(void *stream, int32_t dtype, int32_t form, int32_t tiles, int64_t rows, int64_t cols, const void *x, int64_t ldx, void *out,
+                     void *out_t);
+/* The values that a stored matrix stands for. */
+int tio_op_fp8_load(void *stream, int32_t dtype, int32_t form, int64_t rows, int64_t cols, const void *in, void *x, int64_t ldx);
+/* C[M,N] = A . B^T (+ bias[N]) (+ resid[M,N]) of the values that the stored matrices A [M,K] and B [N,K] stand for; C, bias and resid are of
+ * dtype, C may be resid.  A linear layer y = x w^T: y = (x, w), dx = (dy, w transposed), dw = (dy transposed, x transposed).  fp32: values, products
+ * and sums are those of fp32 arithmetic.  bf16: the matrix cores add 8-bit products, 128 at a time, to the 32-bit sum with products more than 13
+ * bits below the largest of their neighbours cut off; the error of that, 1.2e-5 of the result's norm on normal values, is a hundredth of the
+ * rounding to bf16.  work: device memory of tio_op_gemm_fp8_work bytes (0: NULL will do), contents of no interest before and after, used by one call
+ * at a time. */
+int tio_op_gemm_fp8_work(int64_t M, int64_t N, int64_t K, uint64_t *out_bytes);
+int tio_op_gemm_fp8(void *stream, int32_t dtype, int64_t M, int64_t N, int64_t K, int32_t form_a, const void *A, int32_t form_b, const void *B, const void *bias,
+                    const void *resid, int64_t ldr, void *C, int64_t ldc, void *work);
+
+/* Dropout from a counter.  The 16 bits of element (row, col) are half-word col % 8 (low halves first) of the four words that Philox-4x32 with
+ * ten rounds gives for the counter (row ceil(cols / 8) + col / 8, offset), two words each, under the key `seed`.  With T = p 65536
+ * rounded to the nearest integer (ties to even; at most 65535), an element is dropped, that is zero whatever it was, where its bits are below T, and
+ * multiplied by 65536 / (65536 - T) elsewhere.  The same seed, offset and shape give the same mask: the backward pass of y = dropout(x) + resid is
+ * the same call on dy without resid, and a program that draws several masks takes another offset for each.
+ * y = dropout(x) (+ resid); y may be x or resid.  rows ceil(cols / 8) is below 2^31. */
+int tio_op_dropout(void *stream, int32_t dtype, int64_t rows, int64_t cols, const void *x, int64_t ldx, const void *resid, int64_t ldr, void *y, int64_t ldy,
+                   double p, uint64_t seed, uint64_t offset);
+
+/* Between two blocks of a layer, rows of d elements (at most 16384, rows at most 2^31):
+ *   n = N(branch; post_gain, post_bias), or branch without post_gain;   u = dropout(n), a mask of [rows, d] as above;
+ *   y = resid_scale x + branch_scale gate u;   h = N(y; gain, bias)
+ * N(v; g, b) = (v - mean) / sqrt(mean((v - mean)^2) + eps) g + b, or with rms v / sqrt(mean(v^2) + eps) g.  gate: NULL, one row for all rows (ldg =
+ * 0) or rows of stride ldg.  Biases may be NULL, with rms they are.  h is computed from y before its rounding.  branch, x, y, h and the gradients of
+ * the first two, dy and dh have stride ld; y may be x.  stats: [rows][4] fp32 for the backward pass (branch's mean and 1/sqrt, y's; the first two are
+ * not written without post_gain). */
+typedef struct tio_residual_cfg {
+    int32_t rms;
+    float eps, resid_scale, branch_scale;
+    double p;                        /* 0: no dropout */
+    uint64_t seed, offset;
+} tio_residual_cfg;
+int tio_op_residual_norm(void *stream, int32_t dtype, const tio_residual_cfg *cfg, int64_t rows, int64_t d, int64_t ld, const void *branch, const void *x,
+                         const void *gate, int64_t ldg, const void *post_gain, const void *post_bias, const void *gain, const void *bias, void *y, void *h,
+                         float *stats);
+/* Gradients from dy (of y where it goes on as the residual) and dh, the same cfg, branch, the forward pass's y and stats.  dgate (where there is a
+ * gate) is one row, the sum over the rows, or rows like the gate's; dpost_gain (where there is post_gain), dgain, and of the layer norm dpost_bias and
+ * dbias (NULL: not wanted) are rows summed over all rows, in 32 bits and always in the same order.  dx may be dy.  work: device memory of
+ * tio_op_residual_norm_bwd_work bytes, contents of no interest before and after, used by one call at a time. */
+int tio_op_residual_norm_bwd_work(int64_t rows, int64_t d, uint64_t *out_bytes);
+int tio_op_residual_norm_bwd(void *stream, int32_t dtype, const tio_residual_cfg *cfg, int64_t rows, int64_t d, int64_t ld, const void *branch, const void *y,
+                             const void *gate, int64_t ldg, const void *post_gain, const void *post_bias, const void *gain, const float *stats,
+                             const void *dy, const void *dh, void *dx, void *dbranch, void *dgate, void *dpost_gain, void *dpost_bias, void *dgain, void *dbias,
+                             void *work);
+
+/* Rotary positions with several axes (time, height, width) on rows that begin with `heads` heads of dh elements (a multiple of 8, at most
+ * 256), say the q and k heads of a packed qkv: x's heads, rotated, in y, which may be x; nothing behind them is touched.  Axis a (1 to 8 of them) has
+ * the next sections[a] >= 1 pairs of neighbouring elements (host array), their sum at most dh / 2; what is behind the last pair is copied.  Pair i of a head
+ * turns by positions[row][a] theta^(-2i / dh), or with own_ladder, pair j of its axis by positions[row][a] theta^(-j / sections[a]).  positions: device
+ * int32 [rows][n_axes].  Angles are in 64 bits.  inverse: by the negative angles, which is the gradient. */
+int tio_op_rope_axes(void *stream, int32_t dtype, int64_t rows, int64_t heads, int64_t dh, const void *x, int64_t ldx, void *y, int64_t ldy,
+                     const int32_t *positions, int32_t n_axes, const int32_t *sections, float theta, int32_t own_ladder, int32_t inverse);
+
 /* Measuring aid: launch number kernel_index of the schedule, repeated reps times on the compute stream with the
  * uncapped layout (the arena must hold it) and whatever the arena contains, HIP events around the repetitions;
  * returns average ns per launch.  It overwrites that launch's outputs, and a launch that updates its operands in place

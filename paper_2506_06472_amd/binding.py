@@ -16,6 +16,7 @@ LIB_PATH = os.path.join(_HERE, "libteraio.so")
 ARCH = {"gpt": 0, "llama": 1}
 PREC = {"fp32": 0, "bf16": 1}
 ACT = {"gelu": 0, "swiglu": 1}
+FP8 = {"e4m3": 0, "e5m2": 1}
 PROFILE_MEASURED, PROFILE_MODELLED, PROFILE_OFFLOADED = 0, 1, 2
 OFFLOAD, PREFETCH = 0, 1
 
@@ -99,14 +100,22 @@ class PackingView(C.Structure):
                [("data", C.POINTER(C.c_int32)), ("bytes", C.c_uint64)]
 
 
+class ResidualCfg(C.Structure):
+    _fields_ = [("rms", C.c_int32), ("eps", C.c_float), ("resid_scale", C.c_float), ("branch_scale", C.c_float), ("p", C.c_double),
+                ("seed", C.c_uint64), ("offset", C.c_uint64)]
+
+
 _lib = None
-# Argument types of the operators on packed batches and 8-bit checkpoints (p: pointer, i: int32, l: int64, f: float), declared once: their smallest calls take
-# a few microseconds on the GPU, and an object for each argument costs 0.4 us of the 3.7 that a call takes the host.
-_KINDS = {"p": C.c_void_p, "i": C.c_int32, "l": C.c_int64, "f": C.c_float}
+# Argument types of the operators on packed batches, of 8-bit checkpoints and of layers in 8 bits (p: pointer, i: int32, l: int64, f: float, d: double, u: uint64),
+# declared once: their smallest calls take a few microseconds on the GPU, and an object for each argument costs 0.4 us of the 3.7 that a call takes the host.
+_KINDS = {"p": C.c_void_p, "i": C.c_int32, "l": C.c_int64, "f": C.c_float, "d": C.c_double, "u": C.c_uint64}
 _SIGNATURES = {
     "tio_op_attention_packed": "ppppl" "plp", "tio_op_attention_packed_bwd": "ppppl" "pplppp",
     "tio_op_preference_loss": "pipplplppfflppppp", "tio_op_ckpt8_store": "pillplp", "tio_op_ckpt8_load": "pillppl",
     "tio_op_act_ckpt8": "piillpplplp", "tio_op_act_ckpt8_bwd": "piillpplpplpl",
+    "tio_op_fp8_store": "piiillplpp", "tio_op_fp8_load": "piillppl", "tio_op_gemm_fp8": "pilll" "ipip" "pplplp",
+    "tio_op_dropout": "pillplplpl" "duu", "tio_op_rope_axes": "pilll" "plplp" "ipfii",
+    "tio_op_residual_norm": "piplll" "ppplppppppp", "tio_op_residual_norm_bwd": "piplll" "ppplpppp" "pppppppppp",
 }
 
 
@@ -585,5 +594,77 @@ def tio_op_act_ckpt8(stream_handle, dtype, act, rows, f, gate_ptr, up_ptr, ldu, 
 
 def tio_op_act_ckpt8_bwd(stream_handle, dtype, act, rows, f, ckpt_ptr, dy_ptr, lddy, dgate_ptr, dup_ptr, ldu, y_ptr=0, ldy=0):
     rc = lib().tio_op_act_ckpt8_bwd(stream_handle, PREC[dtype], ACT[act], rows, f, ckpt_ptr, dy_ptr, lddy, dgate_ptr, dup_ptr, ldu, y_ptr, ldy)
+    if rc:
+        _check(rc)
+
+
+# ------------------------------------------------------------------ a layer in 8-bit floating point
+def _number_of(call, *sizes) -> int:
+    n = C.c_uint64()
+    _check(call(*[C.c_int64(v) for v in sizes], C.byref(n)))
+    return n.value
+
+
+def tio_fp8_bytes(rows, cols) -> int:
+    return _number_of(lib().tio_fp8_bytes, rows, cols)
+
+
+def tio_op_fp8_store(stream_handle, dtype, form, tiles, rows, cols, x_ptr, ldx, out_ptr, out_t_ptr=0):
+    rc = lib().tio_op_fp8_store(stream_handle, PREC[dtype], FP8[form], tiles, rows, cols, x_ptr, ldx, out_ptr, out_t_ptr)
+    if rc:
+        _check(rc)
+
+
+def tio_op_fp8_load(stream_handle, dtype, form, rows, cols, in_ptr, x_ptr, ldx):
+    rc = lib().tio_op_fp8_load(stream_handle, PREC[dtype], FP8[form], rows, cols, in_ptr, x_ptr, ldx)
+    if rc:
+        _check(rc)
+
+
+def tio_op_gemm_fp8_work(M, N, K) -> int:
+    return _number_of(lib().tio_op_gemm_fp8_work, M, N, K)
+
+
+def tio_op_gemm_fp8(stream_handle, dtype, M, N, K, form_a, A_ptr, form_b, B_ptr, C_ptr, ldc, bias_ptr=0, resid_ptr=0, ldr=0, work_ptr=0):
+    rc = lib().tio_op_gemm_fp8(stream_handle, PREC[dtype], M, N, K, FP8[form_a], A_ptr, FP8[form_b], B_ptr, bias_ptr, resid_ptr, ldr, C_ptr, ldc, work_ptr)
+    if rc:
+        _check(rc)
+
+
+def tio_op_dropout(stream_handle, dtype, rows, cols, x_ptr, ldx, resid_ptr, ldr, y_ptr, ldy, p, seed, offset):
+    rc = lib().tio_op_dropout(stream_handle, PREC[dtype], rows, cols, x_ptr, ldx, resid_ptr, ldr, y_ptr, ldy, p, seed, offset)
+    if rc:
+        _check(rc)
+
+
+def tio_residual_cfg(rms, eps=1e-5, resid_scale=1.0, branch_scale=1.0, p=0.0, seed=0, offset=0) -> ResidualCfg:
+    return ResidualCfg(1 if rms else 0, eps, resid_scale, branch_scale, p, seed, offset)
+
+
+def tio_op_residual_norm(stream_handle, dtype, cfg, rows, d, ld, branch_ptr, x_ptr, gate_ptr, ldg, post_gain_ptr, post_bias_ptr, gain_ptr, bias_ptr, y_ptr,
+                         h_ptr, stats_ptr):
+    rc = lib().tio_op_residual_norm(stream_handle, PREC[dtype], C.byref(cfg), rows, d, ld, branch_ptr, x_ptr, gate_ptr, ldg, post_gain_ptr, post_bias_ptr,
+                                    gain_ptr, bias_ptr, y_ptr, h_ptr, stats_ptr)
+    if rc:
+        _check(rc)
+
+
+def tio_op_residual_norm_bwd_work(rows, d) -> int:
+    return _number_of(lib().tio_op_residual_norm_bwd_work, rows, d)
+
+
+def tio_op_residual_norm_bwd(stream_handle, dtype, cfg, rows, d, ld, branch_ptr, y_ptr, gate_ptr, ldg, post_gain_ptr, post_bias_ptr, gain_ptr, stats_ptr,
+                             dy_ptr, dh_ptr, dx_ptr, dbranch_ptr, dgate_ptr, dpost_gain_ptr, dpost_bias_ptr, dgain_ptr, dbias_ptr, work_ptr):
+    rc = lib().tio_op_residual_norm_bwd(stream_handle, PREC[dtype], C.byref(cfg), rows, d, ld, branch_ptr, y_ptr, gate_ptr, ldg, post_gain_ptr,
+                                        post_bias_ptr, gain_ptr, stats_ptr, dy_ptr, dh_ptr, dx_ptr, dbranch_ptr, dgate_ptr, dpost_gain_ptr,
+                                        dpost_bias_ptr, dgain_ptr, dbias_ptr, work_ptr)
+    if rc:
+        _check(rc)
+
+
+def tio_op_rope_axes(stream_handle, dtype, rows, heads, dh, x_ptr, ldx, y_ptr, ldy, positions_ptr, sections, theta, own_ladder=False, inverse=False):
+    n = len(sections)
+    rc = lib().tio_op_rope_axes(stream_handle, PREC[dtype], rows, heads, dh, x_ptr, ldx, y_ptr, ldy, positions_ptr, n, (C.c_int32 * n)(*sections), theta,
+                                own_ladder, inverse)
     if rc:
         _check(rc)

@@ -129,6 +129,53 @@ void act_ckpt8(hipStream_t s, int dtype, bool swiglu, int64_t rows, int64_t f, c
                void *kept);
 void act_ckpt8_bwd(hipStream_t s, int dtype, bool swiglu, int64_t rows, int64_t f, const void *kept, const void *dy, int64_t lddy, void *dgate,
                    void *dup, int64_t ldu, void *y, int64_t ldy);
+// ---- layers trained in 8-bit floating point.  form: 0 e4m3, 1 e5m2
+bool fp8_fits(int64_t rows, int64_t cols);
+int64_t fp8_bytes(int64_t rows, int64_t cols);
+// tiles: one power of two for 128 x 128 elements; out, outt: the matrix and its transposed one, nullptr for either
+void fp8_store(hipStream_t s, int dtype, int form, bool tiles, int64_t rows, int64_t cols, const void *x, int64_t ld, void *out, void *outt);
+void fp8_load(hipStream_t s, int dtype, int form, int64_t rows, int64_t cols, const void *in, void *x, int64_t ld);
+struct Fp8Product {
+    int64_t M, N, K;
+    int form_a;
+    const void *A;
+    int form_b;
+    const void *B;
+    const void *bias, *resid;                    // nullptr: none
+    int64_t ldr;
+    void *C;
+    int64_t ldc;
+    void *work;
+};
+int64_t gemm_fp8_work(int64_t M, int64_t N, int64_t K);
+void gemm_fp8(hipStream_t s, int dtype, const Fp8Product &p);
+// a mask from a counter (philox.h)
+struct Dropout {
+    uint32_t key0, key1, offset0, offset1;
+    uint32_t limit;                              // elements whose 16 bits are below are dropped; 0: none
+    float scale;                                 // what the others are multiplied by
+};
+struct ResidualArgs {
+    bool rms;
+    float eps, resid_scale, branch_scale;
+    Dropout drop;
+    int64_t rows, d, ld, ldg;                    // ldg: 0 for one gate for all rows
+    const void *branch, *x, *gate, *post_gain, *post_bias, *gain, *bias;     // gate, post_gain, biases: nullptr for none
+    void *y, *h;
+    float *stats;
+    const void *dy, *dh;                         // the backward pass
+    void *dx, *dbranch, *dgate, *dpost_gain, *dpost_bias, *dgain, *dbias, *work;
+};
+constexpr int64_t RESIDUAL_WIDEST = 16384;
+int64_t residual_norm_bwd_work(int64_t rows, int64_t d);
+void residual_norm(hipStream_t s, int dtype, const ResidualArgs &a);
+void residual_norm_bwd(hipStream_t s, int dtype, const ResidualArgs &a);
+bool dropout_fits(int64_t rows, int64_t cols);
+void dropout(hipStream_t s, int dtype, int64_t rows, int64_t cols, const void *x, int64_t ldx, const void *resid, int64_t ldr, void *y, int64_t ldy,
+             const Dropout &d);
+constexpr int ROPE_PAIRS = 128;                  // of a head, at most
+void rope_axes(hipStream_t s, int dtype, int64_t rows, int heads, int dh, const void *x, int64_t ldx, void *y, int64_t ldy, const int32_t *pos, int axes,
+               const int32_t *sections, float theta, bool own_ladder, bool inverse);
 void embed_bwd(hipStream_t s, int dtype, const void *dx, const int32_t *tok, void *dwte, int64_t S, int64_t d,
                int64_t V, bool accumulate);
 void posemb_bwd(hipStream_t s, int dtype, const void *dx, void *dwpe, int64_t B, int64_t T, int64_t d, bool accumulate);

@@ -1,0 +1,39 @@
+// Eight neighbours of a row: 16 bytes of bf16, or 32 of fp32.
+#pragma once
+#include "device_common.h"
+
+namespace tio {
+namespace k {
+
+template <typename T> struct Row8;
+template <> struct Row8<bf16_t> {
+    Vec16<bf16_t> v;
+    __device__ __forceinline__ void clear() { v.raw = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void load(const bf16_t *p) { v.load(p); }
+    __device__ __forceinline__ void store(bf16_t *p) const { v.store(p); }
+    __device__ __forceinline__ void put(bf16_t *p) const { __builtin_nontemporal_store(__builtin_bit_cast(tio_u32x4, v.raw), reinterpret_cast<tio_u32x4 *>(p)); }
+    __device__ __forceinline__ void get(float *f) const { v.get(f); }
+    __device__ __forceinline__ void set(const float *f) { v.set(f); }
+};
+template <> struct Row8<float> {
+    Vec16<float> lo, hi;
+    __device__ __forceinline__ void clear() { lo.raw = hi.raw = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void load(const float *p) { lo.load(p); hi.load(p + 4); }
+    __device__ __forceinline__ void store(float *p) const { lo.store(p); hi.store(p + 4); }
+    __device__ __forceinline__ void put(float *p) const {                    // past the caches
+        __builtin_nontemporal_store(__builtin_bit_cast(tio_u32x4, lo.raw), reinterpret_cast<tio_u32x4 *>(p));
+        __builtin_nontemporal_store(__builtin_bit_cast(tio_u32x4, hi.raw), reinterpret_cast<tio_u32x4 *>(p + 4));
+    }
+    __device__ __forceinline__ void get(float *f) const { lo.get(f); hi.get(f + 4); }
+    __device__ __forceinline__ void set(const float *f) { lo.set(f); hi.set(f + 4); }
+};
+// columns from n on become zero
+__device__ __forceinline__ void cut8(float *f, int n) {
+    if (n >= 8) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j >= n) f[j] = 0.f;
+}
+
+}  // namespace k
+}  // namespace tio

@@ -1,0 +1,227 @@
+"""GPU: matrices stored in 8-bit floating point with a power of two per block of 128, and their products, against the definition in 64 bits."""
+import numpy as np
+import pytest
+
+import layer8lib as l8
+
+pytestmark = pytest.mark.gpu
+
+
+def _values(rows, cols, dtype, seed=0):
+    rng = np.random.default_rng(rows * 1000 + cols + seed)
+    x = rng.standard_normal((rows, cols)) * np.exp2(rng.integers(-6, 7, (rows, 1))) * np.exp2(rng.integers(-3, 4, (1, cols)))
+    return l8.rounded(x.astype(np.float32), dtype)
+
+
+def _store(x, dtype, form, tiles, which="both"):
+    """(buffer or None, buffer or None) of x and of its transposed; nothing behind them is written"""
+    import torch
+    import paper_2506_06472_amd as tio
+    rows, cols = x.shape
+    t = l8.padded(x, dtype)
+    need = tio.tio_fp8_bytes(rows, cols), tio.tio_fp8_bytes(cols, rows)
+    bufs = [torch.full((n + 64,), 77, device="cuda", dtype=torch.uint8) if which in ("both", w) else None for n, w in zip(need, ("plain", "transposed"))]
+    tio.tio_op_fp8_store(0, dtype, form, tiles, rows, cols, t.data_ptr(), t.stride(0), *[0 if b is None else b.data_ptr() for b in bufs])
+    for b, n in zip(bufs, need):
+        assert b is None or (b[n:] == 77).all()
+    return bufs
+
+
+def _load(buf, dtype, form, rows, cols):
+    import torch
+    import paper_2506_06472_amd as tio
+    out = torch.full((rows + 1, (cols + 7) // 8 * 8 + 8), 7.0, device="cuda", dtype=l8.types(dtype))
+    tio.tio_op_fp8_load(0, dtype, form, rows, cols, buf.data_ptr(), out.data_ptr(), out.stride(0))
+    return l8.clean(out, cols, 7.0, rows)
+
+
+def _same(got, want):
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    assert np.array_equal(np.nan_to_num(got, nan=5.0), np.nan_to_num(want, nan=5.0))
+
+
+SIZES = [(1, 1), (1, 128), (3, 129), (16, 8), (17, 100), (64, 256), (65, 127), (128, 128), (129, 300), (257, 515), (1021, 96)]
+
+
+@pytest.mark.parametrize("tiles", [False, True])
+@pytest.mark.parametrize("form", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,cols", SIZES)
+def test_round_trip(rows, cols, dtype, form, tiles):
+    x = _values(rows, cols, dtype)
+    want = l8.stored(x, form, tiles)
+    want_t = want.T if tiles else l8.stored(np.ascontiguousarray(x.T), form)
+    plain, trans = _store(x, dtype, form, tiles)
+    for d in ("bf16", "fp32"):                                  # the values are exact in both
+        _same(_load(plain, d, form, rows, cols), want)
+        _same(_load(trans, d, form, cols, rows), want_t)
+    import torch
+    a, b = _store(x, dtype, form, tiles, "plain")[0], _store(x, dtype, form, tiles, "transposed")[1]
+    assert torch.equal(a, plain) and torch.equal(b, trans)      # either form alone has the same bytes
+
+
+@pytest.mark.parametrize("tiles", [False, True])
+@pytest.mark.parametrize("form", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_special_values(dtype, form, tiles):
+    """Zeros, ties, the largest codes, subnormal codes and numbers, huge magnitudes, blocks that are not finite."""
+    x = np.zeros((16, 256))
+    top = 448.0 if form == "e4m3" else 57344.0
+    x[0, :128] = np.arange(128) / 16 + 1.0 / 32
+    x[1, :5] = [top, top * (1 - 2.0 ** -7), -top, 1.0, 0.5]
+    x[2, :4] = [1.75, 1.7578125, -1.5, 2.0 ** -9]               # at and above 1.75: the next power of two
+    x[3, :3] = [2.0, 1.0625, 1.1875]                            # ties to even
+    x[4, :64] = np.exp2(-np.arange(64.0))                       # down to subnormal codes and zero
+    x[5, :3] = [2.0 ** -120, 2.0 ** -126, -2.0 ** -119]         # the smallest block
+    x[5, 128:131] = [2.0 ** -127, 1.5 * 2.0 ** -128, 2.0 ** -133]
+    x[6, 0] = 1.75 * 2.0 ** 127
+    x[7, :2] = [1.9921875 * 2.0 ** 127, 2.0 ** 120]             # rounds to 2^128
+    x[8, 3] = np.inf
+    x[9, 200] = np.nan
+    x[10, 255] = -np.inf
+    x[11, :] = -0.0
+    if tiles:                                                   # one power for all of them: a case at a time
+        cases = [np.concatenate([x[i:i + 1], np.full((2, 256), 2.0 ** -130)]) for i in range(12)]
+    else:
+        cases = [x]
+    for c in cases:
+        if dtype == "bf16":
+            c = l8.rounded(c, dtype)
+        want = l8.stored(c, form, tiles)
+        plain, trans = _store(c, dtype, form, tiles)
+        _same(_load(plain, dtype, form, *c.shape), want)
+        _same(_load(trans, dtype, form, c.shape[1], c.shape[0]), want.T if tiles else l8.stored(np.ascontiguousarray(c.T), form))
+
+
+def _product(a, b, dtype, fa, fb, bias=None, resid=None, tiles_b=False, in_place=False):
+    """C of stored a [M, K] and b [N, K], and the values that they stand for"""
+    import torch
+    import paper_2506_06472_amd as tio
+    (M, K), N = a.shape, b.shape[0]
+    qa, qb = _store(a, "fp32", fa, False, "plain")[0], _store(b, "fp32", fb, tiles_b, "plain")[0]
+    t = [None if v is None else l8.padded(v, dtype) for v in (bias, resid)]
+    c = torch.full((M + 1, (N + 7) // 8 * 8 + 8), 7.0, device="cuda", dtype=l8.types(dtype))
+    if in_place:
+        c[:M, :N] = t[1][:, :N]
+        t[1] = c
+    work = torch.full((tio.tio_op_gemm_fp8_work(M, N, K) + 64,), 255, device="cuda", dtype=torch.uint8)
+    ptr = [0 if v is None else v.data_ptr() for v in t]
+    tio.tio_op_gemm_fp8(0, dtype, M, N, K, fa, qa.data_ptr(), fb, qb.data_ptr(), c.data_ptr(), c.stride(0), ptr[0], ptr[1], 0 if t[1] is None else t[1].stride(0),
+                        work.data_ptr())
+    assert (work[-64:] == 255).all()
+    return l8.clean(c, N, 7.0, M), l8.stored(a, fa), l8.stored(b, fb, tiles_b)
+
+
+def _bound(a, b, want, dtype, extra=0.0):
+    """Rounding of the result (twice: the type's half step of a value off by the rest), a rounding of 32 bits for each of K sums and two more, and in bf16 what the
+    matrix cores cut off: of each product in a block of 128 at most 2^-13 of the largest."""
+    K = a.shape[1]
+    total = np.abs(a) @ np.abs(b).T + extra
+    err = (K + 4) * l8.E32 * total
+    if dtype == "bf16":
+        for k in range(0, K, 128):
+            err += 128 * 2.0 ** -13 * np.max(np.abs(a[:, None, k:k + 128] * b[None, :, k:k + 128]), axis=2)
+    return l8.U[dtype] * np.abs(want) + 1.01 * err + 1e-37
+
+
+PRODUCTS = [(1, 1, 1), (1, 40, 129), (2, 515, 352), (4, 1000, 256), (15, 16, 640), (16, 17, 128), (17, 33, 127), (33, 64, 1000), (64, 200, 384), (100, 64, 4200),
+            (128, 128, 256), (130, 257, 136), (256, 256, 512), (257, 300, 100), (512, 520, 1152)]
+
+
+@pytest.mark.parametrize("forms", [("e4m3", "e4m3"), ("e5m2", "e4m3"), ("e4m3", "e5m2"), ("e5m2", "e5m2")])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("M,N,K", PRODUCTS)
+def test_product(M, N, K, dtype, forms):
+    if forms != ("e4m3", "e4m3") and M > 256:
+        pytest.skip("large sizes with one pair of forms")
+    a, b = _values(M, K, "fp32"), _values(N, K, "fp32", 1)
+    got, qa, qb = _product(a, b, dtype, *forms, tiles_b=forms[1] == "e4m3")
+    want = qa @ qb.T
+    assert (np.abs(got - want) <= _bound(qa, qb, want, dtype)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("M,N,K", [(1, 40, 129), (33, 64, 1000), (130, 257, 136), (257, 300, 1100), (700, 900, 300)])
+def test_product_of_small_whole_numbers_is_exact(M, N, K, dtype):
+    """Products up to 2^6 with sums below 2^24 are exact however they are added, and a misplaced element shows; results are rounded once."""
+    rng = np.random.default_rng(K)
+    a, b = rng.integers(-8, 9, (M, K)).astype(float), rng.integers(-8, 9, (N, K)).astype(float)
+    a[:, 0], b[:, 0] = 8, 8
+    got, qa, qb = _product(a, b, dtype, "e4m3", "e4m3")
+    assert np.array_equal(qa, a) and np.array_equal(qb, b)
+    assert np.array_equal(got, l8.rounded(a @ b.T, dtype))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("M,N,K", [(4, 100, 300), (70, 77, 128), (300, 270, 520)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_product_with_bias_and_residual(M, N, K, dtype, in_place):
+    a, b = _values(M, K, "fp32"), _values(N, K, "fp32", 1)
+    rng = np.random.default_rng(5)
+    bias, resid = l8.rounded(rng.standard_normal((1, N)) * 30, dtype), l8.rounded(rng.standard_normal((M, N)) * 100, dtype)
+    for x, r in ((bias, None), (None, resid), (bias, resid)):
+        if in_place and r is None:
+            continue
+        got, qa, qb = _product(a, b, dtype, "e4m3", "e5m2", x, r, in_place=in_place)
+        add = (0 if x is None else x) + (0 if r is None else r)
+        want = qa @ qb.T + add
+        assert (np.abs(got - want) <= _bound(qa, qb, want, dtype, np.abs(0 if x is None else x) + np.abs(0 if r is None else r))).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("M,N,K", [(4, 40, 300), (300, 270, 260)])
+def test_product_with_blocks_that_are_not_finite(M, N, K, dtype):
+    """An infinity or a NaN spoils its rows and columns, and no others."""
+    a, b = _values(M, K, "fp32"), _values(N, K, "fp32", 1)
+    a[2, K - 1], a[3, 0], b[N - 1, 5] = np.inf, np.nan, -np.inf
+    got, qa, qb = _product(a, b, dtype, "e4m3", "e4m3")
+    bad = np.zeros((M, N), bool)
+    bad[2], bad[3], bad[:, N - 1] = True, True, True
+    assert np.isnan(got[bad]).all() and np.isfinite(got[~bad]).all()
+    fine = np.ix_([i for i in range(M) if i not in (2, 3)], range(N - 1))
+    want = (qa @ qb.T)[fine]
+    rows = [i for i in range(M) if i not in (2, 3)]
+    assert (np.abs(got[fine] - want) <= _bound(qa[rows], qb[:-1], want, dtype)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_scales_far_apart(dtype):
+    """Blocks from 2^-100 to 2^100 in the two operands of one product."""
+    a, b = _values(20, 384, "fp32"), _values(30, 384, "fp32", 1)
+    s = np.repeat([100.0, 0.0, -100.0], 128)
+    got, qa, qb = _product((a * np.exp2(s)).astype(np.float32).astype(float), (b * np.exp2(-s)).astype(np.float32).astype(float), dtype, "e4m3", "e4m3")
+    want = qa @ qb.T
+    assert (np.abs(got - want) <= _bound(qa, qb, want, dtype)).all()
+
+
+def test_calls_in_a_graph_and_on_another_stream():
+    """A linear layer's calls captured once and replayed on new values, with eager work in between; the same bits as eager calls."""
+    import torch
+    import paper_2506_06472_amd as tio
+    S, K, N = 200, 260, 150
+    up = lambda n: (n + 7) // 8 * 8
+    x, w, y = (torch.zeros((r, up(c)), device="cuda", dtype=torch.bfloat16) for r, c in ((S, K), (N, K), (S, N)))
+    xq, wq = (torch.zeros(tio.tio_fp8_bytes(r, K), device="cuda", dtype=torch.uint8) for r in (S, N))
+    work = torch.zeros(tio.tio_op_gemm_fp8_work(S, N, K) + 16, device="cuda", dtype=torch.uint8)
+
+    def calls():
+        s = torch.cuda.current_stream().cuda_stream
+        tio.tio_op_fp8_store(s, "bf16", "e4m3", False, S, K, x.data_ptr(), x.stride(0), xq.data_ptr())
+        tio.tio_op_fp8_store(s, "bf16", "e4m3", True, N, K, w.data_ptr(), w.stride(0), wq.data_ptr())
+        tio.tio_op_gemm_fp8(s, "bf16", S, N, K, "e4m3", xq.data_ptr(), "e4m3", wq.data_ptr(), y.data_ptr(), y.stride(0), work_ptr=work.data_ptr())
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        calls()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for i in range(4):
+        x[:, :K], w[:, :K] = torch.randn(S, K, device="cuda") * 3 ** i, torch.randn(N, K, device="cuda")
+        graph.replay()
+        torch.cuda.synchronize()
+        got = y.clone()
+        y.zero_()
+        calls()
+        torch.cuda.synchronize()
+        assert torch.equal(got, y) and y.abs().sum() > 0

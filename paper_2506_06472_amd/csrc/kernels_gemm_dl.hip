@@ -66,7 +66,6 @@ __device__ __forceinline__ void mfma_acc_load(floatx4 &c, const bf16x8 &a, const
                  : "memory", "m0");
 }
 #pragma clang diagnostic pop
-__device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
 
 template <int ROWS, int NT, bool KM> struct DlOperand;
 
@@ -159,36 +158,6 @@ template <int ROWS, int NT> struct DlOperand<ROWS, NT, true> {
     }
     static __device__ __forceinline__ void clear_tail(unsigned char *, int, int) {}       // whole k-rows: masked on their way in
 };
-
-// Workgroup -> output tile and contraction range; each XCD's L2 sees one contiguous part of the tile sequence (and, where the
-// number of ranges allows it, one range).  false: a padding workgroup.
-__device__ __forceinline__ bool place(int tiles_m, int tiles_n, int xsplits, int &split, int &nsplit, int &tm, int &tn) {
-    const int total_tiles = tiles_m * tiles_n;
-    int bid;
-    if (xsplits) {
-        const int x = (int)(blockIdx.x % 8), i = (int)(blockIdx.x / 8);
-        const int parts = 8 / xsplits, chunk = (total_tiles + parts - 1) / parts;
-        nsplit = xsplits;
-        split = x % xsplits;
-        if (i >= chunk) return false;
-        bid = (x / xsplits) * chunk + i;
-    } else {
-        nsplit = (int)gridDim.y;
-        split = (int)blockIdx.y;
-        bid = (int)(blockIdx.x % 8) * ((total_tiles + 7) / 8) + (int)(blockIdx.x / 8);
-    }
-    if (bid >= total_tiles) return false;
-    // consecutive workgroups walk down GROUP tile rows before moving to the next tile column; products with very many tile
-    // rows (weight gradients of the wide layers) do better with the narrower band (measured: +3..5 % there, -2 % elsewhere)
-    const int GROUP = tiles_m > 64 ? 4 : 8;
-    const int per_group = GROUP * tiles_n;
-    const int g = bid / per_group;
-    const int gm0 = g * GROUP;
-    const int gsz = tiles_m - gm0 < GROUP ? tiles_m - gm0 : GROUP;
-    tm = gm0 + (bid % per_group) % gsz;
-    tn = (bid % per_group) / gsz;
-    return true;
-}
 
 // Row sums of A as products with a vector of ones: rs[u] belongs to the 16-row group 2u + wn of the wavefront (the two
 // wavefronts that share A's rows take every other group), lane l holds the sum of its row l%16.

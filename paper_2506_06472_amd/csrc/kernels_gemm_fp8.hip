@@ -1,5 +1,7 @@
 // Products of matrices stored in 8-bit floating point with a power of two for each block of 128 (fp8_blocks.h):
 // C[M,N] = A[M,K] . B[N,K]^T (+ bias[N]) (+ resid[M,N]).
+#include <algorithm>
+#include <cmath>
 #include <type_traits>
 #include <utility>
 
@@ -8,6 +10,7 @@
 #include "fp8_blocks.h"
 #include "kernels.h"
 #include "mfma_tiles.h"
+#include "rows8.h"
 
 namespace tio {
 namespace k {
@@ -105,6 +108,98 @@ __global__ void __launch_bounds__(256) gemm_fp8_direct_k(const uint8_t *__restri
         }
 }
 
+// Eight neighbours of a row of results on their way out: bias and residual added in 32 bits, zeros behind the last column, rounded once.
+template <typename T> struct Out8 {
+    float add[8];
+    int left;                                                  // columns that are there
+    __device__ __forceinline__ Out8(const T *bias, int64_t col, int64_t N) : left(N - col < 0 ? 0 : N - col < 8 ? (int)(N - col) : 8) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) add[e] = bias && e < left ? to_f32(bias[col + e]) : 0.f;
+    }
+    __device__ __forceinline__ void put(float (&v)[8], const T *resid, T *to) const {
+        if (resid) {
+            Row8<T> r;
+            r.load(resid);
+            float f[8];
+            r.get(f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += f[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += add[e];
+        cut8(v, left);
+        Row8<T> r;
+        r.set(v);
+        r.store(to);
+    }
+};
+// The sums of a cut contraction: [range][M][N rounded up to 8] in 32 bits.
+__device__ __forceinline__ void put_partial(float *ws, int split, int64_t M, int64_t N, int64_t row, int64_t col, const float (&v)[8]) {
+    float *const to = ws + ((int64_t)split * M + row) * ((N + 7) / 8 * 8) + col;
+    *reinterpret_cast<float4 *>(to) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<float4 *>(to + 4) = make_float4(v[4], v[5], v[6], v[7]);
+}
+// added in the ranges' order
+template <typename T>
+__global__ void __launch_bounds__(256) gemm_fp8_sums_k(const float *__restrict__ ws, int nsplit, const T *__restrict__ bias, const T *resid, int64_t ldr, T *C,
+                                                       int64_t ldc, int64_t M, int64_t N) {
+    const int64_t per = (N + 7) / 8, idx = (int64_t)blockIdx.x * 256 + threadIdx.x, row = idx / per, col = (idx - row * per) * 8;
+    if (row >= M) return;
+    const float *from = ws + idx * 8;
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = 0; i < nsplit; ++i, from += M * per * 8) {
+        const float4 a = *reinterpret_cast<const float4 *>(from), b = *reinterpret_cast<const float4 *>(from + 4);
+        v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+    }
+    Out8<T>(bias, col, N).put(v, resid ? resid + row * ldr + col : nullptr, C + row * ldc + col);
+}
+
+// A wavefront's 16 TM x 16 TN results, from row mw and column nw on.  Rows of 16 x 32: the two halves of register pairs trade places so that a lane has
+// eight neighbours of a row.  The common case, whole parts without bias and residual, has no tests in it: with them between the stores 8192 x 11008 x
+// 4096 took 335 us instead of 288.
+template <typename T, int TM, int TN>
+__device__ __forceinline__ void store_part(const floatx4 (&acc)[TM][TN], int lane, int64_t mw, int64_t nw, int64_t M, int64_t N, const T *__restrict__ bias,
+                                           const T *resid, int64_t ldr, T *C, int64_t ldc, float *ws, int split, int nsplit) {
+    const int64_t row0 = mw + (lane & 15), col0 = nw + (lane >> 4 & 1) * 16 + (lane >> 5) * 8;
+    auto eight = [&](int i, int j, float (&v)[8]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[i][j][e]), __float_as_uint(acc[i][j + 1][e]), false, false);
+            v[e] = __uint_as_float(t[0]);
+            v[4 + e] = __uint_as_float(t[1]);
+        }
+    };
+    if (nsplit == 1 && !bias && !resid && mw + 16 * TM <= M && nw + 16 * TN <= N) {
+        T *const to = C + row0 * ldc + col0;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; j += 2) {
+                float v[8];
+                eight(i, j, v);
+                Row8<T> r;
+                r.set(v);
+                r.store(to + i * 16 * ldc + j * 16);
+            }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < TN; j += 2) {
+        const int64_t col = col0 + j * 16;
+        const Out8<T> out(bias, col, N);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            float v[8];
+            eight(i, j, v);
+            const int64_t row = row0 + i * 16;
+            if (row >= M || col >= N) continue;                // after the exchange, in which all lanes take part
+            if (nsplit > 1) put_partial(ws, split, M, N, row, col, v);
+            else out.put(v, resid ? resid + row * ldr + col : nullptr, C + row * ldc + col);
+        }
+    }
+}
+
 // ---- large products in bf16
 // c += b's rows . a's rows over a block of 128, the accumulator held in an accumulation register (left to itself the compiler moves accumulators between
 // the register files around the products); SB, SA: which byte of the lane's exponent words.
@@ -133,56 +228,84 @@ __device__ __forceinline__ void load_to_lds_b32(const uint8_t *from, uint32_t ld
 }
 #pragma clang diagnostic pop
 
+// The loads of a tile of 32 TM x 32 TN results by four wavefronts: both operands' fragments from memory straight into LDS, D steps (blocks of 128 of the
+// contraction) deep, and the exponents of each wavefront's rows and columns, a 4-byte load to LDS a step (lanes 0 .. 31 A's, the others B's).
+template <int TM, int TN, int D> struct Loads {
+    static constexpr int BM = 32 * TM, BN = 32 * TN, TILE_A = BM * 128, TILE_B = BN * 128;
+    static constexpr int WA = TM / 4, WB = TN / 4;             // words of exponents a lane has (64 rows each)
+    static constexpr uint32_t EXPS = D * (TILE_A + TILE_B), LDS = EXPS + 4 * D * 256;
+    static constexpr int PER = TM + TN + 1;                    // loads of a wavefront for a step
+    i32x4 rsA, rsB;
+    // 1 KiB pieces of a step: half h of group g is piece 2 g + h, and wavefront p % 4's; groups past the last one repeat it
+    uint32_t soA[TM], soB[TN], lds0, ahead, voff;              // ahead: the step whose loads are next (the last one again when there is none); voff: its codes
+    const uint8_t *exps;
+    int wave, lane, nk;
+    __device__ __forceinline__ Loads(const uint8_t *A, const uint8_t *B, int64_t M, int64_t N, int64_t K, int tm, int tn, int kb0, int steps, int w, int l,
+                                     const unsigned char *smem)
+        : ahead(0), voff(l * 16), wave(w), lane(l), nk(steps) {
+        const Fp8Shape sa{M, K}, sb{N, K};
+        const int64_t KB = sa.kb(), ga0 = (int64_t)tm * (2 * TM), gb0 = (int64_t)tn * (2 * TN);
+        const int64_t atA = (ga0 * KB + kb0) * F8_FRAG, atB = (gb0 * KB + kb0) * F8_FRAG, roomA = sa.code_bytes() - atA, roomB = sb.code_bytes() - atB;
+        rsA = make_rsrc(A + atA, roomA < 0xfffffff0 ? (uint32_t)roomA : 0xfffffff0u);
+        rsB = make_rsrc(B + atB, roomB < 0xfffffff0 ? (uint32_t)roomB : 0xfffffff0u);
+        const int lastA = (int)(sa.groups() - 1 - ga0), lastB = (int)(sb.groups() - 1 - gb0);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int p = i * 4 + wave, g = p >> 1;
+            soA[i] = __builtin_amdgcn_readfirstlane((uint32_t)((g < lastA ? g : lastA) * (int)KB * F8_FRAG + (p & 1) * 1024));
+        }
+#pragma unroll
+        for (int i = 0; i < TN; ++i) {
+            const int p = i * 4 + wave, g = p >> 1;
+            soB[i] = __builtin_amdgcn_readfirstlane((uint32_t)((g < lastB ? g : lastB) * (int)KB * F8_FRAG + (p & 1) * 1024));
+        }
+        const bool isB = lane >= 32;
+        const int64_t most = isB ? (N - 1) / 64 : (M - 1) / 64,
+                      g = (isB ? (int64_t)tn * (2 * WB) + (wave & 1) * WB : (int64_t)tm * (2 * WA) + (wave >> 1) * WA) + (lane >> 4 & 1);
+        exps = (isB ? B + sb.code_bytes() : A + sa.code_bytes()) + ((g < most ? g : most) * KB + kb0) * 64 + (lane & 15) * 4;
+        lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem));
+    }
+    // where piece i of a step goes, in part S of LDS
+    __device__ __forceinline__ uint32_t to_a(int S, int i) const { return lds0 + S * TILE_A + (i * 4 + wave) * 1024; }
+    __device__ __forceinline__ uint32_t to_b(int S, int i) const { return lds0 + D * TILE_A + S * TILE_B + (i * 4 + wave) * 1024; }
+    __device__ __forceinline__ void load_exps(int S) const { load_to_lds_b32(exps + ahead * 64, lds0 + EXPS + (wave * D + S) * 256); }
+    __device__ __forceinline__ void go_on() {
+        ahead = ahead + 1 < (uint32_t)nk ? ahead + 1 : (uint32_t)nk - 1;
+        voff = lane * 16 + ahead * F8_FRAG;
+    }
+    __device__ __forceinline__ void load_step(int S) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) load_to_lds_b128(rsA, to_a(S, i), voff, soA[i]);
+#pragma unroll
+        for (int i = 0; i < TN; ++i) load_to_lds_b128(rsB, to_b(S, i), voff, soB[i]);
+        load_exps(S);
+        go_on();
+    }
+};
+
 // f of each number as a constant
 template <typename F, int... I> __device__ __forceinline__ void each(const F &f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
 
 // A tile of 32 TM x 32 TN results: four wavefronts, 16 TM x 16 TN each.  A step of the contraction is one block of 128: TM TN products of 32 clocks.
-//  * Both operands' fragments go from memory straight into LDS, two steps deep; they are stored as the products take them, so that LDS is written and
-//    read in consecutive KiB.  The exponents of a wavefront's rows and columns are one 4-byte load to LDS a step (lanes 0 .. 31 A's, the others B's).
+//  * Fragments are stored as the products take them, so that LDS is written and read in consecutive KiB.
 //  * While the products of a step run, all fragments of the next one are read into registers: B's into a second set, A's into the registers of the row
 //    group whose products are done, but for the last two groups, which have a second set too.  So a step's LDS is free when its products begin, and
-//    the loads for the step after the next go there in their first half; they have the other half, at least, to land.
+//    the loads for the step D later go there in their first half; with D = 2 they have the other half, at least, to land.
 //  * One wavefront per SIMD (256 x 256) hides nothing by switching, so the order of all of it is pinned.
-template <int FA, int FB, int TM, int TN>
-__global__ void __launch_bounds__(256, TM == 8 ? 1 : 2)
-    gemm_fp8_tile_k(const uint8_t *__restrict__ A, const uint8_t *__restrict__ B, const uint16_t *__restrict__ bias, const uint16_t *resid, int64_t ldr, uint16_t *C,
-                    int64_t ldc, int64_t M, int64_t N, int64_t K, int tiles_m, int tiles_n) {
-    constexpr int BM = 32 * TM, BN = 32 * TN, TILE_A = BM * 128, TILE_B = BN * 128, NQ = TM * TN, NR = TM + TN, NL = TM + TN;
-    constexpr uint32_t EXPS = 2 * (TILE_A + TILE_B);
+template <int FA, int FB, int TM, int TN, int D>
+__global__ void __launch_bounds__(256)
+    gemm_fp8_tile_k(const uint8_t *__restrict__ A, const uint8_t *__restrict__ B, const bf16_t *__restrict__ bias, const bf16_t *resid, int64_t ldr, bf16_t *C, int64_t ldc,
+                    int64_t M, int64_t N, int64_t K, int tiles_m, int tiles_n, float *__restrict__ ws) {
+    using L = Loads<TM, TN, D>;
+    constexpr int BM = L::BM, BN = L::BN, TILE_A = L::TILE_A, TILE_B = L::TILE_B, NQ = TM * TN, NR = TM + TN, NL = TM + TN, WA = L::WA, WB = L::WB;
+    constexpr uint32_t EXPS = L::EXPS;
+    static_assert(D % 2 == 0, "a step's registers go by its parity");
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem8[];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, wm = wave >> 1, wn = wave & 1;
     int split, nsplit, tm, tn;
     if (!place(tiles_m, tiles_n, 0, split, nsplit, tm, tn)) return;
-    const Fp8Shape sa{M, K}, sb{N, K};
-    const int64_t KB = sa.kb(), ga0 = (int64_t)tm * (2 * TM), gb0 = (int64_t)tn * (2 * TN);
-    const int nk = (int)KB;
-
-    // 1 KiB pieces of a step: half h of group g is piece 2 g + h, and wavefront p % 4's; groups past the last one repeat it
-    const uint8_t *const baseA = A + ga0 * KB * F8_FRAG, *const baseB = B + gb0 * KB * F8_FRAG;
-    const int64_t roomA = sa.code_bytes() - ga0 * KB * F8_FRAG, roomB = sb.code_bytes() - gb0 * KB * F8_FRAG;
-    i32x4 rsA = make_rsrc(baseA, roomA < 0xfffffff0 ? (uint32_t)roomA : 0xfffffff0u), rsB = make_rsrc(baseB, roomB < 0xfffffff0 ? (uint32_t)roomB : 0xfffffff0u);
-    const int lastA = (int)(sa.groups() - 1 - ga0), lastB = (int)(sb.groups() - 1 - gb0);
-    uint32_t soA[TM], soB[TN];
-#pragma unroll
-    for (int l = 0; l < TM; ++l) {
-        const int p = l * 4 + wave, g = p >> 1;
-        soA[l] = __builtin_amdgcn_readfirstlane((uint32_t)((g < lastA ? g : lastA) * (int)KB * F8_FRAG + (p & 1) * 1024));
-    }
-#pragma unroll
-    for (int l = 0; l < TN; ++l) {
-        const int p = l * 4 + wave, g = p >> 1;
-        soB[l] = __builtin_amdgcn_readfirstlane((uint32_t)((g < lastB ? g : lastB) * (int)KB * F8_FRAG + (p & 1) * 1024));
-    }
-    // lanes' exponents: words of 64 rows; TM, TN = 4: one of A's and one of B's, 8: two
-    constexpr int WA = TM / 4, WB = TN / 4;
-    const uint8_t *exps;
-    {
-        const bool isB = lane >= 32;
-        const int64_t most = isB ? (N - 1) / 64 : (M - 1) / 64, g = (isB ? (int64_t)tn * (2 * WB) + wn * WB : (int64_t)tm * (2 * WA) + wm * WA) + (lane >> 4 & 1);
-        exps = (isB ? B + sb.code_bytes() : A + sa.code_bytes()) + (g < most ? g : most) * KB * 64 + (lane & 15) * 4;
-    }
-    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem8));
-    uint32_t ahead = 0, voff = lane * 16;                      // the step whose loads are next (the last one again when there is none), and where its codes are
+    const int KB = (int)Fp8Shape{M, K}.kb(), kb0 = (int)((int64_t)KB * split / nsplit), nk = (int)((int64_t)KB * (split + 1) / nsplit) - kb0;
+    L in(A, B, M, N, K, tm, tn, kb0, nk, wave, lane, smem8);
 
     floatx4 acc[TM][TN];
 #pragma unroll
@@ -190,60 +313,45 @@ __global__ void __launch_bounds__(256, TM == 8 ? 1 : 2)
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = (floatx4){0.f, 0.f, 0.f, 0.f};
 
-    // where piece l of a step goes, in half S of LDS
-    auto to_a = [&](auto S, int l) __attribute__((always_inline)) { return lds0 + S() * TILE_A + (l * 4 + wave) * 1024; };
-    auto to_b = [&](auto S, int l) __attribute__((always_inline)) { return lds0 + 2 * TILE_A + S() * TILE_B + (l * 4 + wave) * 1024; };
-    auto load_exps = [&](auto S) __attribute__((always_inline)) {
-        load_to_lds_b32(exps + ahead * 64, lds0 + EXPS + wave * 512 + S() * 256);
-    };
-    auto go_on = [&]() __attribute__((always_inline)) {
-        ahead = ahead + 1 < (uint32_t)nk ? ahead + 1 : (uint32_t)nk - 1;
-        voff = lane * 16 + ahead * F8_FRAG;
-    };
-    auto load_step = [&](auto S) __attribute__((always_inline)) {
-#pragma unroll
-        for (int l = 0; l < TM; ++l) load_to_lds_b128(rsA, to_a(S, l), voff, soA[l]);
-#pragma unroll
-        for (int l = 0; l < TN; ++l) load_to_lds_b128(rsB, to_b(S, l), voff, soB[l]);
-        load_exps(S);
-        go_on();
-    };
     i32x8 fa[TM], fa2[2], fb[2][TN];                           // fa2: of the last two row groups in odd steps
     uint32_t ea[2][WA], eb[2][WB];
     auto read_frag = [&](uint32_t at) __attribute__((always_inline)) {
         const uint4 u = *reinterpret_cast<const uint4 *>(smem8 + at + lane * 16), v = *reinterpret_cast<const uint4 *>(smem8 + at + 1024 + lane * 16);
         return (i32x8){(int)u.x, (int)u.y, (int)u.z, (int)u.w, (int)v.x, (int)v.y, (int)v.z, (int)v.w};
     };
+    // S: the step modulo D, whose part of LDS it is in; its parity says which registers
     auto read_a = [&](auto S, auto I) __attribute__((always_inline)) {
         const i32x8 f = read_frag(S() * TILE_A + (wm * TM + I()) * F8_FRAG);
-        if constexpr (S() == 1 && I() >= TM - 2) fa2[I() - (TM - 2)] = f;
+        if constexpr (S() % 2 == 1 && I() >= TM - 2) fa2[I() - (TM - 2)] = f;
         else fa[I()] = f;
     };
-    auto read_b = [&](auto S, int j) __attribute__((always_inline)) { fb[S()][j] = read_frag(2 * TILE_A + S() * TILE_B + (wn * TN + j) * F8_FRAG); };
+    auto read_b = [&](auto S, int j) __attribute__((always_inline)) { fb[S() % 2][j] = read_frag(D * TILE_A + S() * TILE_B + (wn * TN + j) * F8_FRAG); };
     auto read_exps = [&](auto S) __attribute__((always_inline)) {
-        const unsigned char *const at = smem8 + EXPS + wave * 512 + S() * 256 + (lane & 15) * 4;
+        const unsigned char *const at = smem8 + EXPS + (wave * D + S()) * 256 + (lane & 15) * 4;
 #pragma unroll
-        for (int w = 0; w < WA; ++w) ea[S()][w] = *reinterpret_cast<const uint32_t *>(at + w * 64);
+        for (int w = 0; w < WA; ++w) ea[S() % 2][w] = *reinterpret_cast<const uint32_t *>(at + w * 64);
 #pragma unroll
-        for (int w = 0; w < WB; ++w) eb[S()][w] = *reinterpret_cast<const uint32_t *>(at + 128 + w * 64);
+        for (int w = 0; w < WB; ++w) eb[S() % 2][w] = *reinterpret_cast<const uint32_t *>(at + 128 + w * 64);
     };
     constexpr std::integral_constant<int, 0> c0{};
-    constexpr std::integral_constant<int, 1> c1{};
+    constexpr auto wait_vm = [](int n) { return 0x0070 | (n & 15) | ((n >> 4) << 14); };      // s_waitcnt vmcnt(n) lgkmcnt(0)
+    static_assert((D - 1) * L::PER < 64, "loads in flight fit the counter");
 
     // The products of a step from the registers of parity S.  Reads of the next step (read p at product RSTEP p / 8): B's groups in turn with A's last
-    // two, then A's from the first on, each after its row group's products.  Loads two steps ahead at every NQ / 2 / NL-th product.
+    // two, then A's from the first on, each after its row group's products.  Loads D steps ahead at every NQ / 2 / NL-th product.
     constexpr int RSTEP = NQ * 13 / (NR * 2);                  // in eighths of a product: 0.8 of the step
     auto step = [&](auto S) __attribute__((always_inline)) {
-        constexpr std::integral_constant<int, (S() ^ 1)> next{};
-        load_exps(S);
+        constexpr std::integral_constant<int, (S() + 1) % D> next{};
+        constexpr int P = S() % 2;
+        in.load_exps(S());
         read_exps(next);
         auto product = [&](auto Q) __attribute__((always_inline)) {
             constexpr int q = decltype(Q)::value, i = q / TN, j = i % 2 ? TN - 1 - q % TN : q % TN, l = q * 2 * NL / NQ;
             constexpr bool loads = l < NL && q % (NQ / (2 * NL)) == 0;
-            const i32x8 &a = S() == 1 && i >= TM - 2 ? fa2[i >= TM - 2 ? i - (TM - 2) : 0] : fa[i];
-            if constexpr (loads && l < TM) mfma8_load<FA, FB, i % 4, j % 4>(acc[i][j], fb[S()][j], a, eb[S()][j / 4], ea[S()][i / 4], rsA, to_a(S, l), voff, soA[l]);
-            else if constexpr (loads) mfma8_load<FA, FB, i % 4, j % 4>(acc[i][j], fb[S()][j], a, eb[S()][j / 4], ea[S()][i / 4], rsB, to_b(S, l - TM), voff, soB[l - TM]);
-            else mfma8<FA, FB, i % 4, j % 4>(acc[i][j], fb[S()][j], a, eb[S()][j / 4], ea[S()][i / 4]);
+            const i32x8 &a = P == 1 && i >= TM - 2 ? fa2[i >= TM - 2 ? i - (TM - 2) : 0] : fa[i];
+            if constexpr (loads && l < TM) mfma8_load<FA, FB, i % 4, j % 4>(acc[i][j], fb[P][j], a, eb[P][j / 4], ea[P][i / 4], in.rsA, in.to_a(S(), l), in.voff, in.soA[l]);
+            else if constexpr (loads) mfma8_load<FA, FB, i % 4, j % 4>(acc[i][j], fb[P][j], a, eb[P][j / 4], ea[P][i / 4], in.rsB, in.to_b(S(), l - TM), in.voff, in.soB[l - TM]);
+            else mfma8<FA, FB, i % 4, j % 4>(acc[i][j], fb[P][j], a, eb[P][j / 4], ea[P][i / 4]);
             constexpr int p = (q * 8 + RSTEP - 1) / RSTEP;       // the read whose turn it is
             if constexpr (p < NR && p * RSTEP / 8 == q) {
                 if constexpr (p % 2 == 0) read_b(next, p / 2);
@@ -256,16 +364,17 @@ __global__ void __launch_bounds__(256, TM == 8 ? 1 : 2)
             __builtin_amdgcn_sched_barrier(0);
         };
         each(product, std::make_integer_sequence<int, NQ>{});
-        go_on();
-        __builtin_amdgcn_s_waitcnt(0x0070);                    // vmcnt(0) lgkmcnt(0): the step after the next has landed, the next one is in registers
+        in.go_on();
+        __builtin_amdgcn_s_waitcnt(wait_vm((D - 2) * L::PER));  // the step after the next has landed, the next one is in registers
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
     };
 
-    load_step(c0);
-    if (nk > 1) load_step(c1);
-    __builtin_amdgcn_s_waitcnt(0x0070);
+#pragma unroll
+    for (int t = 0; t < D; ++t) in.load_step(t);
+    __builtin_amdgcn_s_waitcnt(wait_vm((D - 2) * L::PER));
     __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
     each([&](auto I) __attribute__((always_inline)) { read_a(c0, I); }, std::make_integer_sequence<int, TM>{});
 #pragma unroll
     for (int j = 0; j < TN; ++j) read_b(c0, j);
@@ -278,89 +387,152 @@ __global__ void __launch_bounds__(256, TM == 8 ? 1 : 2)
     };
     pin();
     settle();
-    __builtin_amdgcn_s_waitcnt(0x0070);
+    __builtin_amdgcn_s_waitcnt(wait_vm((D - 2) * L::PER));
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
     // One loop for all steps; behind the contraction's end the descriptors are empty, so that nothing is fetched
-    auto end = [&](int kt) __attribute__((always_inline)) {
-        if (kt + 2 >= nk) rsA[2] = rsB[2] = 0;
+    int kt = 0;
+    auto done = [&](auto S) __attribute__((always_inline)) {
+        if (kt + D >= nk) in.rsA[2] = in.rsB[2] = 0;
+        step(S);
+        return ++kt >= nk;
     };
-    for (int kt = 0;; kt += 2) {
-        end(kt);
-        step(c0);
-        if (kt + 1 >= nk) break;
-        end(kt + 1);
-        step(c1);
-        if (kt + 2 >= nk) break;
+    if constexpr (D == 2) {
+        while (!done(c0) && !done(std::integral_constant<int, 1>{})) {}
+    } else {
+        static_assert(D == 4, "steps of the loop");
+        while (!done(c0) && !done(std::integral_constant<int, 1>{}) && !done(std::integral_constant<int, 2>{}) && !done(std::integral_constant<int, 3>{})) {}
     }
+    __builtin_amdgcn_s_waitcnt(wait_vm(0));                    // LDS is the next workgroup's
     settle();
     pin();
 
-    // Rows of 16 x 32 results: the two halves of a wavefront's register pairs trade places so that a lane has eight neighbours of a row.
-    const int64_t row0 = (int64_t)tm * BM + wm * 16 * TM + (lane & 15), col0 = (int64_t)tn * BN + wn * 16 * TN + (lane >> 4 & 1) * 16 + (lane >> 5) * 8;
-#pragma unroll
-    for (int j = 0; j < TN; j += 2) {
-        const int64_t col = col0 + j * 16;
-        const int left = N - col < 0 ? 0 : N - col < 8 ? (int)(N - col) : 8;
-        float add[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) add[e] = bias && e < left ? bf16_bits_to_f32(bias[col + e]) : 0.f;
-#pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[i][j][e]), __float_as_uint(acc[i][j + 1][e]), false, false);
-                v[e] = __uint_as_float(t[0]);
-                v[4 + e] = __uint_as_float(t[1]);
-            }
-            const int64_t row = row0 + i * 16;
-            if (row >= M || col >= N) continue;                // after the exchange, in which all lanes take part
-            if (bias) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] += add[e];
-            }
-            if (resid) {
-                const uint4 r = *reinterpret_cast<const uint4 *>(resid + row * ldr + col);
-                const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] += __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
-            }
-            if (left < 8) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = e < left ? v[e] : 0.f;
-            }
-            *reinterpret_cast<uint4 *>(C + row * ldc + col) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
-        }
-    }
+    store_part<bf16_t, TM, TN>(acc, lane, (int64_t)tm * BM + wm * 16 * TM, (int64_t)tn * BN + wn * 16 * TN, M, N, bias, resid, ldr, C, ldc, ws, split, nsplit);
 }
 
-template <int FA, int FB, int TM, int TN> void launch_tile(hipStream_t s, const Fp8Product &p) {
-    constexpr int BM = 32 * TM, BN = 32 * TN, LDS = 2 * (BM + BN) * 128 + 4 * 512;
-    static const hipError_t set = hipFuncSetAttribute((const void *)gemm_fp8_tile_k<FA, FB, TM, TN>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-    (void)set;
-    const int64_t tiles_m = (p.M + BM - 1) / BM, tiles_n = (p.N + BN - 1) / BN;
-    gemm_fp8_tile_k<FA, FB, TM, TN><<<(unsigned)((tiles_m * tiles_n + 7) / 8 * 8), 256, LDS, s>>>(
-        (const uint8_t *)p.A, (const uint8_t *)p.B, (const uint16_t *)p.bias, (const uint16_t *)p.resid, p.ldr, (uint16_t *)p.C, p.ldc, p.M, p.N, p.K, (int)tiles_m,
-        (int)tiles_n);
+// ---- in fp32: the values, which bf16 holds exactly, in 16-bit products, whose sums are those of 32-bit arithmetic.  A quarter to half of the 8-bit products' rate.
+// 128 x 128 results; two workgroups to a compute unit cover each other's conversions and loads.
+template <int FA, int FB>
+__global__ void __launch_bounds__(256, 2)
+    gemm_fp8_tile32_k(const uint8_t *__restrict__ A, const uint8_t *__restrict__ B, const float *__restrict__ bias, const float *resid, int64_t ldr, float *C, int64_t ldc,
+                      int64_t M, int64_t N, int64_t K, int tiles_m, int tiles_n, float *__restrict__ ws) {
+    constexpr int TM = 4, TN = 4;
+    using L = Loads<TM, TN, 2>;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem8[];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, wm = wave >> 1, wn = wave & 1;
+    int split, nsplit, tm, tn;
+    if (!place(tiles_m, tiles_n, 0, split, nsplit, tm, tn)) return;
+    const int KB = (int)Fp8Shape{M, K}.kb(), kb0 = (int)((int64_t)KB * split / nsplit), nk = (int)((int64_t)KB * (split + 1) / nsplit) - kb0;
+    L in(A, B, M, N, K, tm, tn, kb0, nk, wave, lane, smem8);
+    floatx4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = (floatx4){0.f, 0.f, 0.f, 0.f};
+    auto piece = [&](uint32_t at, uint32_t word, int byte) __attribute__((always_inline)) {
+        Piece8 p;
+        p.h[0] = *reinterpret_cast<const uint4 *>(smem8 + at + lane * 16);
+        p.h[1] = *reinterpret_cast<const uint4 *>(smem8 + at + 1024 + lane * 16);
+        p.e = word >> (8 * byte) & 255u;
+        return p;
+    };
+    in.load_step(0);
+    for (int kt = 0; kt < nk; ++kt) {
+        const int S = kt & 1;
+        __builtin_amdgcn_s_waitcnt(0x0070);                    // this step has landed, and the one before is in registers
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (kt + 1 < nk) in.load_step(S ^ 1);
+        const unsigned char *const e = smem8 + L::EXPS + (wave * 2 + S) * 256 + (lane & 15) * 4;
+        const uint32_t ea = *reinterpret_cast<const uint32_t *>(e), eb = *reinterpret_cast<const uint32_t *>(e + 128);
+        bf16x8 b[TN][4];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const Piece8 p = piece(2 * L::TILE_A + S * L::TILE_B + (wn * TN + j) * F8_FRAG, eb, j);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) b[j][q] = p.template values<FB>(q);
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const Piece8 p = piece(S * L::TILE_A + (wm * TM + i) * F8_FRAG, ea, i);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const bf16x8 a = p.template values<FA>(q);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j][q], a, acc[i][j], 0, 0, 0);
+            }
+        }
+    }
+    store_part<float, TM, TN>(acc, lane, (int64_t)tm * L::BM + wm * 16 * TM, (int64_t)tn * L::BN + wn * 16 * TN, M, N, bias, resid, ldr, C, ldc, ws, split, nsplit);
+}
+
+// How a product is taken: tiles of 128 or 256 (0: few rows, gemm_fp8_direct_k), how many steps deep, and the ranges its contraction is cut into.
+//
+// The least of an estimate of the time, whose constants were fitted to 14 products, each taken in all ways: a workgroup's steps and its beginning and end
+// (us), times the rounds of workgroups, and the sums of the ranges.  A step of a 128 tile is mostly waiting for loads where a compute unit has one such tile:
+// four steps deep it takes 0.37 us (0.5 where all units work), two deep 0.6, but two tiles to a unit share 0.88.  us, 768 x 768 x 8192 in one range: 26.9 four
+// deep, 41.4 two deep, 69.8 in 256 tiles, and 19.1 in three ranges; 8192 x 768 x 768: 13.3, 10.8, 15.5; 8192 x 11008 x 4096: 377, 328, 285.
+struct Route {
+    int tile, deep, splits;
+};
+Route route(bool bf16, int64_t M, int64_t N, int64_t K) {
+    if (M <= 16) return {0, 0, 1};
+    constexpr double UNITS = 256;                              // compute units
+    const int64_t KB = (K + F8_BLOCK - 1) / F8_BLOCK;
+    Route best{};
+    double least = 1e300;
+    auto consider = [&](int tile, int deep, int most, int per_unit, double step, double busy, double ends) {
+        for (int splits = 1; splits <= most && splits <= KB; ++splits) {
+            const double groups = (double)((M + tile - 1) / tile) * ((N + tile - 1) / tile) * splits, full = std::min(1.0, groups / UNITS);
+            if (per_unit > 1 && groups <= UNITS) continue;
+            double t = std::ceil(groups / (UNITS * per_unit)) * ((KB + splits - 1) / splits * (step + busy * full) + ends);
+            if (splits > 1) t += 3.0 + (double)M * N * 8 * (splits + 0.5) / 3.5e6;
+            if (t < least) least = t, best = {tile, deep, splits};
+        }
+    };
+    if (bf16) {
+        consider(256, 2, 16, 1, 1.06, 0.28, 5.0);
+        consider(128, 2, 16, 2, 0.88, 0.0, 4.0);
+        consider(128, 4, 32, 1, 0.37, 0.13, 3.5);
+    } else {
+        consider(128, 2, 16, 2, 1.8, 0.0, 4.0);
+        consider(128, 2, 32, 1, 1.05, 0.0, 3.0);
+    }
+    return best;
 }
 
 template <int FA, int FB, typename T> void launch(hipStream_t s, const Fp8Product &p) {
-#define TIO_DIRECT(TM, TN)                                                                                                                              \
-    do {                                                                                                                                                \
-        const int64_t tiles_m = (p.M + 16 * TM - 1) / (16 * TM), tiles_n = (p.N + 16 * TN - 1) / (16 * TN);                                             \
-        gemm_fp8_direct_k<FA, FB, T, TM, TN><<<(unsigned)(tiles_m * tiles_n), 256, 0, s>>>(                                                             \
-            (const uint8_t *)p.A, (const uint8_t *)p.B, (const T *)p.bias, (const T *)p.resid, p.ldr, (T *)p.C, p.ldc, p.M, p.N, p.K, (int)tiles_n); \
-    } while (0)
-    if (sizeof(T) == 2 && p.M > 256 && p.N > 256) return launch_tile<FA, FB, 8, 8>(s, p);
-    if (p.M <= 16) TIO_DIRECT(1, 1);
-    else TIO_DIRECT(2, 2);
-#undef TIO_DIRECT
+    const Route r = route(sizeof(T) == 2, p.M, p.N, p.K);
+    const T *const bias = (const T *)p.bias, *const resid = (const T *)p.resid;
+    const uint8_t *const A = (const uint8_t *)p.A, *const B = (const uint8_t *)p.B;
+    if (!r.tile) {
+        const int64_t tiles_n = (p.N + 15) / 16;
+        gemm_fp8_direct_k<FA, FB, T, 1, 1><<<(unsigned)tiles_n, 256, 0, s>>>(A, B, bias, resid, p.ldr, (T *)p.C, p.ldc, p.M, p.N, p.K, (int)tiles_n);
+        return;
+    }
+    const int tiles_m = (int)((p.M + r.tile - 1) / r.tile), tiles_n = (int)((p.N + r.tile - 1) / r.tile);
+    const dim3 grid((unsigned)(((int64_t)tiles_m * tiles_n + 7) / 8 * 8), (unsigned)r.splits);
+    // kernels with more LDS than a launch has without asking
+    auto go = [&](auto kernel, uint32_t lds) {
+        static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        (void)allowed;
+        kernel<<<grid, 256, lds, s>>>(A, B, bias, resid, p.ldr, (T *)p.C, p.ldc, p.M, p.N, p.K, tiles_m, tiles_n, (float *)p.work);
+    };
+    if constexpr (sizeof(T) == 2) {
+        if (r.tile == 256) go(gemm_fp8_tile_k<FA, FB, 8, 8, 2>, Loads<8, 8, 2>::LDS);
+        else if (r.deep == 4) go(gemm_fp8_tile_k<FA, FB, 4, 4, 4>, Loads<4, 4, 4>::LDS);
+        else go(gemm_fp8_tile_k<FA, FB, 4, 4, 2>, Loads<4, 4, 2>::LDS);
+    } else go(gemm_fp8_tile32_k<FA, FB>, Loads<4, 4, 2>::LDS);
+    if (r.splits > 1)
+        gemm_fp8_sums_k<T><<<(unsigned)((p.M * ((p.N + 7) / 8) + 255) / 256), 256, 0, s>>>((const float *)p.work, r.splits, bias, resid, p.ldr, (T *)p.C, p.ldc, p.M, p.N);
 }
 
 }  // namespace
 
-int64_t gemm_fp8_work(int64_t, int64_t, int64_t) { return 0; }
+int64_t gemm_fp8_work(int64_t M, int64_t N, int64_t K) {
+    const int a = route(true, M, N, K).splits, b = route(false, M, N, K).splits, most = a > b ? a : b;
+    return most > 1 ? most * M * ((N + 7) / 8 * 8) * 4 : 0;
+}
 
 void gemm_fp8(hipStream_t s, int dtype, const Fp8Product &p) {
 #define TIO_FORMS(T)                                                  \

@@ -125,7 +125,7 @@ def _bound(a, b, want, dtype, extra=0.0):
 
 
 PRODUCTS = [(1, 1, 1), (1, 40, 129), (2, 515, 352), (4, 1000, 256), (15, 16, 640), (16, 17, 128), (17, 33, 127), (33, 64, 1000), (64, 200, 384), (100, 64, 4200),
-            (128, 128, 256), (130, 257, 136), (256, 256, 512), (257, 300, 100), (512, 520, 1152)]
+            (128, 128, 256), (130, 257, 136), (256, 256, 512), (257, 300, 100), (512, 520, 1152), (20, 24, 20000), (300, 200, 5000)]
 
 
 @pytest.mark.parametrize("forms", [("e4m3", "e4m3"), ("e5m2", "e4m3"), ("e4m3", "e5m2"), ("e5m2", "e5m2")])

@@ -466,37 +466,50 @@ __global__ void __launch_bounds__(256, 2)
     store_part<float, TM, TN>(acc, lane, (int64_t)tm * L::BM + wm * 16 * TM, (int64_t)tn * L::BN + wn * 16 * TN, M, N, bias, resid, ldr, C, ldc, ws, split, nsplit);
 }
 
-// How a product is taken: tiles of 128 or 256 (0: few rows, gemm_fp8_direct_k), how many steps deep, and the ranges its contraction is cut into.
+// How a product is taken: tiles of 128 or 256 through LDS, `deep` steps at a time, the contraction cut into ranges, or tiles of 16 or 32 from the caches
+// (gemm_fp8_direct_k).
 //
-// The least of an estimate of the time, whose constants were fitted to 14 products, each taken in all ways: a workgroup's steps and its beginning and end
-// (us), times the rounds of workgroups, and the sums of the ranges.  A step of a 128 tile is mostly waiting for loads where a compute unit has one such tile:
-// four steps deep it takes 0.37 us (0.5 where all units work), two deep 0.6, but two tiles to a unit share 0.88.  us, 768 x 768 x 8192 in one range: 26.9 four
-// deep, 41.4 two deep, 69.8 in 256 tiles, and 19.1 in three ranges; 8192 x 768 x 768: 13.3, 10.8, 15.5; 8192 x 11008 x 4096: 377, 328, 285.
+// The least of an estimate of the time, whose constants were fitted to 39 products, each taken in all ways: a workgroup's steps and its beginning and end
+// (us), times the rounds of workgroups, and the sums of the ranges; of small tiles the chain of steps or the bytes from the caches.  A step of a 128 tile is
+// mostly waiting for loads where a compute unit has one such tile: 0.32 us four steps deep (0.44 where all units work), two deep 0.6, but two tiles to a
+// unit share 0.88.  us, 768 x 768 x 8192 in one range: 26.9 four deep, 41.4 two deep, 69.8 in 256 tiles, and 19.1 in three ranges; 8192 x 768 x 768: 13.3,
+// 10.8, 15.5; 8192 x 11008 x 4096: 377, 328, 285; 1000^3: 8.4 and 7.7, in tiles of 32 6.1; 500 x 500 x 3000: 11.9, 11.4 and 5.0.
 struct Route {
     int tile, deep, splits;
 };
 Route route(bool bf16, int64_t M, int64_t N, int64_t K) {
-    if (M <= 16) return {0, 0, 1};
+    if (M <= 16) return {16, 1, 1};
     constexpr double UNITS = 256;                              // compute units
     const int64_t KB = (K + F8_BLOCK - 1) / F8_BLOCK;
     Route best{};
     double least = 1e300;
-    auto consider = [&](int tile, int deep, int most, int per_unit, double step, double busy, double ends) {
+    auto tiles = [&](int tile) { return (double)((M + tile - 1) / tile) * ((N + tile - 1) / tile); };
+    auto take = [&](double t, Route r) {
+        if (t < least) least = t, best = r;
+    };
+    auto small = [&](int tile, double step, double per_us, double each) {
+        const double groups = tiles(tile), chain = step * (double)((KB + 3) / 4) * std::ceil(groups * tile / 32768);
+        take(2.0 + std::max(chain, groups * KB * tile * 256 / per_us + groups * each), {tile, 1, 1});
+    };
+    small(32, 0.36, 14e6, 0.0013);
+    small(16, 0.20, 16e6, 0.0001);
+    auto large = [&](int tile, int deep, int most, int per_unit, double step, double busy, double ends) {
         for (int splits = 1; splits <= most && splits <= KB; ++splits) {
-            const double groups = (double)((M + tile - 1) / tile) * ((N + tile - 1) / tile) * splits, full = std::min(1.0, groups / UNITS);
+            const double groups = tiles(tile) * splits, full = std::min(1.0, groups / UNITS);
             if (per_unit > 1 && groups <= UNITS) continue;
             double t = std::ceil(groups / (UNITS * per_unit)) * ((KB + splits - 1) / splits * (step + busy * full) + ends);
             if (splits > 1) t += 3.0 + (double)M * N * 8 * (splits + 0.5) / 3.5e6;
-            if (t < least) least = t, best = {tile, deep, splits};
+            take(t, {tile, deep, splits});
         }
     };
     if (bf16) {
-        consider(256, 2, 16, 1, 1.06, 0.28, 5.0);
-        consider(128, 2, 16, 2, 0.88, 0.0, 4.0);
-        consider(128, 4, 32, 1, 0.37, 0.13, 3.5);
+        large(256, 2, 16, 1, 1.06, 0.28, 5.0);
+        large(128, 2, 16, 2, 0.88, 0.0, 4.0);
+        large(128, 2, 1, 1, 0.60, 0.0, 4.2);
+        large(128, 4, 32, 1, 0.32, 0.12, 5.0);
     } else {
-        consider(128, 2, 16, 2, 1.8, 0.0, 4.0);
-        consider(128, 2, 32, 1, 1.05, 0.0, 3.0);
+        large(128, 2, 16, 2, 1.8, 0.0, 4.0);
+        large(128, 2, 32, 1, 1.05, 0.0, 4.6);
     }
     return best;
 }
@@ -505,12 +518,12 @@ template <int FA, int FB, typename T> void launch(hipStream_t s, const Fp8Produc
     const Route r = route(sizeof(T) == 2, p.M, p.N, p.K);
     const T *const bias = (const T *)p.bias, *const resid = (const T *)p.resid;
     const uint8_t *const A = (const uint8_t *)p.A, *const B = (const uint8_t *)p.B;
-    if (!r.tile) {
-        const int64_t tiles_n = (p.N + 15) / 16;
-        gemm_fp8_direct_k<FA, FB, T, 1, 1><<<(unsigned)tiles_n, 256, 0, s>>>(A, B, bias, resid, p.ldr, (T *)p.C, p.ldc, p.M, p.N, p.K, (int)tiles_n);
-        return;
-    }
     const int tiles_m = (int)((p.M + r.tile - 1) / r.tile), tiles_n = (int)((p.N + r.tile - 1) / r.tile);
+    auto direct = [&](auto kernel) {
+        kernel<<<(unsigned)((int64_t)tiles_m * tiles_n), 256, 0, s>>>(A, B, bias, resid, p.ldr, (T *)p.C, p.ldc, p.M, p.N, p.K, tiles_n);
+    };
+    if (r.tile == 16) return direct(gemm_fp8_direct_k<FA, FB, T, 1, 1>);
+    if (r.tile == 32) return direct(gemm_fp8_direct_k<FA, FB, T, 2, 2>);
     const dim3 grid((unsigned)(((int64_t)tiles_m * tiles_n + 7) / 8 * 8), (unsigned)r.splits);
     // kernels with more LDS than a launch has without asking
     auto go = [&](auto kernel, uint32_t lds) {

@@ -496,7 +496,7 @@ int tio_op_gemm_fp8(void *stream, int32_t dtype, int64_t M, int64_t N, int64_t K
 int tio_op_dropout(void *stream, int32_t dtype, int64_t rows, int64_t cols, const void *x, int64_t ldx, const void *resid, int64_t ldr, void *y, int64_t ldy,
                    double p, uint64_t seed, uint64_t offset);
 
-/* Between two blocks of a layer, rows of d elements (at most 16384, rows at most 2^31):
+/* Between two blocks of a layer, rows of d elements (at most 8192, rows at most 2^31):
  *   n = N(branch; post_gain, post_bias), or branch without post_gain;   u = dropout(n), a mask of [rows, d] as above;
  *   y = resid_scale x + branch_scale gate u;   h = N(y; gain, bias)
  * N(v; g, b) = (v - mean) / sqrt(mean((v - mean)^2) + eps) g + b, or with rms v / sqrt(mean(v^2) + eps) g.  gate: NULL, one row for all rows (ldg =

@@ -166,7 +166,7 @@ struct ResidualArgs {
     const void *dy, *dh;                         // the backward pass
     void *dx, *dbranch, *dgate, *dpost_gain, *dpost_bias, *dgain, *dbias, *work;
 };
-constexpr int64_t RESIDUAL_WIDEST = 16384;
+constexpr int64_t RESIDUAL_WIDEST = 8192;
 int64_t residual_norm_bwd_work(int64_t rows, int64_t d);
 void residual_norm(hipStream_t s, int dtype, const ResidualArgs &a);
 void residual_norm_bwd(hipStream_t s, int dtype, const ResidualArgs &a);

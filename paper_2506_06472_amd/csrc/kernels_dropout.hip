@@ -17,12 +17,11 @@ constexpr int TPB = 256;
 template <typename T, bool RESID>
 __global__ void __launch_bounds__(TPB) dropout_k(const T *x, int64_t ldx, const T *resid, int64_t ldr, T *y, int64_t ldy, uint32_t rows, uint32_t cols,
                                                  uint32_t groups, Dropout d) {
-    const uint64_t idx = (uint64_t)blockIdx.x * TPB + threadIdx.x;
-    const uint32_t row = (uint32_t)(idx / groups), c = (uint32_t)(idx - (uint64_t)row * groups);
+    const uint32_t idx = blockIdx.x * TPB + threadIdx.x, row = idx / groups, c = idx - row * groups;      // below 2^31 + TPB
     if (row >= rows) return;
     Row8<T> v, r;
-    v.load(x + row * ldx + c * 8);
-    if (RESID) r.load(resid + row * ldr + c * 8);
+    v.load(x + (int64_t)row * ldx + c * 8);
+    if (RESID) r.load(resid + (int64_t)row * ldr + c * 8);
     Mask8 m;
     m.draw(row, groups, c, d);
     float f[8], g[8];
@@ -35,7 +34,7 @@ __global__ void __launch_bounds__(TPB) dropout_k(const T *x, int64_t ldx, const 
     }
     cut8(f, (int)(cols - c * 8));
     v.set(f);
-    v.put(y + row * ldy + c * 8);
+    v.put(y + (int64_t)row * ldy + c * 8);
 }
 
 }  // namespace

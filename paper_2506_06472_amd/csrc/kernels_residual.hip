@@ -5,9 +5,17 @@
 //   dx = rs D,  dgate = bs u D,  dn = bs gate mask D,  dbranch = N_post^T(dn),
 //   N^T(g) = rstd (g gain - vh mean(g gain vh) [- mean(g gain)]),  vh = (v - mean) rstd,  dgain = sum of g vh and dbias = sum of g over the rows.
 //
-// Bound: HBM.  A row is W wavefronts', who hold it in registers from its loads to its stores; statistics and sums are in 32 bits, the layer norm's
-// variance from centred values.  A workgroup takes rows one after the other and keeps its share of the column sums in registers; a second launch
-// adds the workgroups' shares in their order, so that results do not depend on timing.
+// Both passes have, of every element, only what varies from row to row: with s the mask's factor and bh the branch (normalised, with a norm behind it),
+// the branch's part of y is kept ? bh w + c : 0, where w = bs s gate post_gain and c = bs s gate post_bias are a column's (a gate for every row is one
+// factor more); and with m = kept ? D : 0 the gradients of gate, post_gain and post_bias are a column's factors of the same two sums over the rows,
+//   S1 = sum of m bh,  S2 = sum of m:   dpost_gain = bs s gate S1,  dpost_bias = bs s gate S2,  dgate = bs s (post_gain S1 + post_bias S2).
+//
+// Bound: HBM; the vector ALU, with about 14 (forward) and 24 operations on an element beside the generator's, is not far behind.  A row is W
+// wavefronts', who hold it in registers from its loads to its stores; statistics and sums are in 32 bits, the layer norm's variance from centred values.  A
+// workgroup takes rows one after the other and keeps its share of the column sums in registers; a second launch adds the workgroups' shares in their
+// order, so that results do not depend on timing.
+#include <algorithm>
+
 #include "../../include/teraio.h"
 #include "device_common.h"
 #include "kernels.h"
@@ -19,361 +27,420 @@ namespace k {
 
 namespace {
 
-// Sums of V numbers over a row's wavefronts, in all of their threads.  `red`: LDS of 2 W V floats, halves used in turn (one barrier a sum).
-template <int W, int V> struct RowSum {
+template <int CTRL> __device__ __forceinline__ float dpp_add(float v) {
+    return v + __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+// the sum over a wavefront, in all lanes, without a trip through LDS
+__device__ __forceinline__ float wave_total(float v) {
+    v = dpp_add<0xB1>(v);                                      // lanes 1 0 3 2
+    v = dpp_add<0x4E>(v);                                      // lanes 2 3 0 1
+    v = dpp_add<0x141>(v);                                     // eight lanes mirrored
+    v = dpp_add<0x140>(v);                                     // sixteen lanes mirrored
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// Sums over a row's W wavefronts, in all of their threads.  `red`: LDS of 4 W floats, halves used in turn (one barrier a sum).
+template <int W> struct RowSum {
     float *red;
     int turn = 0;
     __device__ __forceinline__ explicit RowSum(float *r) : red(r) {}
-    __device__ __forceinline__ void operator()(float (&v)[V], int n = V) {
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (i < n) v[i] = wave_sum(v[i]);
+    __device__ __forceinline__ void operator()(float &u) {
+        u = wave_total(u);
         if (W == 1) return;
-        float *const at = red + turn * W * V;
-        turn ^= 1;
-        const int wave = threadIdx.x >> 6;
-        if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (i < n) at[wave * V + i] = v[i];
-        }
+        float *const at = half();
+        if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = u;
         __syncthreads();
+        u = at[0];
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (i < n) {
-                v[i] = at[i];
-#pragma unroll
-                for (int w = 1; w < W; ++w) v[i] += at[w * V + i];
-            }
+        for (int w = 1; w < W; ++w) u += at[w];
+    }
+    __device__ __forceinline__ void operator()(float &u, float &v) {
+        u = wave_total(u);
+        v = wave_total(v);
+        if (W == 1) return;
+        float2 *const at = reinterpret_cast<float2 *>(half());
+        if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = make_float2(u, v);
+        __syncthreads();
+        u = at[0].x;
+        v = at[0].y;
+#pragma unroll 1                                               // sixteen at once would be 32 registers
+        for (int w = 1; w < W; ++w) {
+            u += at[w].x;
+            v += at[w].y;
+        }
+    }
+private:
+    __device__ __forceinline__ float *half() {
+        float *const at = red + turn * 2 * W;
+        turn ^= 1;
+        return at;
     }
 };
 
-template <typename T> __device__ __forceinline__ void load8(float (&f)[8], const T *p) {
-    Row8<T> v;
-    v.load(p);
-    v.get(f);
-}
-template <typename T> __device__ __forceinline__ void put8(T *p, float (&f)[8], int n) {
-    cut8(f, n);
-    Row8<T> v;
-    v.set(f);
-    v.put(p);
-}
+// A thread's eight columns of a row that W wavefronts share, and what stays the same for all rows.  Rows are read and written through descriptors of
+// their columns rounded up to 8, so that threads without columns need no branches.
+template <typename T, int W, bool RMS, bool POST> struct Columns {
+    uint32_t lane, col, bytes;                                 // thread of the row, its first column, bytes of a row
+    int n;                                                     // columns that are there
+    bool ragged;                                               // the last eight are not whole
+    float w[8], c[8], gain[8];                                 // c: of the layer norm behind the block
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t row(const void *base, int64_t at) const { return buffer_over((const T *)base + at, bytes); }
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t row_or_none(const void *base, int64_t at) const { return buffer_over((const T *)base + at, base ? bytes : 0); }
+    __device__ __forceinline__ void get(float (&f)[8], const Row8<T> &v) const {
+        v.get(f);
+        if (ragged) cut8(f, n);
+    }
+    __device__ __forceinline__ void load(float (&f)[8], const void *base) const {
+        Row8<T> v;
+        row_load(v, row(base, 0), col);
+        get(f, v);
+    }
+    __device__ __forceinline__ void put(void *base, int64_t at, float (&f)[8]) const {
+        if (ragged) cut8(f, n);
+        Row8<T> v;
+        v.set(f);
+        row_put(v, row(base, at), col);
+    }
+    __device__ __forceinline__ Columns(const ResidualArgs &a)
+        : lane(W == 1 ? threadIdx.x & 63 : threadIdx.x), col(lane * 8), bytes((uint32_t)((a.d + 7) / 8 * 8 * sizeof(T))), ragged(a.d % 8 != 0) {
+        const int left = (int)a.d - (int)col;
+        n = left < 0 ? 0 : left < 8 ? left : 8;
+        load(gain, a.gain);
+        const float factor = a.branch_scale * (a.drop.limit ? a.drop.scale : 1.f);
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            w[j] = j < n ? factor : 0.f;
+            c[j] = 0.f;
+        }
+        if (a.gate && !a.ldg) {
+            load(f, a.gate);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] *= f[j];
+        }
+        if (POST && !RMS && a.post_bias) {
+            load(f, a.post_bias);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) c[j] = w[j] * f[j];
+        }
+        if (POST) {
+            load(f, a.post_gain);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] *= f[j];
+        }
+    }
+};
 
-// mean and 1 / sqrt(variance + eps) of a row, whose columns past the end are zero
-template <bool RMS, int W, int NCH> __device__ __forceinline__ void stats_of(const float (&v)[NCH][8], const int (&n)[NCH], float inv_d, float eps, RowSum<W, 2> &sum,
-                                                                             float &mean, float &rstd) {
-    float t[2] = {0.f, 0.f};
+// 1 / sqrt(t) from the hardware's, which is off by one unit in the last place and has no subnormal arguments
+__device__ __forceinline__ float inverse_root(float t) {
+    const bool tiny = t < 0x1p-100f;
+    return __builtin_amdgcn_rsqf(tiny ? t * 0x1p100f : t) * (tiny ? 0x1p50f : 1.f);
+}
+// mean and 1 / sqrt(variance + eps) of a row
+template <bool RMS, int W> __device__ __forceinline__ void stats_of(const float (&v)[8], int n, float inv_d, float eps, RowSum<W> &sum, float &mean, float &rstd) {
+    float t = 0.f;
     mean = 0.f;
     if (!RMS) {
 #pragma unroll
-        for (int c = 0; c < NCH; ++c)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) t[0] += v[c][j];
-        sum(t, 1);
-        mean = t[0] * inv_d;
-        t[0] = 0.f;
+        for (int j = 0; j < 8; ++j) t += v[j];
+        sum(t);
+        mean = t * inv_d;
+        t = 0.f;
     }
 #pragma unroll
-    for (int c = 0; c < NCH; ++c)
+    for (int j = 0; j < 8; ++j) {
+        const float e = RMS ? v[j] : j < n ? v[j] - mean : 0.f;
+        t += e * e;
+    }
+    sum(t);
+    rstd = inverse_root(t * inv_d + eps);
+}
+
+constexpr int teams_of(int W) { return W == 1 ? 4 : 1; }       // rows that a workgroup has at a time
+
+template <typename T, int W, bool RMS, bool POST>
+__global__ void __launch_bounds__(W == 1 ? 256 : W * 64) residual_norm_k(ResidualArgs a) {
+    __shared__ float red[4 * W];
+    RowSum<W> sum(red);
+    const Columns<T, W, RMS, POST> col(a);
+    const void *const gate = a.ldg ? a.gate : nullptr;
+    const uint32_t groups = (uint32_t)((a.d + 7) / 8);
+    const float inv_d = 1.0f / (float)a.d;
+    float bias[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (!RMS && a.bias) col.load(bias, a.bias);
+    const int team = W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+    const int64_t stride = (int64_t)gridDim.x * teams_of(W);
+    int64_t row = (int64_t)blockIdx.x * teams_of(W) + team;
+    Row8<T> next[3];
+    auto fetch = [&](int64_t at) __attribute__((always_inline)) {
+        if (at >= a.rows) at = a.rows - 1;
+        row_load(next[0], col.row(a.branch, at * a.ld), col.col);
+        row_load(next[1], col.row(a.x, at * a.ld), col.col);
+        row_load(next[2], col.row_or_none(gate, at * a.ldg), col.col);
+    };
+    fetch(row);
+    for (; row < a.rows; row += stride) {
+        const Row8<T> raw[3] = {next[0], next[1], next[2]};
+        fetch(row + stride);
+        Mask8 m;
+        if (a.drop.limit) m.draw(row, groups, col.lane, a.drop);
+        float v[8], r[8], g[8], mean = 0.f, rstd = 1.f;
+        col.get(v, raw[0]);
+        if (POST) {
+            stats_of<RMS, W>(v, col.n, inv_d, a.eps, sum, mean, rstd);
+            if (col.lane == 0) *reinterpret_cast<float2 *>(a.stats + row * 4) = make_float2(mean, rstd);
+        }
+        col.get(r, raw[1]);
+        if (gate) col.get(g, raw[2]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float e = RMS ? v[c][j] : j < n[c] ? v[c][j] - mean : 0.f;
-            t[0] += e * e;
+            float t = POST ? (v[j] - mean) * rstd * col.w[j] : v[j] * col.w[j];
+            if (POST && !RMS) t += col.c[j];
+            if (gate) t *= g[j];
+            if (a.drop.limit) t = m.kept(j, a.drop) ? t : 0.f;
+            v[j] = a.resid_scale * r[j] + t;
         }
-    sum(t, 1);
-    rstd = 1.0f / sqrtf(t[0] * inv_d + eps);
-}
-
-template <typename T, int W, int NCH, bool RMS, bool POST>
-__global__ void __launch_bounds__(W == 1 ? 256 : W * 64) residual_norm_k(ResidualArgs a) {
-    constexpr int TEAMS = W == 1 ? 4 : 1;
-    __shared__ float red[2 * W * 2];
-    const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x, team = W == 1 ? threadIdx.x >> 6 : 0;
-    RowSum<W, 2> sum(red);
-    const T *const branch = (const T *)a.branch, *const x = (const T *)a.x, *const gate = (const T *)a.gate;
-    const T *const post_gain = (const T *)a.post_gain, *const post_bias = (const T *)a.post_bias, *const gain = (const T *)a.gain, *const bias = (const T *)a.bias;
-    const uint32_t groups = (uint32_t)((a.d + 7) / 8);
-    const float inv_d = 1.0f / (float)a.d;
-    int n[NCH];                                                // columns of this thread's chunks that are there
+        col.put(a.y, row * a.ld, v);
+        stats_of<RMS, W>(v, col.n, inv_d, a.eps, sum, mean, rstd);
+        if (col.lane == 0) *reinterpret_cast<float2 *>(a.stats + row * 4 + 2) = make_float2(mean, rstd);
 #pragma unroll
-    for (int c = 0; c < NCH; ++c) {
-        const int64_t left = a.d - (int64_t)(c * W * 64 + lane) * 8;
-        n[c] = left < 0 ? 0 : left < 8 ? (int)left : 8;
-    }
-    for (int64_t row = (int64_t)blockIdx.x * TEAMS + team; row < a.rows; row += (int64_t)gridDim.x * TEAMS) {
-        float v[NCH][8], r[NCH][8];
-#pragma unroll
-        for (int c = 0; c < NCH; ++c) {
-            const int64_t at = row * a.ld + (c * W * 64 + lane) * 8;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[c][j] = r[c][j] = 0.f;
-            if (n[c]) {
-                load8(v[c], branch + at);
-                load8(r[c], x + at);
-                cut8(v[c], n[c]);
-                cut8(r[c], n[c]);
-            }
-        }
-        float mean, rstd;
-        if (POST) {
-            stats_of<RMS, W, NCH>(v, n, inv_d, a.eps, sum, mean, rstd);
-            if (lane == 0) *reinterpret_cast<float2 *>(a.stats + row * 4) = make_float2(mean, rstd);
-        }
-#pragma unroll
-        for (int c = 0; c < NCH; ++c) {
-            if (!n[c]) continue;
-            const int at = (c * W * 64 + lane) * 8;
-            if (POST) {
-                float g[8], b[8];
-                load8(g, post_gain + at);
-                if (!RMS && post_bias) load8(b, post_bias + at);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[c][j] = (v[c][j] - mean) * rstd * g[j] + (!RMS && post_bias ? b[j] : 0.f);
-            }
-            if (a.drop.limit) {
-                Mask8 m;
-                m.draw(row, groups, c * W * 64 + lane, a.drop);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[c][j] = m.kept(j, a.drop) ? v[c][j] * a.drop.scale : 0.f;
-            }
-            if (gate) {
-                float g[8];
-                load8(g, gate + row * a.ldg + at);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[c][j] *= g[j];
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[c][j] = a.resid_scale * r[c][j] + a.branch_scale * v[c][j];
-            cut8(v[c], n[c]);
-            put8((T *)a.y + row * a.ld + at, v[c], n[c]);
-        }
-        stats_of<RMS, W, NCH>(v, n, inv_d, a.eps, sum, mean, rstd);
-        if (lane == 0) *reinterpret_cast<float2 *>(a.stats + row * 4 + 2) = make_float2(mean, rstd);
-#pragma unroll
-        for (int c = 0; c < NCH; ++c) {
-            if (!n[c]) continue;
-            const int at = (c * W * 64 + lane) * 8;
-            float g[8], b[8];
-            load8(g, gain + at);
-            if (!RMS && bias) load8(b, bias + at);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[c][j] = (v[c][j] - mean) * rstd * g[j] + (!RMS && bias ? b[j] : 0.f);
-            put8((T *)a.h + row * a.ld + at, v[c], n[c]);
-        }
+        for (int j = 0; j < 8; ++j) v[j] = (v[j] - mean) * rstd * col.gain[j] + bias[j];
+        col.put(a.h, row * a.ld, v);
     }
 }
 
-// The column sums of a workgroup's rows: [kind][workgroup][columns rounded up to 8], kinds dgain, dbias, dgate, dpost_gain, dpost_bias.
-template <typename T, int W, int NCH, bool RMS, bool POST>
+// The column sums of a workgroup's rows: [kind][workgroup][columns rounded up to 8], kinds dgain, S1, dbias, S2.
+constexpr int KINDS = 4;
+template <typename T, int W, bool RMS, bool POST>
 __global__ void __launch_bounds__(W == 1 ? 256 : W * 64) residual_norm_bwd_k(ResidualArgs a) {
-    constexpr int TEAMS = W == 1 ? 4 : 1;
-    __shared__ float red[2 * W * 2];
-    const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x, team = W == 1 ? threadIdx.x >> 6 : 0;
-    RowSum<W, 2> sum(red);
-    const T *const branch = (const T *)a.branch, *const y = (const T *)a.y, *const gate = (const T *)a.gate, *const dy = (const T *)a.dy, *const dh = (const T *)a.dh;
-    const T *const post_gain = (const T *)a.post_gain, *const post_bias = (const T *)a.post_bias, *const gain = (const T *)a.gain;
+    __shared__ float red[4 * W];
+    RowSum<W> sum(red);
+    const Columns<T, W, RMS, POST> col(a);
+    const void *const gate = a.ldg ? a.gate : nullptr;
     const uint32_t groups = (uint32_t)((a.d + 7) / 8);
     const float inv_d = 1.0f / (float)a.d;
-    const bool sum_gate = gate && a.ldg == 0;
-    int n[NCH];
-    float s_gain[NCH][8], s_bias[NCH][8], s_gate[NCH][8], s_pgain[NCH][8], s_pbias[NCH][8];
+    const bool sum1 = POST || (a.gate && !a.ldg);
+    const float factor = a.branch_scale * (a.drop.limit ? a.drop.scale : 1.f);
+    float s_gain[8], s_bias[8], s1[8], s2[8];
 #pragma unroll
-    for (int c = 0; c < NCH; ++c) {
-        const int64_t left = a.d - (int64_t)(c * W * 64 + lane) * 8;
-        n[c] = left < 0 ? 0 : left < 8 ? (int)left : 8;
+    for (int j = 0; j < 8; ++j) s_gain[j] = s_bias[j] = s1[j] = s2[j] = 0.f;
+    const int team = W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+    const int64_t stride = (int64_t)gridDim.x * teams_of(W);
+    int64_t row = (int64_t)blockIdx.x * teams_of(W) + team;
+    // The next row's loads are under way while a row is computed, so that they do not wait behind its stores (8192 x 4096: 75 -> 70 us, with half the
+    // workgroups, and so half the sums; forward 62 -> 51); but for the widest rows, whose threads have no registers for them.
+    constexpr bool AHEAD = W < 16 || (RMS && sizeof(T) == 2);
+    Row8<T> next[5];
+    float4 next_st;                                            // branch's mean and 1 / sqrt, y's
+    auto fetch_first = [&](int64_t at) __attribute__((always_inline)) {
+        row_load(next[0], col.row(a.y, at * a.ld), col.col);
+        row_load(next[1], col.row(a.dh, at * a.ld), col.col);
+        next_st = *reinterpret_cast<const float4 *>(a.stats + at * 4);
+    };
+    auto fetch_others = [&](int64_t at) __attribute__((always_inline)) {
+        row_load(next[2], col.row(a.dy, at * a.ld), col.col);
+        row_load(next[3], col.row(a.branch, at * a.ld), col.col);
+        row_load(next[4], col.row_or_none(gate, at * a.ldg), col.col);
+    };
+    auto fetch = [&](int64_t at) __attribute__((always_inline)) {
+        if (at >= a.rows) at = a.rows - 1;
+        fetch_first(at);
+        fetch_others(at);
+    };
+    if (AHEAD) fetch(row);
+    for (; row < a.rows; row += stride) {
+        if (!AHEAD) fetch_first(row);
+        Row8<T> raw[5] = {next[0], next[1], next[2], next[3], next[4]};
+        const float4 st = next_st;
+        const int64_t at = row * a.ld;
+        if (AHEAD) fetch(row + stride);
+        Mask8 m;
+        if (a.drop.limit) m.draw(row, groups, col.lane, a.drop);
+        float r[8], g[8], D[8], v[8], t = 0.f, u = 0.f;
+        col.get(r, raw[0]);
+        col.get(g, raw[1]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s_gain[c][j] = s_bias[c][j] = s_gate[c][j] = s_pgain[c][j] = s_pbias[c][j] = 0.f;
-    }
-    for (int64_t row = (int64_t)blockIdx.x * TEAMS + team; row < a.rows; row += (int64_t)gridDim.x * TEAMS) {
-        const float4 st = *reinterpret_cast<const float4 *>(a.stats + row * 4);      // post mean, post rstd, mean, rstd
-        float v[NCH][8], r[NCH][8], g[NCH][8], D[NCH][8];
-        float t[2] = {0.f, 0.f};
-#pragma unroll
-        for (int c = 0; c < NCH; ++c) {
-            const int64_t at = row * a.ld + (c * W * 64 + lane) * 8;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[c][j] = r[c][j] = g[c][j] = D[c][j] = 0.f;
-            if (n[c]) {
-                float w[8];
-                load8(v[c], branch + at);
-                load8(r[c], y + at);
-                load8(g[c], dh + at);
-                load8(D[c], dy + at);
-                load8(w, gain + (c * W * 64 + lane) * 8);
-                cut8(v[c], n[c]);
-                cut8(g[c], n[c]);
-                cut8(D[c], n[c]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    r[c][j] = j < n[c] ? (r[c][j] - st.z) * st.w : 0.f;
-                    s_gain[c][j] += g[c][j] * r[c][j];
-                    if (!RMS) s_bias[c][j] += g[c][j];
-                    g[c][j] *= j < n[c] ? w[j] : 0.f;
-                    t[0] += g[c][j] * r[c][j];
-                    t[1] += g[c][j];
-                }
-            }
+        for (int j = 0; j < 8; ++j) {
+            r[j] = RMS ? r[j] * st.w : j < col.n ? (r[j] - st.z) * st.w : 0.f;
+            s_gain[j] += g[j] * r[j];
+            if (!RMS) s_bias[j] += g[j];
+            g[j] *= col.gain[j];
+            t += g[j] * r[j];
+            if (!RMS) u += g[j];
         }
-        sum(t, RMS ? 1 : 2);
-        const float c1 = t[0] * inv_d, c2 = RMS ? 0.f : t[1] * inv_d;
-        t[0] = t[1] = 0.f;
+        if (RMS) sum(t);
+        else sum(t, u);
+        const float c1 = t * inv_d, c2 = RMS ? 0.f : u * inv_d;
+        t = u = 0.f;
+        if (!AHEAD) {
+            fetch_others(row);
+            raw[2] = next[2];
+            raw[3] = next[3];
+            raw[4] = next[4];
+        }
+        col.get(D, raw[2]);
 #pragma unroll
-        for (int c = 0; c < NCH; ++c) {
-            if (!n[c]) continue;
-            const int at = (c * W * 64 + lane) * 8;
-            float w[8], b[8], e[8];
+        for (int j = 0; j < 8; ++j) {
+            D[j] += (g[j] - r[j] * c1 - c2) * st.w;
+            r[j] = a.resid_scale * D[j];
+        }
+        col.put(a.dx, at, r);
+        col.get(v, raw[3]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                D[c][j] += (g[c][j] - r[c][j] * c1 - c2) * st.w;
-                e[j] = a.resid_scale * D[c][j];
-            }
-            put8((T *)a.dx + row * a.ld + at, e, n[c]);
-            if (POST) {
-                load8(w, post_gain + at);
-                if (!RMS && post_bias) load8(b, post_bias + at);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    v[c][j] = j < n[c] ? (v[c][j] - st.x) * st.y : 0.f;
-                    e[j] = v[c][j] * w[j] + (!RMS && post_bias ? b[j] : 0.f);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) e[j] = v[c][j];
-            }
-            float scale[8];                                    // what dropout multiplies by
-            Mask8 m;
-            if (a.drop.limit) m.draw(row, groups, c * W * 64 + lane, a.drop);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) scale[j] = !a.drop.limit ? 1.f : m.kept(j, a.drop) ? a.drop.scale : 0.f;
-            float q[8];
-            if (gate) load8(q, gate + row * a.ldg + at);
+        for (int j = 0; j < 8; ++j) {
+            if (a.drop.limit) D[j] = m.kept(j, a.drop) ? D[j] : 0.f;
+            if (POST) v[j] = RMS ? v[j] * st.y : j < col.n ? (v[j] - st.x) * st.y : 0.f;
+            else if (a.drop.limit) v[j] = m.kept(j, a.drop) ? v[j] : 0.f;            // not a number, perhaps
+        }
+        if (gate) {
+            float c[8];
+            if (POST && !RMS && a.post_bias) col.load(c, a.post_bias);
+            col.get(g, raw[4]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float bD = a.branch_scale * D[c][j], u = scale[j] == 0.f ? 0.f : e[j] * scale[j];
-                e[j] = bD * u;                                 // the gate's gradient
-                g[c][j] = j < n[c] ? bD * scale[j] * (gate ? q[j] : 1.f) : 0.f;        // dn
+                r[j] = D[j] * (v[j] * col.w[j] + (POST && !RMS && a.post_bias ? c[j] * factor : 0.f));
+                D[j] *= g[j];
             }
-            if (sum_gate) {
+            col.put(a.dgate, row * a.ldg, r);
+        }
 #pragma unroll
-                for (int j = 0; j < 8; ++j) s_gate[c][j] += e[j];
-            } else if (gate) put8((T *)a.dgate + row * a.ldg + at, e, n[c]);
-            if (POST) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    s_pgain[c][j] += g[c][j] * v[c][j];
-                    if (!RMS) s_pbias[c][j] += g[c][j];
-                    g[c][j] *= j < n[c] ? w[j] : 0.f;
-                    t[0] += g[c][j] * v[c][j];
-                    t[1] += g[c][j];
-                }
-            } else put8((T *)a.dbranch + row * a.ld + at, g[c], n[c]);
+        for (int j = 0; j < 8; ++j) {
+            if (sum1) {
+                const float q = D[j] * v[j];
+                s1[j] += q;
+                if (POST) t += q * col.w[j];
+            }
+            if (POST && !RMS) s2[j] += D[j];
+            g[j] = D[j] * col.w[j];
+            if (POST && !RMS) u += g[j];
         }
         if (POST) {
-            sum(t, RMS ? 1 : 2);
-            const float p1 = t[0] * inv_d, p2 = RMS ? 0.f : t[1] * inv_d;
+            if (RMS) sum(t);
+            else sum(t, u);
+            const float p1 = t * inv_d, p2 = RMS ? 0.f : u * inv_d;
 #pragma unroll
-            for (int c = 0; c < NCH; ++c) {
-                if (!n[c]) continue;
+            for (int j = 0; j < 8; ++j) g[j] = (g[j] - v[j] * p1 - p2) * st.y;
+        }
+        col.put(a.dbranch, at, g);
+    }
+    const int64_t d8 = (int64_t)groups * 8;
+    __shared__ float rows_of[W == 1 ? 4 : 1][W == 1 ? 512 : 1];
+    auto out = [&](int kind, const float (&f)[8]) __attribute__((always_inline)) {
+        float *const to = (float *)a.work + ((int64_t)kind * gridDim.x + blockIdx.x) * d8;
+        if constexpr (W == 1) {                                // the four rows' sums in their order
+            __syncthreads();
 #pragma unroll
-                for (int j = 0; j < 8; ++j) g[c][j] = (g[c][j] - v[c][j] * p1 - p2) * st.y;
-                put8((T *)a.dbranch + row * a.ld + (c * W * 64 + lane) * 8, g[c], n[c]);
+            for (int j = 0; j < 8; ++j) rows_of[team][col.col + j] = f[j];
+            __syncthreads();
+            for (int i = threadIdx.x; i < d8; i += 256) to[i] = rows_of[0][i] + rows_of[1][i] + rows_of[2][i] + rows_of[3][i];
+        } else if (col.n) {
+            *reinterpret_cast<float4 *>(to + col.col) = make_float4(f[0], f[1], f[2], f[3]);
+            *reinterpret_cast<float4 *>(to + col.col + 4) = make_float4(f[4], f[5], f[6], f[7]);
+        }
+    };
+    out(0, s_gain);
+    if (sum1) out(1, s1);
+    if (!RMS) out(2, s_bias);
+    if (POST && !RMS) out(3, s2);
+}
+
+// A workgroup adds 16 columns: sums[k] over the workgroups' shares of kind k, in their order within each of 64 slices, the slices in theirs.
+template <typename T> __global__ void __launch_bounds__(256) residual_sums_k(ResidualArgs a, int64_t parts) {
+    __shared__ float4 part[64][4];
+    __shared__ float sums[KINDS][16];
+    const int q = threadIdx.x & 3, slice = threadIdx.x >> 2;
+    const int64_t d8 = (a.d + 7) / 8 * 8, col = (int64_t)blockIdx.x * 16 + q * 4;
+    const bool post = a.post_gain, shared = a.gate && !a.ldg;
+    const float *const work = (const float *)a.work;
+    for (int kind = 0; kind < KINDS; ++kind) {
+        if ((kind == 1 && !post && !shared) || (kind >= 2 && a.rms) || (kind == 3 && !post)) continue;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (col < d8) {
+            const float *from = work + kind * parts * d8 + col;
+#pragma unroll 8
+            for (int64_t p = slice; p < parts; p += 64) {
+                const float4 t = *reinterpret_cast<const float4 *>(from + p * d8);
+                v.x += t.x; v.y += t.y; v.z += t.z; v.w += t.w;
             }
         }
-    }
-    const int64_t d8 = (int64_t)groups * 8, teams = (int64_t)gridDim.x * TEAMS, mine = (int64_t)blockIdx.x * TEAMS + team;
-    float *const work = (float *)a.work;
-#pragma unroll
-    for (int c = 0; c < NCH; ++c) {
-        if (!n[c]) continue;
-        const int64_t at = mine * d8 + (c * W * 64 + lane) * 8;
-        auto out = [&](int kind, const float (&f)[8]) __attribute__((always_inline)) {
-            float *const to = work + kind * teams * d8 + at;
-            *reinterpret_cast<float4 *>(to) = make_float4(f[0], f[1], f[2], f[3]);
-            *reinterpret_cast<float4 *>(to + 4) = make_float4(f[4], f[5], f[6], f[7]);
-        };
-        out(0, s_gain[c]);
-        if (!RMS) out(1, s_bias[c]);
-        if (sum_gate) out(2, s_gate[c]);
-        if (POST) out(3, s_pgain[c]);
-        if (POST && !RMS) out(4, s_pbias[c]);
-    }
-}
-
-struct Sums {
-    void *out[5];                // nullptr: none of that kind
-};
-// A workgroup adds 64 columns of one kind: four lanes' width of rows of parts, sixteen of which go on at a time.
-template <typename T> __global__ void __launch_bounds__(256) residual_sums_k(const float *__restrict__ work, int64_t parts, int64_t d, Sums s) {
-    __shared__ float4 part[16][16];
-    const int kind = blockIdx.y, q = threadIdx.x & 15, slice = threadIdx.x >> 4;
-    T *const out = (T *)s.out[kind];
-    if (!out) return;
-    const int64_t d8 = (d + 7) / 8 * 8, col = (int64_t)blockIdx.x * 64 + q * 4;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (col < d8)
-        for (int64_t p = slice; p < parts; p += 16) {
-            const float4 t = *reinterpret_cast<const float4 *>(work + (kind * parts + p) * d8 + col);
-            v.x += t.x; v.y += t.y; v.z += t.z; v.w += t.w;
+        __syncthreads();
+        part[slice][q] = v;
+        __syncthreads();
+        if (threadIdx.x < 16) {
+            float t = 0.f;
+#pragma unroll 16
+            for (int i = 0; i < 64; ++i) t += reinterpret_cast<const float *>(part[i])[threadIdx.x];
+            sums[kind][threadIdx.x] = t;
         }
-    part[slice][q] = v;
-    __syncthreads();
-    if (threadIdx.x >= 64) return;
-    const int64_t at = (int64_t)blockIdx.x * 64 + threadIdx.x;
-    float t = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) t += reinterpret_cast<const float *>(part[i])[threadIdx.x];
-    if (at < d8) out[at] = from_f32<T>(at < d ? t : 0.f);
+    }
+    const int64_t at = (int64_t)blockIdx.x * 16 + threadIdx.x;
+    if (threadIdx.x >= 16 || at >= d8) return;                 // each thread reads its own sums
+    const bool there = at < a.d;
+    const float factor = a.branch_scale * (a.drop.limit ? a.drop.scale : 1.f);
+    auto value = [&](const void *p) __attribute__((always_inline)) { return there && p ? to_f32(((const T *)p)[at]) : 0.f; };
+    auto out = [&](void *p, float f) __attribute__((always_inline)) {
+        if (p) ((T *)p)[at] = from_f32<T>(there ? f : 0.f);
+    };
+    out(a.dgain, sums[0][threadIdx.x]);
+    if (!a.rms) out(a.dbias, sums[2][threadIdx.x]);
+    const float g = factor * (shared ? value(a.gate) : 1.f), one = sums[1][threadIdx.x], two = a.rms || !post ? 0.f : sums[3][threadIdx.x];
+    if (post) out(a.dpost_gain, g * one);
+    if (post && !a.rms) out(a.dpost_bias, g * two);
+    if (shared) out(a.dgate, factor * (post ? value(a.post_gain) * one + (a.post_bias ? value(a.post_bias) * two : 0.f) : one));
 }
 
-constexpr int64_t MAX_GROUPS = 1024;                           // workgroups of the backward pass
-// wavefronts of a row, and the workgroups that take them
-int row_waves(int64_t d) { return d <= 1024 ? 1 : d <= 4096 ? 4 : d <= 8192 ? 8 : 16; }
-int64_t groups_of(int64_t rows, int64_t d) {
-    const int64_t teams = row_waves(d) == 1 ? 4 : 1, g = (rows + teams - 1) / teams;
-    return g < MAX_GROUPS ? g : MAX_GROUPS;
+// wavefronts of a row, and the workgroups that take the rows: what the compute units hold at a time
+int row_waves(int64_t d) { return d <= 512 ? 1 : d <= 1024 ? 2 : d <= 2048 ? 4 : d <= 4096 ? 8 : 16; }
+int64_t groups_of(int64_t rows, int64_t d, int waves, int64_t most) {
+    const int W = row_waves(d), teams = teams_of(W);
+    return std::min(std::min((rows + teams - 1) / teams, most), (int64_t)256 * std::max(1, waves / (W * teams)));
 }
-int64_t parts_of(int64_t rows, int64_t d) { return groups_of(rows, d) * (row_waves(d) == 1 ? 4 : 1); }
+int64_t forward_groups(int64_t rows, int64_t d) { return groups_of(rows, d, 24, 4096); }
+int64_t backward_groups(int64_t rows, int64_t d) { return groups_of(rows, d, 16, 1024); }
 
 }  // namespace
 
-int64_t residual_norm_bwd_work(int64_t rows, int64_t d) { return 5 * parts_of(rows, d) * ((d + 7) / 8 * 8) * 4; }
+int64_t residual_norm_bwd_work(int64_t rows, int64_t d) { return KINDS * backward_groups(rows, d) * ((d + 7) / 8 * 8) * 4; }
 
-#define TIO_BY_NORM(KERNEL, W, NCH)                                                                                                     \
-    do {                                                                                                                                \
-        const unsigned grid = (unsigned)groups_of(a.rows, a.d), block = W == 1 ? 256 : W * 64;                                          \
-        if (dtype == TIO_PREC_BF16) {                                                                                                   \
-            if (a.rms && a.post_gain) KERNEL<bf16_t, W, NCH, true, true><<<grid, block, 0, s>>>(a);                                     \
-            else if (a.rms) KERNEL<bf16_t, W, NCH, true, false><<<grid, block, 0, s>>>(a);                                              \
-            else if (a.post_gain) KERNEL<bf16_t, W, NCH, false, true><<<grid, block, 0, s>>>(a);                                        \
-            else KERNEL<bf16_t, W, NCH, false, false><<<grid, block, 0, s>>>(a);                                                        \
-        } else {                                                                                                                        \
-            if (a.rms && a.post_gain) KERNEL<float, W, NCH, true, true><<<grid, block, 0, s>>>(a);                                      \
-            else if (a.rms) KERNEL<float, W, NCH, true, false><<<grid, block, 0, s>>>(a);                                               \
-            else if (a.post_gain) KERNEL<float, W, NCH, false, true><<<grid, block, 0, s>>>(a);                                         \
-            else KERNEL<float, W, NCH, false, false><<<grid, block, 0, s>>>(a);                                                         \
-        }                                                                                                                               \
+#define TIO_BY_NORM(KERNEL, W)                                                                                                      \
+    do {                                                                                                                            \
+        const unsigned block = W == 1 ? 256 : W * 64;                                      \
+        if (dtype == TIO_PREC_BF16) {                                                                                               \
+            if (a.rms && a.post_gain) KERNEL<bf16_t, W, true, true><<<grid, block, 0, s>>>(a);                                      \
+            else if (a.rms) KERNEL<bf16_t, W, true, false><<<grid, block, 0, s>>>(a);                                               \
+            else if (a.post_gain) KERNEL<bf16_t, W, false, true><<<grid, block, 0, s>>>(a);                                         \
+            else KERNEL<bf16_t, W, false, false><<<grid, block, 0, s>>>(a);                                                         \
+        } else {                                                                                                                    \
+            if (a.rms && a.post_gain) KERNEL<float, W, true, true><<<grid, block, 0, s>>>(a);                                       \
+            else if (a.rms) KERNEL<float, W, true, false><<<grid, block, 0, s>>>(a);                                                \
+            else if (a.post_gain) KERNEL<float, W, false, true><<<grid, block, 0, s>>>(a);                                          \
+            else KERNEL<float, W, false, false><<<grid, block, 0, s>>>(a);                                                          \
+        }                                                                                                                           \
     } while (0)
-#define TIO_BY_WIDTH(KERNEL)                          \
-    do {                                              \
-        if (a.d <= 512) TIO_BY_NORM(KERNEL, 1, 1);    \
-        else if (a.d <= 1024) TIO_BY_NORM(KERNEL, 1, 2); \
-        else if (a.d <= 2048) TIO_BY_NORM(KERNEL, 4, 1); \
-        else if (a.d <= 4096) TIO_BY_NORM(KERNEL, 4, 2); \
-        else if (a.d <= 8192) TIO_BY_NORM(KERNEL, 8, 2); \
-        else TIO_BY_NORM(KERNEL, 16, 2);              \
+#define TIO_BY_WIDTH(KERNEL)                  \
+    do {                                      \
+        switch (row_waves(a.d)) {             \
+        case 1: TIO_BY_NORM(KERNEL, 1); break;  \
+        case 2: TIO_BY_NORM(KERNEL, 2); break;  \
+        case 4: TIO_BY_NORM(KERNEL, 4); break;  \
+        case 8: TIO_BY_NORM(KERNEL, 8); break;  \
+        default: TIO_BY_NORM(KERNEL, 16); break; \
+        }                                     \
     } while (0)
 
-void residual_norm(hipStream_t s, int dtype, const ResidualArgs &a) { TIO_BY_WIDTH(residual_norm_k); }
+void residual_norm(hipStream_t s, int dtype, const ResidualArgs &a) {
+    const unsigned grid = (unsigned)forward_groups(a.rows, a.d);
+    TIO_BY_WIDTH(residual_norm_k);
+}
 
 void residual_norm_bwd(hipStream_t s, int dtype, const ResidualArgs &a) {
+    const unsigned grid = (unsigned)backward_groups(a.rows, a.d), columns = (unsigned)((a.d + 15) / 16);
     TIO_BY_WIDTH(residual_norm_bwd_k);
-    const Sums sums{{a.dgain, a.rms ? nullptr : a.dbias, a.gate && a.ldg == 0 ? a.dgate : nullptr, a.post_gain ? a.dpost_gain : nullptr,
-                     a.post_gain && !a.rms ? a.dpost_bias : nullptr}};
-    const dim3 grid((unsigned)((a.d + 63) / 64), 5);
-    const int64_t parts = parts_of(a.rows, a.d);
-    if (dtype == TIO_PREC_BF16) residual_sums_k<bf16_t><<<grid, 256, 0, s>>>((const float *)a.work, parts, a.d, sums);
-    else residual_sums_k<float><<<grid, 256, 0, s>>>((const float *)a.work, parts, a.d, sums);
+    if (dtype == TIO_PREC_BF16) residual_sums_k<bf16_t><<<columns, 256, 0, s>>>(a, grid);
+    else residual_sums_k<float><<<columns, 256, 0, s>>>(a, grid);
 }
 
 }  // namespace k

@@ -38,7 +38,7 @@ const char *residual_args(int32_t dtype, const tio_residual_cfg *cfg, int64_t ro
     if (!cfg || !gain) return "null argument";
     if (!known_type(dtype)) return "unknown element type";
     if (rows < 1 || d < 1) return "non-positive dimension";
-    if (d > k::RESIDUAL_WIDEST) return "a row must be at most 16384 wide";
+    if (d > k::RESIDUAL_WIDEST) return "a row must be at most 8192 wide";
     if (rows > (int64_t)1 << 31) return "at most 2^31 rows";
     if (!stride_ok(ld, d) || (gate && ldg != 0 && !stride_ok(ldg, d))) return BAD_STRIDE;
     if (!(cfg->eps >= 0.f) || !std::isfinite(cfg->eps) || !std::isfinite(cfg->resid_scale) || !std::isfinite(cfg->branch_scale))
@@ -140,7 +140,7 @@ int tio_op_residual_norm(void *stream, int32_t dtype, const tio_residual_cfg *cf
 
 int tio_op_residual_norm_bwd_work(int64_t rows, int64_t d, uint64_t *out_bytes) {
     if (!out_bytes) return fail(TIO_ERR_INVALID_ARG, "null argument");
-    if (rows < 1 || d < 1 || d > k::RESIDUAL_WIDEST || rows > (int64_t)1 << 31) return fail(TIO_ERR_INVALID_ARG, "rows must be 1 to 2^31, their width 1 to 16384");
+    if (rows < 1 || d < 1 || d > k::RESIDUAL_WIDEST || rows > (int64_t)1 << 31) return fail(TIO_ERR_INVALID_ARG, "rows must be 1 to 2^31, their width 1 to 8192");
     *out_bytes = (uint64_t)k::residual_norm_bwd_work(rows, d);
     return TIO_OK;
 }

@@ -27,6 +27,20 @@ template <> struct Row8<float> {
     __device__ __forceinline__ void get(float *f) const { lo.get(f); hi.get(f + 4); }
     __device__ __forceinline__ void set(const float *f) { lo.set(f); hi.set(f + 4); }
 };
+// through a buffer descriptor over a row: columns past its end read as zeros, and are not written; stores go past the caches
+__device__ __forceinline__ void row_load(Row8<bf16_t> &v, __amdgpu_buffer_rsrc_t row, uint32_t col) { buffer_load16(v.v, row, col * 2); }
+__device__ __forceinline__ void row_load(Row8<float> &v, __amdgpu_buffer_rsrc_t row, uint32_t col) {
+    buffer_load16(v.lo, row, col * 4);
+    buffer_load16(v.hi, row, col * 4 + 16);
+}
+constexpr int BUFFER_NT = 2;
+__device__ __forceinline__ void row_put(const Row8<bf16_t> &v, __amdgpu_buffer_rsrc_t row, uint32_t col) {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(tio_u32x4, v.v.raw), row, (int)(col * 2), 0, BUFFER_NT);
+}
+__device__ __forceinline__ void row_put(const Row8<float> &v, __amdgpu_buffer_rsrc_t row, uint32_t col) {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(tio_u32x4, v.lo.raw), row, (int)(col * 4), 0, BUFFER_NT);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(tio_u32x4, v.hi.raw), row, (int)(col * 4 + 16), 0, BUFFER_NT);
+}
 // columns from n on become zero
 __device__ __forceinline__ void cut8(float *f, int n) {
     if (n >= 8) return;

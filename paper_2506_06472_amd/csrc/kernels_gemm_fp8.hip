@@ -155,6 +155,18 @@ __global__ void __launch_bounds__(256) gemm_fp8_sums_k(const float *__restrict__
     Out8<T>(bias, col, N).put(v, resid ? resid + row * ldr + col : nullptr, C + row * ldc + col);
 }
 
+// p: sixteen rows of 32 columns, four lanes to a row, q: the 32 columns behind them.  top: rows 0 .. 7 of all 64, eight lanes to a row; low: rows 8 .. 15.
+__device__ __forceinline__ void trade_rows(const Row8<bf16_t> &p, const Row8<bf16_t> &q, Row8<bf16_t> &top, Row8<bf16_t> &low) {
+    const uint32_t a[4] = {p.v.raw.x, p.v.raw.y, p.v.raw.z, p.v.raw.w}, b[4] = {q.v.raw.x, q.v.raw.y, q.v.raw.z, q.v.raw.w};
+    uint32_t t[4], l[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {                              // lanes rotated by eight within sixteen; the others' lanes keep what they have
+        t[e] = (uint32_t)__builtin_amdgcn_update_dpp((int)a[e], (int)b[e], 0x128, 0xf, 0xc, false);
+        l[e] = (uint32_t)__builtin_amdgcn_update_dpp((int)b[e], (int)a[e], 0x128, 0xf, 0x3, false);
+    }
+    top.v.raw = make_uint4(t[0], t[1], t[2], t[3]);
+    low.v.raw = make_uint4(l[0], l[1], l[2], l[3]);
+}
 // A wavefront's 16 TM x 16 TN results, from row mw and column nw on.  Rows of 16 x 32: the two halves of register pairs trade places so that a lane has
 // eight neighbours of a row.  The common case, whole parts without bias and residual, has no tests between its stores.  Outputs of 64 MiB and more go past the
 // caches, which they would push the operands out of: with operands and outputs that are in no cache 8192 x 11008 x 4096 330 -> 321 us, 11008 x 4096 x
@@ -172,19 +184,40 @@ __device__ __forceinline__ void store_part(const floatx4 (&acc)[TM][TN], int lan
         }
     };
     if (nsplit == 1 && !bias && !resid && mw + 16 * TM <= M && nw + 16 * TN <= N) {
-        T *const to = C + row0 * ldc + col0;
         auto whole = [&](auto STREAM) __attribute__((always_inline)) {
+            auto out = [&](const Row8<T> &r, T *to) __attribute__((always_inline)) {
+                if constexpr (STREAM()) r.put(to);
+                else r.store(to);
+            };
+            if constexpr (sizeof(T) == 2 && TN % 4 == 0) {
+                T *const to = C + (mw + (lane & 7)) * ldc + nw + (lane >> 3 & 1) * 32 + (lane >> 4 & 1) * 16 + (lane >> 5) * 8;
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+                for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int j = 0; j < TN; j += 2) {
-                    float v[8];
-                    eight(i, j, v);
-                    Row8<T> r;
-                    r.set(v);
-                    if constexpr (STREAM()) r.put(to + i * 16 * ldc + j * 16);
-                    else r.store(to + i * 16 * ldc + j * 16);
-                }
+                    for (int j = 0; j < TN; j += 4) {
+                        float v[8], w[8];
+                        eight(i, j, v);
+                        eight(i, j + 2, w);
+                        Row8<T> p, q, top, low;
+                        p.set(v);
+                        q.set(w);
+                        trade_rows(p, q, top, low);
+                        out(top, to + i * 16 * ldc + j * 16);
+                        out(low, to + (i * 16 + 8) * ldc + j * 16);
+                    }
+            } else {
+                T *const to = C + row0 * ldc + col0;
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; j += 2) {
+                        float v[8];
+                        eight(i, j, v);
+                        Row8<T> r;
+                        r.set(v);
+                        out(r, to + i * 16 * ldc + j * 16);
+                    }
+            }
         };
         if (M * N * (int64_t)sizeof(T) >= (int64_t)64 << 20) whole(std::true_type{});
         else whole(std::false_type{});

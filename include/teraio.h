@@ -512,7 +512,7 @@ typedef struct tio_residual_cfg {
 int tio_op_residual_norm(void *stream, int32_t dtype, const tio_residual_cfg *cfg, int64_t rows, int64_t d, int64_t ld, const void *branch, const void *x,
                          const void *gate, int64_t ldg, const void *post_gain, const void *post_bias, const void *gain, const void *bias, void *y, void *h,
                          float *stats);
-/* Gradients from dy (of y where it goes on as the residual) and dh, the same cfg, branch, the forward pass's y and stats.  dgate (where there is a
+/* Gradients from dy (of y where it goes on as the residual) and dh, the same cfg, branch, and the forward pass's y, as it was rounded, and stats.  dgate (where there is a
  * gate) is one row, the sum over the rows, or rows like the gate's; dpost_gain (where there is post_gain), dgain, and of the layer norm dpost_bias and
  * dbias (NULL: not wanted) are rows summed over all rows, in 32 bits and always in the same order.  dx may be dy.  work: device memory of
  * tio_op_residual_norm_bwd_work bytes, contents of no interest before and after, used by one call at a time. */

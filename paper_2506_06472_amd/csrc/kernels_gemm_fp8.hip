@@ -553,6 +553,12 @@ Route route(bool bf16, int64_t M, int64_t N, int64_t K) {
     return best;
 }
 
+// more LDS than a launch has without asking; asked for once for each kernel
+template <auto KERNEL, uint32_t LDS> void allow_lds() {
+    static const hipError_t allowed = hipFuncSetAttribute((const void *)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, (int)LDS);
+    (void)allowed;
+}
+
 template <int FA, int FB, typename T> void launch(hipStream_t s, const Fp8Product &p) {
     const Route r = route(sizeof(T) == 2, p.M, p.N, p.K);
     const T *const bias = (const T *)p.bias, *const resid = (const T *)p.resid;
@@ -564,17 +570,12 @@ template <int FA, int FB, typename T> void launch(hipStream_t s, const Fp8Produc
     if (r.tile == 16) return direct(gemm_fp8_direct_k<FA, FB, T, 1, 1>);
     if (r.tile == 32) return direct(gemm_fp8_direct_k<FA, FB, T, 2, 2>);
     const dim3 grid((unsigned)(((int64_t)tiles_m * tiles_n + 7) / 8 * 8), (unsigned)r.splits);
-    // kernels with more LDS than a launch has without asking
-    auto go = [&](auto kernel, uint32_t lds) {
-        static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        (void)allowed;
-        kernel<<<grid, 256, lds, s>>>(A, B, bias, resid, p.ldr, (T *)p.C, p.ldc, p.M, p.N, p.K, tiles_m, tiles_n, (float *)p.work);
-    };
+    auto go = [&](auto kernel, uint32_t lds) { kernel<<<grid, 256, lds, s>>>(A, B, bias, resid, p.ldr, (T *)p.C, p.ldc, p.M, p.N, p.K, tiles_m, tiles_n, (float *)p.work); };
     if constexpr (sizeof(T) == 2) {
-        if (r.tile == 256) go(gemm_fp8_tile_k<FA, FB, 8, 8, 2>, Loads<8, 8, 2>::LDS);
-        else if (r.deep == 4) go(gemm_fp8_tile_k<FA, FB, 4, 4, 4>, Loads<4, 4, 4>::LDS);
-        else go(gemm_fp8_tile_k<FA, FB, 4, 4, 2>, Loads<4, 4, 2>::LDS);
-    } else go(gemm_fp8_tile32_k<FA, FB>, Loads<4, 4, 2>::LDS);
+        if (r.tile == 256) allow_lds<gemm_fp8_tile_k<FA, FB, 8, 8, 2>, Loads<8, 8, 2>::LDS>(), go(gemm_fp8_tile_k<FA, FB, 8, 8, 2>, Loads<8, 8, 2>::LDS);
+        else if (r.deep == 4) allow_lds<gemm_fp8_tile_k<FA, FB, 4, 4, 4>, Loads<4, 4, 4>::LDS>(), go(gemm_fp8_tile_k<FA, FB, 4, 4, 4>, Loads<4, 4, 4>::LDS);
+        else allow_lds<gemm_fp8_tile_k<FA, FB, 4, 4, 2>, Loads<4, 4, 2>::LDS>(), go(gemm_fp8_tile_k<FA, FB, 4, 4, 2>, Loads<4, 4, 2>::LDS);
+    } else allow_lds<gemm_fp8_tile32_k<FA, FB>, Loads<4, 4, 2>::LDS>(), go(gemm_fp8_tile32_k<FA, FB>, Loads<4, 4, 2>::LDS);
     if (r.splits > 1)
         gemm_fp8_sums_k<T><<<(unsigned)((p.M * ((p.N + 7) / 8) + 255) / 256), 256, 0, s>>>((const float *)p.work, r.splits, bias, resid, p.ldr, (T *)p.C, p.ldc, p.M, p.N);
 }

@@ -631,6 +631,13 @@ def tio_op_gemm_fp8(stream_handle, dtype, M, N, K, form_a, A_ptr, form_b, B_ptr,
         _check(rc)
 
 
+def tio_op_gemm_fp8_route(dtype, M, N, K):
+    """(tile, steps on their way, ranges of the contraction) of a product of stored matrices; host only."""
+    out = [C.c_int32() for _ in range(3)]
+    _check(lib().tio_op_gemm_fp8_route(PREC[dtype], C.c_int64(M), C.c_int64(N), C.c_int64(K), *[C.byref(v) for v in out]))
+    return tuple(v.value for v in out)
+
+
 def tio_op_dropout(stream_handle, dtype, rows, cols, x_ptr, ldx, resid_ptr, ldr, y_ptr, ldy, p, seed, offset):
     rc = lib().tio_op_dropout(stream_handle, PREC[dtype], rows, cols, x_ptr, ldx, resid_ptr, ldr, y_ptr, ldy, p, seed, offset)
     if rc:

@@ -587,6 +587,13 @@ int64_t gemm_fp8_work(int64_t M, int64_t N, int64_t K) {
     return most > 1 ? most * M * ((N + 7) / 8 * 8) * 4 : 0;
 }
 
+void gemm_fp8_route(int dtype, int64_t M, int64_t N, int64_t K, int *tile, int *deep, int *ranges) {
+    const Route r = route(dtype == TIO_PREC_BF16, M, N, K);
+    *tile = r.tile;
+    *deep = r.deep;
+    *ranges = r.splits;
+}
+
 void gemm_fp8(hipStream_t s, int dtype, const Fp8Product &p) {
 #define TIO_FORMS(T)                                                  \
     do {                                                              \

@@ -119,6 +119,15 @@ int tio_op_gemm_fp8(void *stream, int32_t dtype, int64_t M, int64_t N, int64_t K
     TIO_OP_END
 }
 
+int tio_op_gemm_fp8_route(int32_t dtype, int64_t M, int64_t N, int64_t K, int32_t *out_tile, int32_t *out_deep, int32_t *out_ranges) {
+    if (!out_tile || !out_deep || !out_ranges) return fail(TIO_ERR_INVALID_ARG, "null argument");
+    if (!known_type(dtype)) return fail(TIO_ERR_INVALID_ARG, "unknown element type");
+    if (const char *wrong = fp8_args(M, K)) return fail(TIO_ERR_INVALID_ARG, wrong);
+    if (const char *wrong = fp8_args(N, K)) return fail(TIO_ERR_INVALID_ARG, wrong);
+    k::gemm_fp8_route(dtype, M, N, K, out_tile, out_deep, out_ranges);
+    return TIO_OK;
+}
+
 int tio_op_residual_norm(void *stream, int32_t dtype, const tio_residual_cfg *cfg, int64_t rows, int64_t d, int64_t ld, const void *branch, const void *x,
                          const void *gate, int64_t ldg, const void *post_gain, const void *post_bias, const void *gain, const void *bias, void *y, void *h,
                          float *stats) {

@@ -194,6 +194,48 @@ def test_scales_far_apart(dtype):
     assert (np.abs(got - want) <= _bound(qa, qb, want, dtype)).all()
 
 
+WAYS = [("bf16", 9, 700, 1000, (16, 1, 1)), ("bf16", 33, 500, 9000, (16, 1, 1)), ("bf16", 1000, 500, 300, (32, 1, 1)), ("bf16", 768, 768, 8000, (128, 4, 4)),
+        ("bf16", 1000, 4000, 4000, (128, 4, 1)), ("bf16", 4100, 770, 700, (128, 4, 1)), ("bf16", 8000, 750, 780, (128, 2, 1)), ("bf16", 4000, 4100, 1000, (256, 2, 1)),
+        ("bf16", 2048, 768, 30000, (128, 4, 2)), ("bf16", 17, 4163, 38991, (128, 2, 15)), ("bf16", 154, 5450, 30935, (256, 2, 11)),
+        ("bf16", 6000, 5000, 130, (256, 2, 1)), ("fp32", 9, 700, 1000, (16, 1, 1)), ("fp32", 1000, 500, 300, (32, 1, 1)),
+        ("fp32", 1000, 1000, 8000, (128, 2, 4)), ("fp32", 4000, 1500, 500, (128, 2, 1)), ("fp32", 2000, 2050, 300, (128, 2, 1))]
+
+
+@pytest.mark.parametrize("dtype,M,N,K,way", WAYS)
+def test_every_way_to_take_a_product(dtype, M, N, K, way):
+    """Small whole numbers, whose products and sums are exact however they are added (up to 2^6 each, 2^24 in all): the rounded result, alone and with bias and
+    residual, whose sum with a product is exact too."""
+    import torch
+    import paper_2506_06472_amd as tio
+    assert tio.tio_op_gemm_fp8_route(dtype, M, N, K) == way
+    t, up = l8.types(dtype), lambda n: (n + 7) // 8 * 8
+    g = torch.Generator(device="cuda").manual_seed(K)
+    whole = lambda r, c, top: torch.randint(-top, top + 1, (r, c), device="cuda", generator=g).float()
+
+    def padded(v, fill):
+        b = torch.full((v.shape[0], up(v.shape[1]) + 8), fill, device="cuda", dtype=t)
+        b[:, :v.shape[1]] = v
+        return b
+    a, b, bias, resid = whole(M, K, 8), whole(N, K, 8), whole(1, N, 100), whole(M, N, 100)
+    assert K * 64 < 1 << 24
+    q = []
+    for v, rows in ((a, M), (b, N)):
+        v[:, ::128] = 8.0                                       # blocks have a scale of their own, but the same for all
+        p = padded(v, float("nan"))
+        q.append(torch.empty(tio.tio_fp8_bytes(rows, K), device="cuda", dtype=torch.uint8))
+        tio.tio_op_fp8_store(0, dtype, "e4m3", False, rows, K, p.data_ptr(), p.stride(0), q[-1].data_ptr())
+    work = torch.full((tio.tio_op_gemm_fp8_work(M, N, K) + 64,), 255, device="cuda", dtype=torch.uint8)
+    pb, pr = padded(bias, float("nan")), padded(resid, float("nan"))
+    want = a.double() @ b.double().t()
+    for with_bias, with_resid in ((0, 0), (1, 1)):
+        c = torch.full((M + 1, up(N) + 8), 7.0, device="cuda", dtype=t)
+        tio.tio_op_gemm_fp8(0, dtype, M, N, K, "e4m3", q[0].data_ptr(), "e4m3", q[1].data_ptr(), c.data_ptr(), c.stride(0), pb.data_ptr() * with_bias,
+                            pr.data_ptr() * with_resid, pr.stride(0), work.data_ptr())
+        ref = want + with_bias * bias + with_resid * resid
+        assert torch.equal(c[:M, :N], ref.to(t)) and (c[:M, N:up(N)] == 0).all() and (c[:M, up(N):] == 7.0).all() and (c[M:] == 7.0).all()
+    assert (work[-64:] == 255).all()
+
+
 def test_calls_in_a_graph_and_on_another_stream():
     """A linear layer's calls captured once and replayed on new values, with eager work in between; the same bits as eager calls."""
     import torch

@@ -36,16 +36,17 @@ typedef short f8_s16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 f8_bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f8_f32x2 __attribute__((ext_vector_type(2)));
 
-// FORM: 0 e4m3, 1 e5m2.  Exponent byte of a block from the bits of its largest magnitude.
-template <int FORM> __device__ __forceinline__ uint32_t f8_exponent(uint32_t top) {
-    const int e = (int)((top + 0x1fffffu) >> 23) - (FORM ? 15 : 8);
-    return (uint32_t)(e < F8_LEAST ? F8_LEAST : e);
+// FORM: 0 e4m3, 1 e5m2.  A block's power of two, as the bits of an fp32, from the bits of its largest magnitude: the sum carries into the exponent where the
+// fraction is above 1.75.
+template <int FORM> __device__ __forceinline__ uint32_t f8_power(uint32_t top) {
+    const int e = (int)(top + 0x1fffffu - ((FORM ? 15u : 8u) << 23)) & (int)0xff800000u;
+    return (uint32_t)(e < (F8_LEAST << 23) ? F8_LEAST << 23 : e);
 }
 __device__ __forceinline__ bool f8_finite(uint32_t top) { return top < 0x7f800000u; }
 
 // codes of four neighbours, each divided by `scale`, a power of two: the instructions round to nearest even
 template <int FORM> __device__ __forceinline__ uint32_t f8_codes(uint32_t ab, uint32_t cd, float scale) {          // pairs of bf16
-    f8_s16x2 w = {0, 0};
+    f8_s16x2 w = __builtin_nondeterministic_value(w);           // both halves are written
     const f8_bf16x2 lo = __builtin_bit_cast(f8_bf16x2, ab), hi = __builtin_bit_cast(f8_bf16x2, cd);
     if (FORM) {
         w = __builtin_amdgcn_cvt_scalef32_pk_bf8_bf16(w, lo, scale, false);
@@ -57,7 +58,7 @@ template <int FORM> __device__ __forceinline__ uint32_t f8_codes(uint32_t ab, ui
     return __builtin_bit_cast(uint32_t, w);
 }
 template <int FORM> __device__ __forceinline__ uint32_t f8_codes(float a, float b, float c, float d, float scale) {
-    f8_s16x2 w = {0, 0};
+    f8_s16x2 w = __builtin_nondeterministic_value(w);
     if (FORM) {
         w = __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(w, a, b, scale, false);
         w = __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(w, c, d, scale, true);

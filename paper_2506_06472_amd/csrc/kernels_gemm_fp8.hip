@@ -133,13 +133,7 @@ template <typename T> struct Out8 {
         r.store(to);
     }
 };
-// The sums of a cut contraction: [range][M][N rounded up to 8] in 32 bits.
-__device__ __forceinline__ void put_partial(float *ws, int split, int64_t M, int64_t N, int64_t row, int64_t col, const float (&v)[8]) {
-    float *const to = ws + ((int64_t)split * M + row) * ((N + 7) / 8 * 8) + col;
-    *reinterpret_cast<float4 *>(to) = make_float4(v[0], v[1], v[2], v[3]);
-    *reinterpret_cast<float4 *>(to + 4) = make_float4(v[4], v[5], v[6], v[7]);
-}
-// added in the ranges' order
+// The sums of a cut contraction, [range][M][N rounded up to 8] in 32 bits, added in the ranges' order
 template <typename T>
 __global__ void __launch_bounds__(256) gemm_fp8_sums_k(const float *__restrict__ ws, int nsplit, const T *__restrict__ bias, const T *resid, int64_t ldr, T *C,
                                                        int64_t ldc, int64_t M, int64_t N) {
@@ -155,88 +149,94 @@ __global__ void __launch_bounds__(256) gemm_fp8_sums_k(const float *__restrict__
     Out8<T>(bias, col, N).put(v, resid ? resid + row * ldr + col : nullptr, C + row * ldc + col);
 }
 
-// p: sixteen rows of 32 columns, four lanes to a row, q: the 32 columns behind them.  top: rows 0 .. 7 of all 64, eight lanes to a row; low: rows 8 .. 15.
-__device__ __forceinline__ void trade_rows(const Row8<bf16_t> &p, const Row8<bf16_t> &q, Row8<bf16_t> &top, Row8<bf16_t> &low) {
-    const uint32_t a[4] = {p.v.raw.x, p.v.raw.y, p.v.raw.z, p.v.raw.w}, b[4] = {q.v.raw.x, q.v.raw.y, q.v.raw.z, q.v.raw.w};
-    uint32_t t[4], l[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {                              // lanes rotated by eight within sixteen; the others' lanes keep what they have
-        t[e] = (uint32_t)__builtin_amdgcn_update_dpp((int)a[e], (int)b[e], 0x128, 0xf, 0xc, false);
-        l[e] = (uint32_t)__builtin_amdgcn_update_dpp((int)b[e], (int)a[e], 0x128, 0xf, 0x3, false);
-    }
-    top.v.raw = make_uint4(t[0], t[1], t[2], t[3]);
-    low.v.raw = make_uint4(l[0], l[1], l[2], l[3]);
-}
-// A wavefront's 16 TM x 16 TN results, from row mw and column nw on.  Rows of 16 x 32: the two halves of register pairs trade places so that a lane has
-// eight neighbours of a row.  The common case, whole parts without bias and residual, has no tests between its stores.  Outputs of 64 MiB and more go past the
-// caches, which they would push the operands out of: with operands and outputs that are in no cache 8192 x 11008 x 4096 330 -> 321 us, 11008 x 4096 x
-// 8192 287 -> 279.
+// A wavefront's 16 TM x 16 TN results, from row mw and column nw on, 16 rows at a time through LDS (`stage`: STAGE bytes of its own), since a store or load
+// whose neighbouring lanes are neighbours in memory moves 64 bytes a clock, one whose neighbouring lanes are in different rows, as the products leave their
+// results, 16 (8192 x 11008 x 4096 with cold caches 305 -> 293 us).  Rows are rotated in LDS by an exclusive or with the row number, so that sixteen lanes
+// write to different banks.  Outputs of 64 MiB and more go past the caches, which they would push the operands out of (330 -> 321 us).
+template <int TN> constexpr int stage_bytes() { return 64 * 64 * TN; }
 template <typename T, int TM, int TN>
-__device__ __forceinline__ void store_part(const floatx4 (&acc)[TM][TN], int lane, int64_t mw, int64_t nw, int64_t M, int64_t N, const T *__restrict__ bias,
-                                           const T *resid, int64_t ldr, T *C, int64_t ldc, float *ws, int split, int nsplit) {
-    const int64_t row0 = mw + (lane & 15), col0 = nw + (lane >> 4 & 1) * 16 + (lane >> 5) * 8;
-    auto eight = [&](int i, int j, float (&v)[8]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[i][j][e]), __float_as_uint(acc[i][j + 1][e]), false, false);
-            v[e] = __uint_as_float(t[0]);
-            v[4 + e] = __uint_as_float(t[1]);
-        }
-    };
-    if (nsplit == 1 && !bias && !resid && mw + 16 * TM <= M && nw + 16 * TN <= N) {
+__device__ __forceinline__ void store_part(floatx4 (&acc)[TM][TN], unsigned char *stage, int lane, int64_t mw, int64_t nw, int64_t M, int64_t N,
+                                           const T *__restrict__ bias, const T *resid, int64_t ldr, T *C, int64_t ldc, float *ws, int split, int nsplit) {
+    const int r16 = lane & 15, g4 = lane >> 4;
+    if (sizeof(T) == 2 && nsplit == 1 && !bias && !resid && mw + 16 * TM <= M && nw + 16 * TN <= N) {
+        // As bf16: the two halves of register pairs trade places so that a lane has eight neighbours of a row.
+        constexpr int CHUNKS = 2 * TN;                         // of eight results, to a row
+        auto turn = [](int row) __attribute__((always_inline)) { return CHUNKS == 16 ? row : row >> 1 & 7; };
         auto whole = [&](auto STREAM) __attribute__((always_inline)) {
-            auto out = [&](const Row8<T> &r, T *to) __attribute__((always_inline)) {
-                if constexpr (STREAM()) r.put(to);
-                else r.store(to);
-            };
-            if constexpr (sizeof(T) == 2 && TN % 4 == 0) {
-                T *const to = C + (mw + (lane & 7)) * ldc + nw + (lane >> 3 & 1) * 32 + (lane >> 4 & 1) * 16 + (lane >> 5) * 8;
 #pragma unroll
-                for (int i = 0; i < TM; ++i)
+            for (int i = 0; i < TM; ++i) {
+                unsigned char *const at = stage + (i & 1) * 16 * CHUNKS * 16;
+                int l = lane;
+                asm volatile("" : "+v"(l));                    // addresses are found anew: all blocks' at once would take more registers than there are
 #pragma unroll
-                    for (int j = 0; j < TN; j += 4) {
-                        float v[8], w[8];
-                        eight(i, j, v);
-                        eight(i, j + 2, w);
-                        Row8<T> p, q, top, low;
-                        p.set(v);
-                        q.set(w);
-                        trade_rows(p, q, top, low);
-                        out(top, to + i * 16 * ldc + j * 16);
-                        out(low, to + (i * 16 + 8) * ldc + j * 16);
+                for (int j = 0; j < TN; j += 2) {
+                    float v[8];
+                    // not found before the choice of STREAM, in which both ways would have all results in registers
+                    if constexpr (STREAM()) asm volatile("; past the caches" : "+v"(acc[i][j]), "+v"(acc[i][j + 1]));
+                    else asm volatile("; kept" : "+v"(acc[i][j]), "+v"(acc[i][j + 1]));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[i][j][e]), __float_as_uint(acc[i][j + 1][e]), false, false);
+                        v[e] = __uint_as_float(t[0]);
+                        v[4 + e] = __uint_as_float(t[1]);
                     }
-            } else {
-                T *const to = C + row0 * ldc + col0;
+                    *reinterpret_cast<uint4 *>(at + (r16 * CHUNKS + ((j * 2 + (g4 & 1) * 2 + (g4 >> 1)) ^ turn(r16))) * 16) =
+                        make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+                }
+                __builtin_amdgcn_wave_barrier();
 #pragma unroll
-                for (int i = 0; i < TM; ++i)
-#pragma unroll
-                    for (int j = 0; j < TN; j += 2) {
-                        float v[8];
-                        eight(i, j, v);
-                        Row8<T> r;
-                        r.set(v);
-                        out(r, to + i * 16 * ldc + j * 16);
-                    }
+                for (int p = 0; p < CHUNKS / 4; ++p) {
+                    const int row = (p * 64 + l) / CHUNKS, chunk = l % CHUNKS;
+                    Row8<bf16_t> out;
+                    out.v.raw = *reinterpret_cast<const uint4 *>(at + (row * CHUNKS + (chunk ^ turn(row))) * 16);
+                    bf16_t *const to = (bf16_t *)C + (mw + i * 16 + row) * ldc + nw + chunk * 8;
+                    if constexpr (STREAM()) out.put(to);
+                    else out.store(to);
+                }
+                __builtin_amdgcn_wave_barrier();
             }
         };
         if (M * N * (int64_t)sizeof(T) >= (int64_t)64 << 20) whole(std::true_type{});
         else whole(std::false_type{});
         return;
     }
+    // As fp32, for sums of ranges, bias, residual and edges, 64 rows at a time; a loop, since straight-line code for what few wavefronts run has to be
+    // fetched by them alone.
+    constexpr int QUADS = 4 * TN;                              // of four results, to a row
+    auto quad = [&](int row, int q) __attribute__((always_inline)) { return reinterpret_cast<float4 *>(stage + (row * QUADS + (q ^ (row & 15))) * 16); };
+    auto rows64 = [&](auto FIRST) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < TN; j += 2) {
-        const int64_t col = col0 + j * 16;
-        const Out8<T> out(bias, col, N);
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            float v[8];
-            eight(i, j, v);
-            const int64_t row = row0 + i * 16;
-            if (row >= M || col >= N) continue;                // after the exchange, in which all lanes take part
-            if (nsplit > 1) put_partial(ws, split, M, N, row, col, v);
-            else out.put(v, resid ? resid + row * ldr + col : nullptr, C + row * ldc + col);
+            for (int j = 0; j < TN; ++j) {
+                const floatx4 &t = acc[FIRST() + i][j];
+                *quad(i * 16 + r16, j * 4 + g4) = make_float4(t[0], t[1], t[2], t[3]);
+            }
+        __builtin_amdgcn_wave_barrier();
+        const int64_t m0 = mw + FIRST() * 16, N8 = (N + 7) / 8 * 8;
+        if (nsplit > 1) {
+            const int q = lane % QUADS;
+            const int64_t n = nw + q * 4;
+#pragma unroll 4
+            for (int row = lane / QUADS; row < 64; row += 64 / QUADS)
+                if (m0 + row < M && n < N8) *reinterpret_cast<float4 *>(ws + ((int64_t)split * M + m0 + row) * N8 + n) = *quad(row, q);
+        } else {
+            const int q = lane % (QUADS / 2) * 2;
+            const int64_t n = nw + q * 4;
+            const Out8<T> out(bias, n, N);
+#pragma unroll 2
+            for (int row = lane / (QUADS / 2); row < 64; row += 128 / QUADS) {
+                if (m0 + row >= M || n >= N) continue;
+                const float4 a = *quad(row, q), b = *quad(row, q + 1);
+                float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                out.put(v, resid ? resid + (m0 + row) * ldr + n : nullptr, C + (m0 + row) * ldc + n);
+            }
         }
-    }
+        __builtin_amdgcn_wave_barrier();
+    };
+    static_assert(TM == 4 || TM == 8, "64 rows, once or twice");
+    rows64(std::integral_constant<int, 0>{});
+    if constexpr (TM == 8) rows64(std::integral_constant<int, 4>{});
 }
 
 // ---- large products in bf16
@@ -442,11 +442,15 @@ __global__ void __launch_bounds__(256)
         static_assert(D == 4, "steps of the loop");
         while (!done(c0) && !done(std::integral_constant<int, 1>{}) && !done(std::integral_constant<int, 2>{}) && !done(std::integral_constant<int, 3>{})) {}
     }
-    __builtin_amdgcn_s_waitcnt(wait_vm(0));                    // LDS is the next workgroup's
+    __builtin_amdgcn_s_waitcnt(wait_vm(0));                    // nothing is on its way to LDS any more, for any wavefront: it takes the results
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
     settle();
     pin();
 
-    store_part<bf16_t, TM, TN>(acc, lane, (int64_t)tm * BM + wm * 16 * TM, (int64_t)tn * BN + wn * 16 * TN, M, N, bias, resid, ldr, C, ldc, ws, split, nsplit);
+    static_assert(4 * stage_bytes<TN>() <= (int)L::EXPS, "the results' places fit the fragments'");
+    store_part<bf16_t, TM, TN>(acc, smem8 + wave * stage_bytes<TN>(), lane, (int64_t)tm * BM + wm * 16 * TM, (int64_t)tn * BN + wn * 16 * TN, M, N, bias, resid,
+                               ldr, C, ldc, ws, split, nsplit);
 }
 
 // ---- in fp32: the values, which bf16 holds exactly, in 16-bit products, whose sums are those of 32-bit arithmetic.  A quarter to half of the 8-bit products' rate.
@@ -502,7 +506,10 @@ __global__ void __launch_bounds__(256, 2)
             }
         }
     }
-    store_part<float, TM, TN>(acc, lane, (int64_t)tm * L::BM + wm * 16 * TM, (int64_t)tn * L::BN + wn * 16 * TN, M, N, bias, resid, ldr, C, ldc, ws, split, nsplit);
+    __builtin_amdgcn_s_waitcnt(0x0070);
+    __builtin_amdgcn_s_barrier();                              // every wavefront is done with the fragments: LDS takes the results
+    asm volatile("" ::: "memory");
+    store_part<float, TM, TN>(acc, smem8 + wave * stage_bytes<TN>(), lane, (int64_t)tm * L::BM + wm * 16 * TM, (int64_t)tn * L::BN + wn * 16 * TN, M, N, bias, resid, ldr, C, ldc, ws, split, nsplit);
 }
 
 // How a product is taken: tiles of 128 or 256 through LDS, `deep` steps at a time, the contraction cut into ranges, or tiles of 16 or 32 from the caches

@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(W == 1 ? 256 : W * 64) residual_norm_k(Residua
 // The column sums of a workgroup's rows: [kind][workgroup][columns rounded up to 8], kinds dgain, S1, dbias, S2.
 constexpr int KINDS = 4;
 template <typename T, int W, bool RMS, bool POST>
-__global__ void __launch_bounds__(W == 1 ? 256 : W * 64) residual_norm_bwd_k(ResidualArgs a) {
+__global__ void __launch_bounds__(W == 1 ? 256 : W * 64, 4) residual_norm_bwd_k(ResidualArgs a) {
     __shared__ float red[4 * W];
     RowSum<W> sum(red);
     const Columns<T, W, RMS, POST> col(a);
@@ -231,8 +231,9 @@ __global__ void __launch_bounds__(W == 1 ? 256 : W * 64) residual_norm_bwd_k(Res
     const int64_t stride = (int64_t)gridDim.x * teams_of(W);
     int64_t row = (int64_t)blockIdx.x * teams_of(W) + team;
     // The next row's loads are under way while a row is computed, so that they do not wait behind its stores (8192 x 4096: 75 -> 70 us, with half the
-    // workgroups, and so half the sums; forward 62 -> 51); but for the widest rows, whose threads have no registers for them.
-    constexpr bool AHEAD = W < 16 || (RMS && sizeof(T) == 2);
+    // workgroups, and so half the sums; forward 62 -> 51), where a thread has registers for them: four wavefronts to a SIMD count for more (layer norm, bf16,
+    // 1000 x 4096, both passes: 50 us ahead, 45 so).
+    constexpr bool AHEAD = sizeof(T) == 2 && (RMS || !POST);
     Row8<T> next[5];
     float4 next_st;                                            // branch's mean and 1 / sqrt, y's
     auto fetch_first = [&](int64_t at) __attribute__((always_inline)) {
@@ -347,37 +348,34 @@ __global__ void __launch_bounds__(W == 1 ? 256 : W * 64) residual_norm_bwd_k(Res
     if (POST && !RMS) out(3, s2);
 }
 
-// A workgroup adds 16 columns: sums[k] over the workgroups' shares of kind k, in their order within each of 64 slices, the slices in theirs.
-template <typename T> __global__ void __launch_bounds__(256) residual_sums_k(ResidualArgs a, int64_t parts) {
-    __shared__ float4 part[64][4];
+// A workgroup adds 16 columns, four wavefronts a kind: the workgroups' shares in their order within each of 64 slices, the slices in theirs.
+template <typename T> __global__ void __launch_bounds__(256 * KINDS) residual_sums_k(ResidualArgs a, int64_t parts) {
+    __shared__ float4 part[KINDS][64][4];
     __shared__ float sums[KINDS][16];
-    const int q = threadIdx.x & 3, slice = threadIdx.x >> 2;
+    const int kind = threadIdx.x >> 8, q = threadIdx.x & 3, slice = threadIdx.x >> 2 & 63;
     const int64_t d8 = (a.d + 7) / 8 * 8, col = (int64_t)blockIdx.x * 16 + q * 4;
     const bool post = a.post_gain, shared = a.gate && !a.ldg;
-    const float *const work = (const float *)a.work;
-    for (int kind = 0; kind < KINDS; ++kind) {
-        if ((kind == 1 && !post && !shared) || (kind >= 2 && a.rms) || (kind == 3 && !post)) continue;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (col < d8) {
-            const float *from = work + kind * parts * d8 + col;
+    const bool there_is = kind == 0 || (kind == 1 ? post || shared : !a.rms && (kind == 2 || post));
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (there_is && col < d8) {
+        const float *from = (const float *)a.work + kind * parts * d8 + col;
 #pragma unroll 8
-            for (int64_t p = slice; p < parts; p += 64) {
-                const float4 t = *reinterpret_cast<const float4 *>(from + p * d8);
-                v.x += t.x; v.y += t.y; v.z += t.z; v.w += t.w;
-            }
-        }
-        __syncthreads();
-        part[slice][q] = v;
-        __syncthreads();
-        if (threadIdx.x < 16) {
-            float t = 0.f;
-#pragma unroll 16
-            for (int i = 0; i < 64; ++i) t += reinterpret_cast<const float *>(part[i])[threadIdx.x];
-            sums[kind][threadIdx.x] = t;
+        for (int64_t p = slice; p < parts; p += 64) {
+            const float4 t = *reinterpret_cast<const float4 *>(from + p * d8);
+            v.x += t.x; v.y += t.y; v.z += t.z; v.w += t.w;
         }
     }
+    part[kind][slice][q] = v;
+    __syncthreads();
+    if ((threadIdx.x & 255) < 16) {
+        float t = 0.f;
+#pragma unroll 16
+        for (int i = 0; i < 64; ++i) t += reinterpret_cast<const float *>(part[kind][i])[threadIdx.x & 15];
+        sums[kind][threadIdx.x & 15] = t;
+    }
+    __syncthreads();
     const int64_t at = (int64_t)blockIdx.x * 16 + threadIdx.x;
-    if (threadIdx.x >= 16 || at >= d8) return;                 // each thread reads its own sums
+    if (threadIdx.x >= 16 || at >= d8) return;
     const bool there = at < a.d;
     const float factor = a.branch_scale * (a.drop.limit ? a.drop.scale : 1.f);
     auto value = [&](const void *p) __attribute__((always_inline)) { return there && p ? to_f32(((const T *)p)[at]) : 0.f; };
@@ -439,8 +437,8 @@ void residual_norm(hipStream_t s, int dtype, const ResidualArgs &a) {
 void residual_norm_bwd(hipStream_t s, int dtype, const ResidualArgs &a) {
     const unsigned grid = (unsigned)backward_groups(a.rows, a.d), columns = (unsigned)((a.d + 15) / 16);
     TIO_BY_WIDTH(residual_norm_bwd_k);
-    if (dtype == TIO_PREC_BF16) residual_sums_k<bf16_t><<<columns, 256, 0, s>>>(a, grid);
-    else residual_sums_k<float><<<columns, 256, 0, s>>>(a, grid);
+    if (dtype == TIO_PREC_BF16) residual_sums_k<bf16_t><<<columns, 256 * KINDS, 0, s>>>(a, grid);
+    else residual_sums_k<float><<<columns, 256 * KINDS, 0, s>>>(a, grid);
 }
 
 }  // namespace k

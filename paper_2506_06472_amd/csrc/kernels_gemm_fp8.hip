@@ -62,13 +62,13 @@ template <int FA, int FB> __device__ __forceinline__ floatx4 product16(const Pie
 
 template <typename T> __device__ __forceinline__ float element(const T *p) { return to_f32(*p); }
 
-// A workgroup's tile of 16 TM x 16 TN results: its four wavefronts share the contraction, their sums are added in order.
-template <int FA, int FB, typename T, int TM, int TN>
-__global__ void __launch_bounds__(256) gemm_fp8_direct_k(const uint8_t *__restrict__ A, const uint8_t *__restrict__ B, const T *__restrict__ bias,
+// A workgroup's tile of 16 TM x 16 TN results: its NW wavefronts share the contraction, their sums are added in order.
+template <int FA, int FB, typename T, int TM, int TN, int NW>
+__global__ void __launch_bounds__(NW * 64) gemm_fp8_direct_k(const uint8_t *__restrict__ A, const uint8_t *__restrict__ B, const T *__restrict__ bias,
                                                          const T *__restrict__ resid, int64_t ldr, T *__restrict__ C, int64_t ldc, int64_t M, int64_t N,
                                                          int64_t K, int tiles_n) {
-    __shared__ float sums[4][TM * TN][256];
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    __shared__ float sums[NW][TM * TN][256];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int64_t tm = blockIdx.x / tiles_n, tn = blockIdx.x - tm * tiles_n;
     const Fp8Shape sa{M, K}, sb{N, K};
     const int64_t KB = sa.kb(), ga = sa.groups(), gb = sb.groups();
@@ -77,22 +77,43 @@ __global__ void __launch_bounds__(256) gemm_fp8_direct_k(const uint8_t *__restri
     for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = (floatx4){0.f, 0.f, 0.f, 0.f};
-    for (int64_t kb = wave; kb < KB; kb += 4) {
-        Piece8 a[TM], b[TN];
+    const uint8_t *fa[TM], *ea[TM], *fb[TN], *eb[TN];          // block 0 of each group; past the last one: the last
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            const int64_t g = tm * TM + i < ga ? tm * TM + i : ga - 1;
-            a[i].load(A + (g * KB + kb) * F8_FRAG, A + sa.code_bytes() + ((g >> 2) * KB + kb) * 64 + (g & 3), lane);
+    for (int i = 0; i < TM; ++i) {
+        const int64_t g = tm * TM + i < ga ? tm * TM + i : ga - 1;
+        fa[i] = A + g * KB * F8_FRAG;
+        ea[i] = A + sa.code_bytes() + (g >> 2) * KB * 64 + (g & 3);
+    }
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        const int64_t g = tn * TN + j < gb ? tn * TN + j : gb - 1;
+        fb[j] = B + g * KB * F8_FRAG;
+        eb[j] = B + sb.code_bytes() + (g >> 2) * KB * 64 + (g & 3);
+    }
+    // U blocks' loads before the first one's products: one after the other a wavefront waits for each (16 x 4096 x 11008, operands in no cache: 16.6 us, with
+    // eight wavefronts of four at once 11.2)
+    constexpr int U = NW == 8 ? 4 : TM == 2 ? 1 : 2;
+    for (int64_t kb = wave; kb < KB; kb += NW * U) {
+        Piece8 a[U][TM], b[U][TN];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = kb + NW * u;
+            if (at >= KB) continue;
+#pragma unroll
+            for (int i = 0; i < TM; ++i) a[u][i].load(fa[i] + at * F8_FRAG, ea[i] + at * 64, lane);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) b[u][j].load(fb[j] + at * F8_FRAG, eb[j] + at * 64, lane);
         }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            const int64_t g = tn * TN + j < gb ? tn * TN + j : gb - 1;
-            b[j].load(B + (g * KB + kb) * F8_FRAG, B + sb.code_bytes() + ((g >> 2) * KB + kb) * 64 + (g & 3), lane);
+        for (int u = 0; u < U; ++u) {
+            if (kb + NW * u >= KB) continue;
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+                    acc[i][j] = sizeof(T) == 2 ? product8<FA, FB>(a[u][i], b[u][j], acc[i][j]) : product16<FA, FB>(a[u][i], b[u][j], acc[i][j]);
         }
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = sizeof(T) == 2 ? product8<FA, FB>(a[i], b[j], acc[i][j]) : product16<FA, FB>(a[i], b[j], acc[i][j]);
     }
 #pragma unroll
     for (int i = 0; i < TM; ++i)
@@ -106,10 +127,10 @@ __global__ void __launch_bounds__(256) gemm_fp8_direct_k(const uint8_t *__restri
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
             const int64_t m = (tm * TM + i) * 16 + row, n = (tn * TN + j) * 16 + col;
-            if (m >= M || n >= (N + 7) / 8 * 8) continue;
+            if (tid >= 256 || m >= M || n >= (N + 7) / 8 * 8) continue;
             float v = sums[0][i * TN + j][at];
 #pragma unroll
-            for (int w = 1; w < 4; ++w) v += sums[w][i * TN + j][at];
+            for (int w = 1; w < NW; ++w) v += sums[w][i * TN + j][at];
             if (bias && n < N) v += element(bias + n);
             if (resid && n < N) v += element(resid + m * ldr + n);
             C[m * ldc + n] = from_f32<T>(n < N ? v : 0.f);
@@ -580,11 +601,13 @@ template <int FA, int FB, typename T> void launch(hipStream_t s, const Fp8Produc
     const T *const bias = (const T *)p.bias, *const resid = (const T *)p.resid;
     const uint8_t *const A = (const uint8_t *)p.A, *const B = (const uint8_t *)p.B;
     const int tiles_m = (int)((p.M + r.tile - 1) / r.tile), tiles_n = (int)((p.N + r.tile - 1) / r.tile);
-    auto direct = [&](auto kernel) {
-        kernel<<<(unsigned)((int64_t)tiles_m * tiles_n), 256, 0, s>>>(A, B, bias, resid, p.ldr, (T *)p.C, p.ldc, p.M, p.N, p.K, tiles_n);
+    auto direct = [&](auto kernel, int waves) {
+        kernel<<<(unsigned)((int64_t)tiles_m * tiles_n), (unsigned)waves * 64, 0, s>>>(A, B, bias, resid, p.ldr, (T *)p.C, p.ldc, p.M, p.N, p.K, tiles_n);
     };
-    if (r.tile == 16) return direct(gemm_fp8_direct_k<FA, FB, T, 1, 1>);
-    if (r.tile == 32) return direct(gemm_fp8_direct_k<FA, FB, T, 2, 2>);
+    // eight wavefronts where each has two blocks or more: 4 x 32000 x 4096 27.6 -> 25.4 us, 1 x 50256 x 768 8.6 -> 13
+    if (r.tile == 16 && p.K > 15 * F8_BLOCK) return direct(gemm_fp8_direct_k<FA, FB, T, 1, 1, 8>, 8);
+    if (r.tile == 16) return direct(gemm_fp8_direct_k<FA, FB, T, 1, 1, 4>, 4);
+    if (r.tile == 32) return direct(gemm_fp8_direct_k<FA, FB, T, 2, 2, 4>, 4);
     const dim3 grid((unsigned)(((int64_t)tiles_m * tiles_n + 7) / 8 * 8), (unsigned)r.splits);
     auto go = [&](auto kernel, uint32_t lds) { kernel<<<grid, 256, lds, s>>>(A, B, bias, resid, p.ldr, (T *)p.C, p.ldc, p.M, p.N, p.K, tiles_m, tiles_n, (float *)p.work); };
     if constexpr (sizeof(T) == 2) {

@@ -462,7 +462,8 @@ int tio_op_act_ckpt8_bwd(void *stream, int32_t dtype, int32_t act, int64_t rows,
 /* ---- a decoder layer trained in 8-bit floating point: single operators on caller-provided device buffers --------------------
  * They are asynchronous on `stream`, allocate nothing, keep nothing between calls, and may be captured into a graph.  Matrices are rows of
  * ld elements, a multiple of 8 and at least the columns rounded up to 8; the columns up to there are not used where a matrix is read, and get
- * zeros where one is written.  Device pointers, 16-byte aligned; buffers do not overlap but where said.
+ * zeros where one is written.  Vectors (biases, gains, a gate of one row, and their gradients) end with the last column: nothing behind it is read or
+ * written.  Device pointers, 16-byte aligned; buffers do not overlap but where one may be another, which then has the same stride.
  *
  * Matrices stored in 8 bits.  Blocks of 128 neighbours of a row (tiles = 1: of 128 x 128 elements) share a power of two: with a the block's
  * largest magnitude and M = 448 (e4m3) or 57344 (e5m2), e = max(the smallest e with a <= M 2^e, -110); an element x becomes the

@@ -65,7 +65,7 @@ template <typename T> __device__ __forceinline__ float element(const T *p) { ret
 // A workgroup's tile of 16 TM x 16 TN results: its NW wavefronts share the contraction, their sums are added in order.
 template <int FA, int FB, typename T, int TM, int TN, int NW>
 __global__ void __launch_bounds__(NW * 64) gemm_fp8_direct_k(const uint8_t *__restrict__ A, const uint8_t *__restrict__ B, const T *__restrict__ bias,
-                                                         const T *__restrict__ resid, int64_t ldr, T *__restrict__ C, int64_t ldc, int64_t M, int64_t N,
+                                                         const T *resid, int64_t ldr, T *C, int64_t ldc, int64_t M, int64_t N,
                                                          int64_t K, int tiles_n) {
     __shared__ float sums[NW][TM * TN][256];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;

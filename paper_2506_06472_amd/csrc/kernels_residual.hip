@@ -93,10 +93,20 @@ template <typename T, int W, bool RMS, bool POST> struct Columns {
         v.get(f);
         if (ragged) cut8(f, n);
     }
+    // of a vector, which ends with the last column
     __device__ __forceinline__ void load(float (&f)[8], const void *base) const {
-        Row8<T> v;
-        row_load(v, row(base, 0), col);
-        get(f, v);
+        const T *const from = (const T *)base + col;
+        if (n == 8) {
+            Row8<T> v;
+            v.load(from);
+            v.get(f);
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+            if (j < n) f[j] = to_f32(from[j]);
     }
     __device__ __forceinline__ void put(void *base, int64_t at, float (&f)[8]) const {
         if (ragged) cut8(f, n);
@@ -223,10 +233,17 @@ __global__ void __launch_bounds__(W == 1 ? 256 : W * 64, 4) residual_norm_bwd_k(
     const uint32_t groups = (uint32_t)((a.d + 7) / 8);
     const float inv_d = 1.0f / (float)a.d;
     const bool sum1 = POST || (a.gate && !a.ldg);
-    const float factor = a.branch_scale * (a.drop.limit ? a.drop.scale : 1.f);
     float s_gain[8], s_bias[8], s1[8], s2[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) s_gain[j] = s_bias[j] = s1[j] = s2[j] = 0.f;
+    // with a gate for every row, what the layer norm's bias adds to its gradient: a thread's own, in LDS for want of registers
+    constexpr bool MOVED = POST && !RMS;
+    constexpr int THREADS = W == 1 ? 256 : W * 64;
+    __shared__ float4 moved[MOVED ? 2 : 1][MOVED ? THREADS : 1];
+    if (MOVED) {
+        moved[0][threadIdx.x] = make_float4(col.c[0], col.c[1], col.c[2], col.c[3]);
+        moved[MOVED][threadIdx.x] = make_float4(col.c[4], col.c[5], col.c[6], col.c[7]);
+    }
     const int team = W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
     const int64_t stride = (int64_t)gridDim.x * teams_of(W);
     int64_t row = (int64_t)blockIdx.x * teams_of(W) + team;
@@ -297,12 +314,15 @@ __global__ void __launch_bounds__(W == 1 ? 256 : W * 64, 4) residual_norm_bwd_k(
             else if (a.drop.limit) v[j] = m.kept(j, a.drop) ? v[j] : 0.f;            // not a number, perhaps
         }
         if (gate) {
-            float c[8];
-            if (POST && !RMS && a.post_bias) col.load(c, a.post_bias);
             col.get(g, raw[4]);
+            float4 c[2];
+            if (MOVED) {
+                c[0] = moved[0][threadIdx.x];
+                c[1] = moved[MOVED][threadIdx.x];
+            }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                r[j] = D[j] * (v[j] * col.w[j] + (POST && !RMS && a.post_bias ? c[j] * factor : 0.f));
+                r[j] = D[j] * (v[j] * col.w[j] + (MOVED ? reinterpret_cast<const float *>(&c[j >> 2])[j & 3] : 0.f));
                 D[j] *= g[j];
             }
             col.put(a.dgate, row * a.ldg, r);
@@ -375,12 +395,11 @@ template <typename T> __global__ void __launch_bounds__(256 * KINDS) residual_su
     }
     __syncthreads();
     const int64_t at = (int64_t)blockIdx.x * 16 + threadIdx.x;
-    if (threadIdx.x >= 16 || at >= d8) return;
-    const bool there = at < a.d;
+    if (threadIdx.x >= 16 || at >= a.d) return;
     const float factor = a.branch_scale * (a.drop.limit ? a.drop.scale : 1.f);
-    auto value = [&](const void *p) __attribute__((always_inline)) { return there && p ? to_f32(((const T *)p)[at]) : 0.f; };
+    auto value = [&](const void *p) __attribute__((always_inline)) { return p ? to_f32(((const T *)p)[at]) : 0.f; };
     auto out = [&](void *p, float f) __attribute__((always_inline)) {
-        if (p) ((T *)p)[at] = from_f32<T>(there ? f : 0.f);
+        if (p) ((T *)p)[at] = from_f32<T>(f);
     };
     out(a.dgain, sums[0][threadIdx.x]);
     if (!a.rms) out(a.dbias, sums[2][threadIdx.x]);

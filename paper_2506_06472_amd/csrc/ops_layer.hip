@@ -15,6 +15,10 @@ namespace {
 
 bool known_form(int32_t form) { return form == TIO_FP8_E4M3 || form == TIO_FP8_E5M2; }
 
+// is one buffer handed in as two matrices whose rows are at different places?
+bool crossed(const void *x, int64_t ldx, const void *y, int64_t ldy, int64_t rows) { return x == y && ldx != ldy && rows > 1; }
+const char *const CROSSED = "a buffer that is read and written must have one stride";
+
 // what is wrong with a stored matrix's sizes, or nullptr
 const char *fp8_args(int64_t rows, int64_t cols) {
     if (rows < 1 || cols < 1) return "non-positive dimension";
@@ -112,6 +116,7 @@ int tio_op_gemm_fp8(void *stream, int32_t dtype, int64_t M, int64_t N, int64_t K
     if (const char *wrong = fp8_args(N, K)) return fail(TIO_ERR_INVALID_ARG, wrong);
     if (!stride_ok(ldc, N) || (resid && !stride_ok(ldr, N))) return fail(TIO_ERR_INVALID_ARG, BAD_STRIDE);
     if (!aligned(A) || !aligned(B) || !aligned(bias) || !aligned(resid) || !aligned(C) || !aligned(work)) return fail(TIO_ERR_INVALID_ARG, BAD_POINTER);
+    if (crossed(resid, ldr, C, ldc, M)) return fail(TIO_ERR_INVALID_ARG, CROSSED);
     if (!work && k::gemm_fp8_work(M, N, K)) return fail(TIO_ERR_INVALID_ARG, "this product needs work memory");
     const OnDeviceOf device((hipStream_t)stream);
     k::gemm_fp8((hipStream_t)stream, dtype, k::Fp8Product{M, N, K, form_a, A, form_b, B, bias, resid, ldr, C, ldc, work});
@@ -189,6 +194,7 @@ int tio_op_dropout(void *stream, int32_t dtype, int64_t rows, int64_t cols, cons
     if (!k::dropout_fits(rows, cols)) return fail(TIO_ERR_INVALID_ARG, "rows times columns (in eights) must be below 2^31");
     if (!stride_ok(ldx, cols) || !stride_ok(ldy, cols) || (resid && !stride_ok(ldr, cols))) return fail(TIO_ERR_INVALID_ARG, BAD_STRIDE);
     if (!aligned(x) || !aligned(resid) || !aligned(y)) return fail(TIO_ERR_INVALID_ARG, BAD_POINTER);
+    if (crossed(x, ldx, y, ldy, rows) || crossed(resid, ldr, y, ldy, rows)) return fail(TIO_ERR_INVALID_ARG, CROSSED);
     k::Dropout d;
     if (!make_dropout(p, seed, offset, d)) return fail(TIO_ERR_INVALID_ARG, BAD_PROBABILITY);
     const OnDeviceOf device((hipStream_t)stream);
@@ -207,13 +213,14 @@ int tio_op_rope_axes(void *stream, int32_t dtype, int64_t rows, int64_t heads, i
     if (n_axes < 1 || n_axes > 8) return fail(TIO_ERR_INVALID_ARG, "1 to 8 axes");
     int64_t pairs = 0;
     for (int i = 0; i < n_axes; ++i) {
-        if (sections[i] < 1 || sections[i] > k::ROPE_PAIRS) return fail(TIO_ERR_INVALID_ARG, "every axis has at least one pair");
+        if (sections[i] < 1 || sections[i] > k::ROPE_PAIRS) return fail(TIO_ERR_INVALID_ARG, "every axis has 1 to 128 pairs");
         pairs += sections[i];
     }
     if (pairs > dh / 2) return fail(TIO_ERR_INVALID_ARG, "the axes have more pairs than a head");
     if (!(theta > 0.f) || !std::isfinite(theta)) return fail(TIO_ERR_INVALID_ARG, "theta must be positive");
     if (!stride_ok(ldx, heads * dh) || !stride_ok(ldy, heads * dh)) return fail(TIO_ERR_INVALID_ARG, BAD_STRIDE);
     if (!aligned(x) || !aligned(y) || !aligned(positions, 4)) return fail(TIO_ERR_INVALID_ARG, BAD_POINTER);
+    if (crossed(x, ldx, y, ldy, rows)) return fail(TIO_ERR_INVALID_ARG, CROSSED);
     const OnDeviceOf device((hipStream_t)stream);
     k::rope_axes((hipStream_t)stream, dtype, rows, (int)heads, (int)dh, x, ldx, y, ldy, positions, n_axes, sections, theta, own_ladder != 0, inverse != 0);
     return launched();

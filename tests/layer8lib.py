@@ -36,6 +36,12 @@ def clean(t, cols, fill, rows=None):
     return t[:n, :cols].double().cpu().numpy()
 
 
+def untouched(t, cols, fill):
+    """a vector [1, ..]: everything behind the last column holds `fill`; the values as float64"""
+    assert (t[:, cols:] == fill).all()
+    return t[:, :cols].double().cpu().numpy()
+
+
 def stored(x, form, tiles=False):
     """The values that a stored matrix [rows, cols] stands for, in blocks along the columns."""
     rows, cols = x.shape

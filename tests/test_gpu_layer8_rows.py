@@ -107,7 +107,8 @@ class _Case:
                                          stats.data_ptr(), P("dy"), P("dh"), G("dx"), G("dbranch"), G("dgate"), G("dpost_gain"), G("dpost_bias"), G("dgain"),
                                          G("dbias"), work.data_ptr())
             assert (work[-64:] == 255).all()
-        return {n: l8.clean(v, d, 7.0) for n, v in self.raw.items()}
+        vector = lambda n: "gain" in n or "bias" in n or (n == "dgate" and not ldg)
+        return {n: (l8.untouched if vector(n) else l8.clean)(v, d, 7.0) for n, v in self.raw.items()}
 
     def want(self, y_rounded):
         """{name: (value, bound of the error without the result's rounding)}.  Arithmetic in 32 bits: c roundings of the magnitudes that meet in a sum, c = 64 for
@@ -298,6 +299,90 @@ def test_residual_norm_in_a_graph():
             assert torch.equal(got[n], out[n]), n
 
 
+def test_residual_norm_rows_past_4_gib():
+    """Rows whose places need more than 32 bits, all matrices side by side in one buffer: the bits of rows one behind the other."""
+    import torch
+    import paper_2506_06472_amd as tio
+    rows, d, far = 5, 72, 1 << 29
+    c = _Case(rows, d, "bf16", False, True, "rows", 0.3)
+    c.run()
+    flat = torch.full(((rows - 1) * far + 16 * 128,), 7.0, device="cuda", dtype=torch.bfloat16)
+    place = {n: flat.as_strided((rows, d), (far, 1), 128 * i) for i, n in enumerate(("branch", "x", "gate", "y", "h", "dy", "dh", "dx", "dbranch", "dgate"))}
+    for n in ("branch", "x", "gate", "dy", "dh"):
+        place[n].copy_(c.t[n][:, :d])
+    one = {n: torch.full_like(c.t["gain"], 7.0) for n in ("dpost_gain", "dpost_bias", "dgain", "dbias")}
+    stats, work = torch.empty((rows, 4), device="cuda"), torch.empty(tio.tio_op_residual_norm_bwd_work(rows, d), device="cuda", dtype=torch.uint8)
+    P = lambda n: (place.get(n) if n in place else one[n] if n in one else c.t[n]).data_ptr()
+    cfg = tio.tio_residual_cfg(False, c.eps, c.rs, c.bs, c.p, c.seed, c.offset)
+    tio.tio_op_residual_norm(0, "bf16", cfg, rows, d, far, P("branch"), P("x"), P("gate"), far, P("post_gain"), P("post_bias"), P("gain"), P("bias"), P("y"), P("h"),
+                             stats.data_ptr())
+    tio.tio_op_residual_norm_bwd(0, "bf16", cfg, rows, d, far, P("branch"), P("y"), P("gate"), far, P("post_gain"), P("post_bias"), P("gain"), stats.data_ptr(),
+                                 P("dy"), P("dh"), P("dx"), P("dbranch"), P("dgate"), P("dpost_gain"), P("dpost_bias"), P("dgain"), P("dbias"), work.data_ptr())
+    for n in ("y", "h", "dx", "dbranch", "dgate"):
+        assert torch.equal(place[n], c.raw[n][:, :d]), n
+    for n, v in one.items():
+        assert torch.equal(v, c.raw[n]), n
+
+
+def test_two_backward_passes_at_once():
+    """On two streams, each with a work memory of its own: the bits of one after the other."""
+    import torch
+    import paper_2506_06472_amd as tio
+    cases = [_Case(700, 264, "fp32", True, True, "shared", 0.1, seed=i) for i in range(2)]
+    want = [c.run() for c in cases]
+    streams, outs, keep = [torch.cuda.Stream(), torch.cuda.Stream()], [], []
+    for c in cases:
+        cfg = tio.tio_residual_cfg(True, c.eps, c.rs, c.bs, c.p, c.seed, c.offset)
+        o = {n: torch.full_like(v, 7.0) for n, v in c.raw.items()}
+        outs.append(o)
+        keep.append((cfg, torch.empty((700, 4), device="cuda"), torch.empty(tio.tio_op_residual_norm_bwd_work(700, 264), device="cuda", dtype=torch.uint8)))
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for c, o, (cfg, stats, work), s in zip(cases, outs, keep, streams):
+            t, ld, P, G = c.t, c.t["x"].stride(0), lambda n: c.t[n].data_ptr(), lambda n: o[n].data_ptr()
+            tio.tio_op_residual_norm(s.cuda_stream, "fp32", cfg, 700, 264, ld, P("branch"), P("x"), P("gate"), 0, P("post_gain"), 0, P("gain"), 0, G("y"), G("h"),
+                                     stats.data_ptr())
+            tio.tio_op_residual_norm_bwd(s.cuda_stream, "fp32", cfg, 700, 264, ld, P("branch"), G("y"), P("gate"), 0, P("post_gain"), 0, P("gain"), stats.data_ptr(),
+                                         P("dy"), P("dh"), G("dx"), G("dbranch"), G("dgate"), G("dpost_gain"), 0, G("dgain"), 0, work.data_ptr())
+    torch.cuda.synchronize()
+    for w, o in zip(want, outs):
+        for n, v in o.items():
+            assert np.array_equal(v[:, :264].double().cpu().numpy(), w[n]), n
+
+
+def test_dropout_and_rope_in_a_graph_and_on_another_stream():
+    """Captured once and replayed on other values and positions, with eager work between: the bits of eager calls."""
+    import torch
+    import paper_2506_06472_amd as tio
+    rows, heads, dh = 300, 5, 64
+    x = torch.zeros((rows, heads * dh), device="cuda", dtype=torch.bfloat16)
+    y, z = torch.zeros_like(x), torch.zeros_like(x)
+    pos = torch.zeros((rows, 2), device="cuda", dtype=torch.int32)
+
+    def calls():
+        s = torch.cuda.current_stream().cuda_stream
+        tio.tio_op_dropout(s, "bf16", rows, heads * dh, x.data_ptr(), heads * dh, x.data_ptr(), heads * dh, y.data_ptr(), heads * dh, 0.25, 9, 10)
+        tio.tio_op_rope_axes(s, "bf16", rows, heads, dh, y.data_ptr(), heads * dh, z.data_ptr(), heads * dh, pos.data_ptr(), [20, 12], 10000.0)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    side = torch.cuda.Stream()
+    for i in range(4):
+        x.copy_(torch.randn((rows, heads * dh), device="cuda") * (i + 1))
+        pos.copy_(torch.randint(0, 1000, (rows, 2), device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = z.clone()
+        y.zero_()
+        z.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            calls()
+        torch.cuda.synchronize()
+        assert torch.equal(got, z) and z.abs().sum() > 0
+
+
 # ------------------------------------------------------------------ rotary positions
 def _turned(x, pos, heads, dh, sections, theta, own, inverse):
     """value, and the angles' magnitudes and the pairs' that the bound needs"""
@@ -355,3 +440,17 @@ def test_rope_of_one_axis_is_the_steps_rotation():
     for k in range(T):
         diagonal = np.diagonal(s, k)
         assert np.abs(diagonal - diagonal[0]).max() <= 64 * l8.E32 * scale
+
+
+def test_rope_rows_past_4_gib():
+    import torch
+    import paper_2506_06472_amd as tio
+    rows, far = 5, 1 << 29
+    flat = torch.full(((rows - 1) * far + 256,), 7.0, device="cuda", dtype=torch.bfloat16)
+    x = torch.randn((rows, 128), device="cuda").to(torch.bfloat16)
+    pos = torch.randint(0, 1 << 20, (rows, 1), device="cuda", dtype=torch.int32)
+    wide, y = flat.as_strided((rows, 128), (far, 1)), torch.empty_like(x)
+    wide.copy_(x)
+    tio.tio_op_rope_axes(0, "bf16", rows, 2, 64, x.data_ptr(), 128, y.data_ptr(), 128, pos.data_ptr(), [32], 10000.0)
+    tio.tio_op_rope_axes(0, "bf16", rows, 2, 64, flat.data_ptr(), far, flat.data_ptr(), far, pos.data_ptr(), [32], 10000.0)
+    assert torch.equal(wide, y) and (flat[128:256] == 7.0).all()

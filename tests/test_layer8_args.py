@@ -71,6 +71,15 @@ def test_product_refused():
     product(resid=Q, ldr=24)
     product(bias=Q)
     product(work=Q)
+    product(resid=P, ldr=32)                                    # in place, with another stride
+    for M, N, K in ((0, 8, 8), (8, 0, 8), (8, 8, 0), ((1 << 22) + 1, 8, 8), (8, (1 << 22) + 1, 8), (8, 8, (1 << 22) + 1), (1 << 22, 8, 1 << 22)):
+        _refused(tio.tio_op_gemm_fp8_route, "bf16", M, N, K)
+
+
+def test_product_without_the_work_it_needs_refused():
+    M, N, K = 768, 768, 8000
+    assert tio.tio_op_gemm_fp8_work(M, N, K) >= M * N * 8 and tio.tio_op_gemm_fp8_work(4, 1000, 1000) == 0
+    _refused(tio.tio_op_gemm_fp8, 0, "bf16", M, N, K, "e4m3", P, "e4m3", P, P, N, 0, 0, 0, 0)
 
 
 @pytest.mark.parametrize("p", [-0.1, 1.0, 1.5, float("nan"), float("inf"), 65535.6 / 65536])
@@ -94,6 +103,8 @@ def test_dropout_refused():
     drop(resid=P, ldr=16)
     drop(ldx=20)
     drop(ldy=16)
+    drop(ldx=32)                                                # in place, with another stride
+    drop(x=2 * P, resid=P, ldr=32)
     assert tio.binding.lib().tio_op_dropout(0, 2, 4, 20, P, 24, 0, 0, P, 24, 0.1, 1, 2) == -1
 
 
@@ -148,7 +159,7 @@ def test_rope_refused():
     for kw in (dict(rows=0), dict(rows=1 << 31), dict(heads=0), dict(heads=65537, ldx=1 << 22, ldy=1 << 22), dict(dh=0), dict(dh=12), dict(dh=264, ldx=528, ldy=528),
                dict(x=0), dict(y=0), dict(pos=0), dict(x=Q), dict(y=Q), dict(pos=P + 2), dict(sections=()), dict(sections=(8, 0)), dict(sections=(8, -1)),
                dict(sections=(8, 9)), dict(sections=(1,) * 9), dict(sections=(2147483647,)), dict(theta=0.0), dict(theta=-1.0),
-               dict(theta=float("nan")), dict(theta=float("inf")), dict(ldx=56), dict(ldy=60)):
+               dict(theta=float("nan")), dict(theta=float("inf")), dict(ldx=56), dict(ldy=60), dict(ldy=72)):
         rope(**kw)
 
 

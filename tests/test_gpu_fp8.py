@@ -267,3 +267,96 @@ def test_calls_in_a_graph_and_on_another_stream():
         calls()
         torch.cuda.synchronize()
         assert torch.equal(got, y) and y.abs().sum() > 0
+
+
+def test_rows_past_4_gib():
+    """Matrices whose rows lie past 4 GiB of their buffer have the bits of rows side by side."""
+    import torch
+    import paper_2506_06472_amd as tio
+    R, C, far = 40, 200, 1 << 26
+    flat = torch.full(((R - 1) * far + C + 8,), 7.0, device="cuda", dtype=torch.bfloat16)
+    wide = flat.as_strided((R, C), (far, 1))
+    x = torch.randn((R, C), device="cuda").to(torch.bfloat16)
+    wide.copy_(x)
+    q = torch.zeros((4, max(tio.tio_fp8_bytes(R, C), tio.tio_fp8_bytes(C, R))), device="cuda", dtype=torch.uint8)
+    for i, (v, ld) in enumerate(((x, C), (wide, far))):
+        tio.tio_op_fp8_store(0, "bf16", "e4m3", False, R, C, v.data_ptr(), ld, q[2 * i].data_ptr(), q[2 * i + 1].data_ptr())
+    assert torch.equal(q[:2], q[2:])
+    near = torch.empty_like(x)
+    tio.tio_op_fp8_load(0, "bf16", "e4m3", R, C, q[0].data_ptr(), near.data_ptr(), C)
+    tio.tio_op_fp8_load(0, "bf16", "e4m3", R, C, q[0].data_ptr(), flat.data_ptr(), far)
+    assert torch.equal(wide, near)
+    for M, N, tile in ((40, 200, 16), (1000, 600, 32), (2000, 2000, 128), (4000, 4104, 256)):
+        assert tio.tio_op_gemm_fp8_route("bf16", M, N, 1000)[0] == tile
+        a, b = torch.randn((M, 1000), device="cuda"), torch.randn((N, 1000), device="cuda")
+        s = [torch.zeros(tio.tio_fp8_bytes(len(v), 1000), device="cuda", dtype=torch.uint8) for v in (a, b)]
+        for v, to in zip((a, b), s):
+            tio.tio_op_fp8_store(0, "fp32", "e4m3", False, len(v), 1000, v.data_ptr(), 1000, to.data_ptr())
+        work = torch.empty(tio.tio_op_gemm_fp8_work(M, N, 1000) + 16, device="cuda", dtype=torch.uint8)
+        ld = flat.numel() // M // 8 * 8
+        big = torch.as_strided(flat, (M, N), (ld, 1))
+        near = torch.empty((M, N), device="cuda", dtype=torch.bfloat16)
+        big.copy_(torch.randn((M, N), device="cuda"))
+        resid = big.clone()
+        for c, c_ld, r, r_ld in ((near, N, resid, N), (big, ld, big, ld)):
+            tio.tio_op_gemm_fp8(0, "bf16", M, N, 1000, "e4m3", s[0].data_ptr(), "e4m3", s[1].data_ptr(), c.data_ptr(), c_ld, 0, r.data_ptr(), r_ld, work.data_ptr())
+        assert torch.equal(big, near) and not torch.equal(near, resid)
+
+
+def test_stored_matrix_past_4_gib():
+    """Codes behind the first 4 GiB: values read back, and products of them, of whole numbers, which are exact."""
+    import torch
+    import paper_2506_06472_amd as tio
+    R, C, N = (1 << 17) + 17, 1 << 15, 264
+    x = torch.randint(-8, 9, (R, C), device="cuda", dtype=torch.bfloat16)
+    q = torch.empty(tio.tio_fp8_bytes(R, C), device="cuda", dtype=torch.uint8)
+    tio.tio_op_fp8_store(0, "bf16", "e4m3", False, R, C, x.data_ptr(), C, q.data_ptr())
+    back = torch.empty_like(x)
+    tio.tio_op_fp8_load(0, "bf16", "e4m3", R, C, q.data_ptr(), back.data_ptr(), C)
+    assert q.numel() > 1 << 32 and torch.equal(back, x)
+    del back
+    w = torch.randint(-8, 9, (N, C), device="cuda", dtype=torch.bfloat16)
+    wq = torch.empty(tio.tio_fp8_bytes(N, C), device="cuda", dtype=torch.uint8)
+    tio.tio_op_fp8_store(0, "bf16", "e4m3", False, N, C, w.data_ptr(), C, wq.data_ptr())
+    work = torch.empty(tio.tio_op_gemm_fp8_work(R, N, C) + 16, device="cuda", dtype=torch.uint8)
+    for dtype in ("fp32", "bf16"):
+        y = torch.empty((R, N), device="cuda", dtype=l8.types(dtype))
+        tio.tio_op_gemm_fp8(0, dtype, R, N, C, "e4m3", q.data_ptr(), "e4m3", wq.data_ptr(), y.data_ptr(), N, work_ptr=work.data_ptr())
+        for at in (0, 1 << 16, R - 500):
+            assert torch.equal(y[at:at + 500], (x[at:at + 500].float() @ w.float().t()).to(y.dtype))
+    del y, q, work, wq
+    xt = torch.empty(tio.tio_fp8_bytes(C, R), device="cuda", dtype=torch.uint8)
+    even = x // 2 * 2                                           # up to 8: two bits
+    tio.tio_op_fp8_store(0, "bf16", "e5m2", True, R, C, even.data_ptr(), C, 0, xt.data_ptr())
+    back = torch.empty((C, (R + 7) // 8 * 8), device="cuda", dtype=torch.bfloat16)
+    tio.tio_op_fp8_load(0, "bf16", "e5m2", C, R, xt.data_ptr(), back.data_ptr(), back.stride(0))
+    for at in (0, C // 2, C - 300):
+        assert torch.equal(back[at:at + 300, :R], even[:, at:at + 300].t()) and (back[at:at + 300, R:] == 0).all()
+
+
+def test_two_products_at_once():
+    """On two streams, each with a work memory of its own: the bits of one after the other."""
+    import torch
+    import paper_2506_06472_amd as tio
+    M, N, K = 768, 768, 8000
+    assert tio.tio_op_gemm_fp8_route("bf16", M, N, K)[2] > 1
+    q = []
+    for i in range(4):
+        v = torch.randn((M, K), device="cuda")
+        q.append(torch.empty(tio.tio_fp8_bytes(M, K), device="cuda", dtype=torch.uint8))
+        tio.tio_op_fp8_store(0, "fp32", "e4m3", False, M, K, v.data_ptr(), K, q[-1].data_ptr())
+    work = [torch.empty(tio.tio_op_gemm_fp8_work(M, N, K), device="cuda", dtype=torch.uint8) for _ in range(2)]
+    y = torch.zeros((2, 2, M, N), device="cuda", dtype=torch.bfloat16)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+
+    def call(i, out, stream):
+        tio.tio_op_gemm_fp8(stream, "bf16", M, N, K, "e4m3", q[2 * i].data_ptr(), "e4m3", q[2 * i + 1].data_ptr(), out.data_ptr(), N, work_ptr=work[i].data_ptr())
+    for _ in range(8):
+        for i in range(2):
+            call(i, y[0, i], streams[i].cuda_stream)
+    torch.cuda.synchronize()
+    for i in range(2):
+        call(i, y[1, i], 0)
+    torch.cuda.synchronize()
+    assert torch.equal(y[0], y[1]) and not torch.equal(y[0, 0], y[0, 1])

@@ -10,7 +10,8 @@
 // factor more); and with m = kept ? D : 0 the gradients of gate, post_gain and post_bias are a column's factors of the same two sums over the rows,
 //   S1 = sum of m bh,  S2 = sum of m:   dpost_gain = bs s gate S1,  dpost_bias = bs s gate S2,  dgate = bs s (post_gain S1 + post_bias S2).
 //
-// Bound: HBM; the vector ALU, with about 14 (forward) and 24 operations on an element beside the generator's, is not far behind.  A row is W
+// Bound: HBM; the vector ALU, with about 14 (forward) and 24 operations on an element beside the generator's, is not far behind (8192 x 4096 in bf16: forward
+// 51 us, 5.3 TB/s; backward 70, 5.8, and the sums 8).  A row is W
 // wavefronts', who hold it in registers from its loads to its stores; statistics and sums are in 32 bits, the layer norm's variance from centred values.  A
 // workgroup takes rows one after the other and keeps its share of the column sums in registers; a second launch adds the workgroups' shares in their
 // order, so that results do not depend on timing.

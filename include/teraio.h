@@ -487,9 +487,9 @@ int tio_op_fp8_load(void *stream, int32_t dtype, int32_t form, int64_t rows, int
 int tio_op_gemm_fp8_work(int64_t M, int64_t N, int64_t K, uint64_t *out_bytes);
 int tio_op_gemm_fp8(void *stream, int32_t dtype, int64_t M, int64_t N, int64_t K, int32_t form_a, const void *A, int32_t form_b, const void *B, const void *bias,
                     const void *resid, int64_t ldr, void *C, int64_t ldc, void *work);
-/* Measuring aid, host only: how such a product is taken: in tiles of 16, 32, 128 or 256 rows and columns, with so many steps of its contraction on
- * their way (1: from the caches, without LDS), the contraction cut into so many ranges. */
-int tio_op_gemm_fp8_route(int32_t dtype, int64_t M, int64_t N, int64_t K, int32_t *out_tile, int32_t *out_deep, int32_t *out_ranges);
+/* Measuring aid, host only: how such a product is taken: in tiles of so many rows and columns, with so many steps of its contraction on their way (1: from the
+ * caches), the contraction cut into so many ranges (from the caches: shares of a workgroup's wavefronts). */
+int tio_op_gemm_fp8_route(int32_t dtype, int64_t M, int64_t N, int64_t K, int32_t *out_rows, int32_t *out_cols, int32_t *out_deep, int32_t *out_ranges);
 
 /* Dropout from a counter.  The 16 bits of element (row, col) are half-word col % 8 (low halves first) of the four words that Philox-4x32 with
  * ten rounds gives for the counter (row ceil(cols / 8) + col / 8, offset), two words each, under the key `seed`.  With T = p 65536

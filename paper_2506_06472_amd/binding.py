@@ -632,8 +632,8 @@ def tio_op_gemm_fp8(stream_handle, dtype, M, N, K, form_a, A_ptr, form_b, B_ptr,
 
 
 def tio_op_gemm_fp8_route(dtype, M, N, K):
-    """(tile, steps on their way, ranges of the contraction) of a product of stored matrices; host only."""
-    out = [C.c_int32() for _ in range(3)]
+    """(rows and columns of a tile, steps on their way, ranges of the contraction) of a product of stored matrices; host only."""
+    out = [C.c_int32() for _ in range(4)]
     _check(lib().tio_op_gemm_fp8_route(PREC[dtype], C.c_int64(M), C.c_int64(N), C.c_int64(K), *[C.byref(v) for v in out]))
     return tuple(v.value for v in out)
 

@@ -149,7 +149,7 @@ struct Fp8Product {
 };
 int64_t gemm_fp8_work(int64_t M, int64_t N, int64_t K);
 // how it is taken: tiles of that size, steps in LDS, ranges of the contraction; host only
-void gemm_fp8_route(int dtype, int64_t M, int64_t N, int64_t K, int *tile, int *deep, int *ranges);
+void gemm_fp8_route(int dtype, int64_t M, int64_t N, int64_t K, int *rows, int *cols, int *deep, int *ranges);
 void gemm_fp8(hipStream_t s, int dtype, const Fp8Product &p);
 // a mask from a counter (philox.h)
 struct Dropout {

@@ -62,7 +62,7 @@ template <int FA, int FB> __device__ __forceinline__ floatx4 product16(const Pie
 
 template <typename T> __device__ __forceinline__ float element(const T *p) { return to_f32(*p); }
 
-// A workgroup's tile of 16 TM x 16 TN results: its NW wavefronts share the contraction, their sums are added in order.
+// A workgroup's tile of 16 TM x 16 TN results, for products of few rows or few tiles: its NW wavefronts share the contraction, their sums are added in order.
 template <int FA, int FB, typename T, int TM, int TN, int NW>
 __global__ void __launch_bounds__(NW * 64) gemm_fp8_direct_k(const uint8_t *__restrict__ A, const uint8_t *__restrict__ B, const T *__restrict__ bias,
                                                          const T *resid, int64_t ldr, T *C, int64_t ldc, int64_t M, int64_t N,
@@ -91,8 +91,8 @@ __global__ void __launch_bounds__(NW * 64) gemm_fp8_direct_k(const uint8_t *__re
         eb[j] = B + sb.code_bytes() + (g >> 2) * KB * 64 + (g & 3);
     }
     // U blocks' loads before the first one's products: one after the other a wavefront waits for each (16 x 4096 x 11008, operands in no cache: 16.6 us, with
-    // eight wavefronts of four at once 11.2)
-    constexpr int U = NW == 8 ? 4 : TM == 2 ? 1 : 2;
+    // eight wavefronts of four at once 11.2); larger tiles have as many loads in one block
+    constexpr int U = TM * TN > 2 ? 1 : TM * TN == 2 ? (sizeof(T) == 2 ? 4 : 2) : NW == 8 ? 4 : 2;
     for (int64_t kb = wave; kb < KB; kb += NW * U) {
         Piece8 a[U][TM], b[U][TN];
 #pragma unroll
@@ -542,40 +542,48 @@ __global__ void __launch_bounds__(256, 2)
     store_part<float, TM, TN>(acc, smem8 + wave * stage_bytes<TN>(), lane, (int64_t)tm * L::BM + wm * 16 * TM, (int64_t)tn * L::BN + wn * 16 * TN, M, N, bias, resid, ldr, C, ldc, ws, split, nsplit);
 }
 
-// How a product is taken: tiles of 128 or 256 through LDS, `deep` steps at a time, the contraction cut into ranges, or tiles of 16 or 32 from the caches
-// (gemm_fp8_direct_k).
+// How a product is taken: tiles of 128 x 128 or 256 x 256 through LDS, `deep` steps at a time, the contraction cut into ranges, or (deep 1) smaller ones from the
+// caches, the contraction cut into the shares of four or eight wavefronts (gemm_fp8_direct_k).
 //
-// The least of an estimate of the time, whose constants were fitted to 39 products, each taken in all ways: a workgroup's steps and its beginning and end
-// (us), times the rounds of workgroups, and the sums of the ranges; of small tiles the chain of steps or the bytes from the caches.  A step of a 128 tile is
-// mostly waiting for loads where a compute unit has one such tile: 0.32 us four steps deep (0.44 where all units work), two deep 0.6, but two tiles to a
-// unit share 0.88.  us, 768 x 768 x 8192 in one range: 26.9 four deep, 41.4 two deep, 69.8 in 256 tiles, and 19.1 in three ranges; 8192 x 768 x 768: 13.3,
-// 10.8, 15.5; 8192 x 11008 x 4096: 377, 328, 285; 1000^3: 8.4 and 7.7, in tiles of 32 6.1; 500 x 500 x 3000: 11.9, 11.4 and 5.0.
+// The least of an estimate of the time.  The large tiles' constants were fitted to 39 products, each taken in all ways: a workgroup's steps and its beginning and
+// end (us), times the rounds of workgroups, and the sums of the ranges.  A step of a 128 tile is mostly waiting for loads where a compute unit has one
+// such tile: 0.32 us four steps deep (0.44 where all units work), two deep 0.6, but two tiles to a unit share 0.88.  us, 768 x 768 x 8192 in one range: 26.9 four
+// deep, 41.4 two deep, 69.8 in 256 tiles, and 19.1 in three ranges; 8192 x 768 x 768: 13.3, 10.8, 15.5; 8192 x 11008 x 4096: 377, 328, 285.  The small ones' were
+// fitted to 380 products with B in no cache, so that the choice is 1.5 % behind the best way on average (7 % with tiles of 16 x 16 and 32 x 32 by four wavefronts
+// alone): the larger of a wavefront's chain of steps, in rounds of workgroups, and the bytes from the caches.  us, bf16: 32 x 4096 x 11008: 18.4 in 32 x 32 by
+// four wavefronts, in 32 x 16 by eight 13.9, in 16 x 16 16.0; 64 x 4096 x 11008: 18.2 in 32 x 32 by four, by eight 16.4; 256 x 4096 x 4096: 21.7 in 128 x 128,
+// in 64 x 32 15.2, in 32 x 32 by eight 17.0; 1024 x 1000 x 1000: 8.2 in 128 x 128, 6.6 in 32 x 32 by four, by eight 7.2.
 struct Route {
-    int tile, deep, splits;
+    int rows, cols, deep, splits;                              // splits: ranges, or wavefronts that share a contraction
 };
 Route route(bool bf16, int64_t M, int64_t N, int64_t K) {
-    if (M <= 16) return {16, 1, 1};
     constexpr double UNITS = 256;                              // compute units
     const int64_t KB = (K + F8_BLOCK - 1) / F8_BLOCK;
+    // eight wavefronts where each has two blocks or more: 4 x 32000 x 4096 27.6 -> 25.4 us, 1 x 50256 x 768 8.6 -> 13
+    if (M <= 16) return {16, 16, 1, KB > 15 ? 8 : 4};
     Route best{};
     double least = 1e300;
-    auto tiles = [&](int tile) { return (double)((M + tile - 1) / tile) * ((N + tile - 1) / tile); };
+    auto tiles = [&](int rows, int cols) { return (double)((M + rows - 1) / rows) * ((N + cols - 1) / cols); };
     auto take = [&](double t, Route r) {
         if (t < least) least = t, best = r;
     };
-    auto small = [&](int tile, double step, double per_us, double each) {
-        const double groups = tiles(tile), chain = step * (double)((KB + 3) / 4) * std::ceil(groups * tile / 32768);
-        take(2.0 + std::max(chain, groups * KB * tile * 256 / per_us + groups * each), {tile, 1, 1});
+    auto small = [&](int rows, int cols, int waves, double step, int per_unit, double per_us, double each) {
+        const double groups = tiles(rows, cols), chain = step * (double)((KB + waves - 1) / waves) * std::ceil(groups / (UNITS * per_unit));
+        take(2.0 + std::max(chain, groups * KB * (rows + cols) * 128 / per_us + groups * each), {rows, cols, 1, waves});
     };
-    small(32, 0.36, 14e6, 0.0013);
-    small(16, 0.20, 16e6, 0.0001);
+    small(16, 16, 4, 0.17, 4, 17e6, 0.00016);
+    small(16, 16, 8, 0.30, 2, 22e6, 0.00093);
+    small(32, 16, 8, 0.42, 1, 20.5e6, 0.0014);
+    small(32, 32, 4, 0.58, 2, 18e6, 0.0006);
+    small(32, 32, 8, 0.80, 1, 18.5e6, 0.00106);
+    small(64, 32, 8, 1.13, 1, 18e6, 0.0046);
     auto large = [&](int tile, int deep, int most, int per_unit, double step, double busy, double ends) {
         for (int splits = 1; splits <= most && splits <= KB; ++splits) {
-            const double groups = tiles(tile) * splits, full = std::min(1.0, groups / UNITS);
+            const double groups = tiles(tile, tile) * splits, full = std::min(1.0, groups / UNITS);
             if (per_unit > 1 && groups <= UNITS) continue;
             double t = std::ceil(groups / (UNITS * per_unit)) * ((KB + splits - 1) / splits * (step + busy * full) + ends);
             if (splits > 1) t += 3.0 + (double)M * N * 8 * (splits + 0.5) / 3.5e6;
-            take(t, {tile, deep, splits});
+            take(t, {tile, tile, deep, splits});
         }
     };
     if (bf16) {
@@ -600,18 +608,29 @@ template <int FA, int FB, typename T> void launch(hipStream_t s, const Fp8Produc
     const Route r = route(sizeof(T) == 2, p.M, p.N, p.K);
     const T *const bias = (const T *)p.bias, *const resid = (const T *)p.resid;
     const uint8_t *const A = (const uint8_t *)p.A, *const B = (const uint8_t *)p.B;
-    const int tiles_m = (int)((p.M + r.tile - 1) / r.tile), tiles_n = (int)((p.N + r.tile - 1) / r.tile);
-    auto direct = [&](auto kernel, int waves) {
-        kernel<<<(unsigned)((int64_t)tiles_m * tiles_n), (unsigned)waves * 64, 0, s>>>(A, B, bias, resid, p.ldr, (T *)p.C, p.ldc, p.M, p.N, p.K, tiles_n);
-    };
-    // eight wavefronts where each has two blocks or more: 4 x 32000 x 4096 27.6 -> 25.4 us, 1 x 50256 x 768 8.6 -> 13
-    if (r.tile == 16 && p.K > 15 * F8_BLOCK) return direct(gemm_fp8_direct_k<FA, FB, T, 1, 1, 8>, 8);
-    if (r.tile == 16) return direct(gemm_fp8_direct_k<FA, FB, T, 1, 1, 4>, 4);
-    if (r.tile == 32) return direct(gemm_fp8_direct_k<FA, FB, T, 2, 2, 4>, 4);
+    const int tiles_m = (int)((p.M + r.rows - 1) / r.rows), tiles_n = (int)((p.N + r.cols - 1) / r.cols);
+    if (r.deep == 1) {
+        auto direct = [&](auto TM, auto TN, auto NW) {
+            if (r.rows != 16 * TM() || r.cols != 16 * TN() || r.splits != NW()) return;
+            gemm_fp8_direct_k<FA, FB, T, TM(), TN(), NW()><<<(unsigned)((int64_t)tiles_m * tiles_n), NW() * 64, 0, s>>>(A, B, bias, resid, p.ldr, (T *)p.C, p.ldc, p.M,
+                                                                                                                    p.N, p.K, tiles_n);
+        };
+        using One = std::integral_constant<int, 1>;
+        using Two = std::integral_constant<int, 2>;
+        using Four = std::integral_constant<int, 4>;
+        using Eight = std::integral_constant<int, 8>;
+        direct(One{}, One{}, Four{});
+        direct(One{}, One{}, Eight{});
+        direct(Two{}, One{}, Eight{});
+        direct(Two{}, Two{}, Four{});
+        direct(Two{}, Two{}, Eight{});
+        direct(Four{}, Two{}, Eight{});
+        return;
+    }
     const dim3 grid((unsigned)(((int64_t)tiles_m * tiles_n + 7) / 8 * 8), (unsigned)r.splits);
     auto go = [&](auto kernel, uint32_t lds) { kernel<<<grid, 256, lds, s>>>(A, B, bias, resid, p.ldr, (T *)p.C, p.ldc, p.M, p.N, p.K, tiles_m, tiles_n, (float *)p.work); };
     if constexpr (sizeof(T) == 2) {
-        if (r.tile == 256) allow_lds<gemm_fp8_tile_k<FA, FB, 8, 8, 2>, Loads<8, 8, 2>::LDS>(), go(gemm_fp8_tile_k<FA, FB, 8, 8, 2>, Loads<8, 8, 2>::LDS);
+        if (r.rows == 256) allow_lds<gemm_fp8_tile_k<FA, FB, 8, 8, 2>, Loads<8, 8, 2>::LDS>(), go(gemm_fp8_tile_k<FA, FB, 8, 8, 2>, Loads<8, 8, 2>::LDS);
         else if (r.deep == 4) allow_lds<gemm_fp8_tile_k<FA, FB, 4, 4, 4>, Loads<4, 4, 4>::LDS>(), go(gemm_fp8_tile_k<FA, FB, 4, 4, 4>, Loads<4, 4, 4>::LDS);
         else allow_lds<gemm_fp8_tile_k<FA, FB, 4, 4, 2>, Loads<4, 4, 2>::LDS>(), go(gemm_fp8_tile_k<FA, FB, 4, 4, 2>, Loads<4, 4, 2>::LDS);
     } else allow_lds<gemm_fp8_tile32_k<FA, FB>, Loads<4, 4, 2>::LDS>(), go(gemm_fp8_tile32_k<FA, FB>, Loads<4, 4, 2>::LDS);
@@ -622,13 +641,15 @@ template <int FA, int FB, typename T> void launch(hipStream_t s, const Fp8Produc
 }  // namespace
 
 int64_t gemm_fp8_work(int64_t M, int64_t N, int64_t K) {
-    const int a = route(true, M, N, K).splits, b = route(false, M, N, K).splits, most = a > b ? a : b;
+    const Route a = route(true, M, N, K), b = route(false, M, N, K);
+    const int most = std::max(a.deep > 1 ? a.splits : 1, b.deep > 1 ? b.splits : 1);
     return most > 1 ? most * M * ((N + 7) / 8 * 8) * 4 : 0;
 }
 
-void gemm_fp8_route(int dtype, int64_t M, int64_t N, int64_t K, int *tile, int *deep, int *ranges) {
+void gemm_fp8_route(int dtype, int64_t M, int64_t N, int64_t K, int *rows, int *cols, int *deep, int *ranges) {
     const Route r = route(dtype == TIO_PREC_BF16, M, N, K);
-    *tile = r.tile;
+    *rows = r.rows;
+    *cols = r.cols;
     *deep = r.deep;
     *ranges = r.splits;
 }

@@ -124,12 +124,13 @@ int tio_op_gemm_fp8(void *stream, int32_t dtype, int64_t M, int64_t N, int64_t K
     TIO_OP_END
 }
 
-int tio_op_gemm_fp8_route(int32_t dtype, int64_t M, int64_t N, int64_t K, int32_t *out_tile, int32_t *out_deep, int32_t *out_ranges) {
-    if (!out_tile || !out_deep || !out_ranges) return fail(TIO_ERR_INVALID_ARG, "null argument");
+int tio_op_gemm_fp8_route(int32_t dtype, int64_t M, int64_t N, int64_t K, int32_t *out_rows, int32_t *out_cols, int32_t *out_deep,
+                          int32_t *out_ranges) {
+    if (!out_rows || !out_cols || !out_deep || !out_ranges) return fail(TIO_ERR_INVALID_ARG, "null argument");
     if (!known_type(dtype)) return fail(TIO_ERR_INVALID_ARG, "unknown element type");
     if (const char *wrong = fp8_args(M, K)) return fail(TIO_ERR_INVALID_ARG, wrong);
     if (const char *wrong = fp8_args(N, K)) return fail(TIO_ERR_INVALID_ARG, wrong);
-    k::gemm_fp8_route(dtype, M, N, K, out_tile, out_deep, out_ranges);
+    k::gemm_fp8_route(dtype, M, N, K, out_rows, out_cols, out_deep, out_ranges);
     return TIO_OK;
 }
 

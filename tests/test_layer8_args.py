@@ -77,7 +77,7 @@ def test_product_refused():
 
 
 def test_product_without_the_work_it_needs_refused():
-    M, N, K = 768, 768, 8000
+    M, N, K = 768, 768, 16000
     assert tio.tio_op_gemm_fp8_work(M, N, K) >= M * N * 8 and tio.tio_op_gemm_fp8_work(4, 1000, 1000) == 0
     _refused(tio.tio_op_gemm_fp8, 0, "bf16", M, N, K, "e4m3", P, "e4m3", P, P, N, 0, 0, 0, 0)
 

@@ -14,7 +14,8 @@ ALL = itertools.product
 FORMS = {
     "fp8_store_k": [f"I{t}Li{form}ELb{tiles}ELb{both}E" for t, form, tiles, both in ALL(T, FLAGS, FLAGS, FLAGS)],
     "fp8_load_k": [f"I{t}Li{form}E" for t, form in ALL(T, FLAGS)],
-    "gemm_fp8_direct_k": [f"ILi{a}ELi{b}E{t}Li{n}ELi{n}ELi{w}E" for a, b, t, (n, w) in ALL(FLAGS, FLAGS, T, ((1, 4), (1, 8), (2, 4)))],
+    "gemm_fp8_direct_k": [f"ILi{a}ELi{b}E{t}Li{m}ELi{n}ELi{w}E"
+                          for a, b, t, (m, n, w) in ALL(FLAGS, FLAGS, T, ((1, 1, 4), (1, 1, 8), (2, 1, 8), (2, 2, 4), (2, 2, 8), (4, 2, 8)))],
     # forms; groups of 16 rows and columns to a wavefront, steps in LDS
     "gemm_fp8_tile_k": [f"ILi{a}ELi{b}ELi{n}ELi{n}ELi{d}E" for a, b, (n, d) in ALL(FLAGS, FLAGS, ((8, 2), (4, 4), (4, 2)))],
     "gemm_fp8_tile32_k": [f"ILi{a}ELi{b}E" for a, b in ALL(FLAGS, FLAGS)],

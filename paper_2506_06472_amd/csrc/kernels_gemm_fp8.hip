@@ -549,7 +549,7 @@ __global__ void __launch_bounds__(256, 2)
 // end (us), times the rounds of workgroups, and the sums of the ranges.  A step of a 128 tile is mostly waiting for loads where a compute unit has one
 // such tile: 0.32 us four steps deep (0.44 where all units work), two deep 0.6, but two tiles to a unit share 0.88.  us, 768 x 768 x 8192 in one range: 26.9 four
 // deep, 41.4 two deep, 69.8 in 256 tiles, and 19.1 in three ranges; 8192 x 768 x 768: 13.3, 10.8, 15.5; 8192 x 11008 x 4096: 377, 328, 285.  The small ones' were
-// fitted to 380 products with B in no cache, so that the choice is 1.5 % behind the best way on average (7 % with tiles of 16 x 16 and 32 x 32 by four wavefronts
+// fitted to 380 products with B in no cache, so that the choice is 1.6 % behind the best way on average (7 % with tiles of 16 x 16 and 32 x 32 by four wavefronts
 // alone): the larger of a wavefront's chain of steps, in rounds of workgroups, and the bytes from the caches.  us, bf16: 32 x 4096 x 11008: 18.4 in 32 x 32 by
 // four wavefronts, in 32 x 16 by eight 13.9, in 16 x 16 16.0; 64 x 4096 x 11008: 18.2 in 32 x 32 by four, by eight 16.4; 256 x 4096 x 4096: 21.7 in 128 x 128,
 // in 64 x 32 15.2, in 32 x 32 by eight 17.0; 1024 x 1000 x 1000: 8.2 in 128 x 128, 6.6 in 32 x 32 by four, by eight 7.2.
@@ -576,7 +576,7 @@ Route route(bool bf16, int64_t M, int64_t N, int64_t K) {
     small(32, 16, 8, 0.42, 1, 20.5e6, 0.0014);
     small(32, 32, 4, 0.58, 2, 18e6, 0.0006);
     small(32, 32, 8, 0.80, 1, 18.5e6, 0.00106);
-    small(64, 32, 8, 1.13, 1, 18e6, 0.0046);
+    small(64, 32, 8, 1.2, 1, 18e6, 0.0046);
     auto large = [&](int tile, int deep, int most, int per_unit, double step, double busy, double ends) {
         for (int splits = 1; splits <= most && splits <= KB; ++splits) {
             const double groups = tiles(tile, tile) * splits, full = std::min(1.0, groups / UNITS);

@@ -195,8 +195,8 @@ def test_scales_far_apart(dtype):
 
 
 WAYS = [("bf16", 9, 700, 1000, (16, 16, 1, 4)), ("bf16", 33, 500, 9000, (16, 16, 1, 8)), ("bf16", 70, 1101, 9000, (32, 16, 1, 8)),
-        ("bf16", 1000, 500, 300, (32, 32, 1, 4)), ("bf16", 1113, 158, 7105, (32, 32, 1, 8)), ("bf16", 768, 768, 8000, (64, 32, 1, 8)),
-        ("bf16", 1001, 700, 9000, (64, 32, 1, 8)), ("bf16", 768, 768, 16000, (128, 128, 4, 5)), ("bf16", 1000, 4000, 4000, (128, 128, 4, 1)),
+        ("bf16", 1000, 500, 300, (32, 32, 1, 4)), ("bf16", 1113, 158, 7105, (32, 32, 1, 8)), ("bf16", 250, 4090, 4100, (64, 32, 1, 8)),
+        ("bf16", 768, 768, 8000, (128, 128, 4, 4)), ("bf16", 768, 768, 16000, (128, 128, 4, 5)), ("bf16", 1000, 4000, 4000, (128, 128, 4, 1)),
         ("bf16", 4100, 770, 700, (128, 128, 4, 1)), ("bf16", 8000, 750, 780, (128, 128, 2, 1)), ("bf16", 4000, 4100, 1000, (256, 256, 2, 1)),
         ("bf16", 2048, 768, 30000, (128, 128, 4, 2)), ("bf16", 17, 4163, 38991, (128, 128, 2, 15)), ("bf16", 154, 5450, 30935, (256, 256, 2, 11)),
         ("bf16", 6000, 5000, 130, (256, 256, 2, 1)), ("fp32", 9, 700, 1000, (16, 16, 1, 4)), ("fp32", 33, 500, 9000, (16, 16, 1, 8)),

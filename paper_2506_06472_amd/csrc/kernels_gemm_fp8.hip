@@ -191,7 +191,7 @@ __device__ __forceinline__ void store_part(floatx4 (&acc)[TM][TN], unsigned char
     if (sizeof(T) == 2 && nsplit == 1 && !bias && !resid && mw + 16 * TM <= M && nw + 16 * TN <= N) {
         // As bf16: the two halves of register pairs trade places so that a lane has eight neighbours of a row.
         constexpr int CHUNKS = 2 * TN;                         // of eight results, to a row
-        auto turn = [](int row) __attribute__((always_inline)) { return CHUNKS == 16 ? row : row >> 1 & 7; };
+        auto turn = [](int row) __attribute__((always_inline)) { return CHUNKS == 16 ? row : CHUNKS == 8 ? row >> 1 & 7 : row >> 2 & 3; };
         auto whole = [&](auto STREAM) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
@@ -233,7 +233,7 @@ __device__ __forceinline__ void store_part(floatx4 (&acc)[TM][TN], unsigned char
     // As fp32, for sums of ranges, bias, residual and edges, 64 rows at a time; a loop, since straight-line code for what few wavefronts run has to be
     // fetched by them alone.
     constexpr int QUADS = 4 * TN;                              // of four results, to a row
-    auto quad = [&](int row, int q) __attribute__((always_inline)) { return reinterpret_cast<float4 *>(stage + (row * QUADS + (q ^ (row & 15))) * 16); };
+    auto quad = [&](int row, int q) __attribute__((always_inline)) { return reinterpret_cast<float4 *>(stage + (row * QUADS + (q ^ (QUADS == 8 ? row >> 1 & 7 : row & 15))) * 16); };
     auto rows64 = [&](auto FIRST) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -298,8 +298,9 @@ __device__ __forceinline__ void load_to_lds_b32(const uint8_t *from, uint32_t ld
 #pragma clang diagnostic pop
 
 // The loads of a tile of 32 TM x 32 TN results by four wavefronts: both operands' fragments from memory straight into LDS, D steps (blocks of 128 of the
-// contraction) deep, and the exponents of each wavefront's rows and columns, a 4-byte load to LDS a step (lanes 0 .. 31 A's, the others B's).
-template <int TM, int TN, int D> struct Loads {
+// contraction) deep, and the exponents of each wavefront's rows and columns, a 4-byte load to LDS a step (lanes 0 .. 31 A's, the others B's).  Wavefronts are two
+// by two, or with STRIPS side by side in a tile of 64 rows.
+template <int TM, int TN, int D, bool STRIPS = false> struct Loads {
     static constexpr int BM = 32 * TM, BN = 32 * TN, TILE_A = BM * 128, TILE_B = BN * 128;
     static constexpr int WA = TM / 4, WB = TN / 4;             // words of exponents a lane has (64 rows each)
     static constexpr uint32_t EXPS = D * (TILE_A + TILE_B), LDS = EXPS + 4 * D * 256;
@@ -330,7 +331,8 @@ template <int TM, int TN, int D> struct Loads {
         }
         const bool isB = lane >= 32;
         const int64_t most = isB ? (N - 1) / 64 : (M - 1) / 64,
-                      g = (isB ? (int64_t)tn * (2 * WB) + (wave & 1) * WB : (int64_t)tm * (2 * WA) + (wave >> 1) * WA) + (lane >> 4 & 1);
+                      g = STRIPS ? (isB ? (int64_t)tn * 2 + (wave >> 1) : tm)
+                               : (isB ? (int64_t)tn * (2 * WB) + (wave & 1) * WB : (int64_t)tm * (2 * WA) + (wave >> 1) * WA) + (lane >> 4 & 1);
         exps = (isB ? B + sb.code_bytes() : A + sa.code_bytes()) + ((g < most ? g : most) * KB + kb0) * 64 + (lane & 15) * 4;
         lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem));
     }
@@ -342,11 +344,14 @@ template <int TM, int TN, int D> struct Loads {
         ahead = ahead + 1 < (uint32_t)nk ? ahead + 1 : (uint32_t)nk - 1;
         voff = lane * 16 + ahead * F8_FRAG;
     }
-    __device__ __forceinline__ void load_step(int S) {
+    // there_is false: the counters' loads, but nothing is fetched
+    __device__ __forceinline__ void load_step(int S, bool there_is = true) {
+        i32x4 a = rsA, b = rsB;
+        if (!there_is) a[2] = b[2] = 0;
 #pragma unroll
-        for (int i = 0; i < TM; ++i) load_to_lds_b128(rsA, to_a(S, i), voff, soA[i]);
+        for (int i = 0; i < TM; ++i) load_to_lds_b128(a, to_a(S, i), voff, soA[i]);
 #pragma unroll
-        for (int i = 0; i < TN; ++i) load_to_lds_b128(rsB, to_b(S, i), voff, soB[i]);
+        for (int i = 0; i < TN; ++i) load_to_lds_b128(b, to_b(S, i), voff, soB[i]);
         load_exps(S);
         go_on();
     }
@@ -483,6 +488,85 @@ __global__ void __launch_bounds__(256)
                                ldr, C, ldc, ws, split, nsplit);
 }
 
+using StripLoads = Loads<2, 4, 3, true>;
+
+// Tiles of 64 x 128 for products of some hundred rows or columns, which have too few tiles of 128 x 128 for all compute units (512 x 4096 x 11008 50 -> 39 us,
+// 128 x 11008 x 4096 23 -> 18.8): each wavefront has all rows and 32 columns.  A step's fragments are read into a second set of registers while the products of the
+// one before run, as above, in the compiler's order; two workgroups to a compute unit cover each other's waits (six steps deep and one to a unit: 40 and 20).
+template <int FA, int FB>
+__global__ void __launch_bounds__(256, 2)
+    gemm_fp8_strip_k(const uint8_t *__restrict__ A, const uint8_t *__restrict__ B, const bf16_t *__restrict__ bias, const bf16_t *resid, int64_t ldr, bf16_t *C, int64_t ldc,
+                     int64_t M, int64_t N, int64_t K, int tiles_m, int tiles_n, float *__restrict__ ws) {
+    constexpr int D = 3;
+    constexpr int TM = 4, TN = 2;                              // a wavefront's
+    using L = StripLoads;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem8[];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    int split, nsplit, tm, tn;
+    if (!place(tiles_m, tiles_n, 0, split, nsplit, tm, tn)) return;
+    const int KB = (int)Fp8Shape{M, K}.kb(), kb0 = (int)((int64_t)KB * split / nsplit), nk = (int)((int64_t)KB * (split + 1) / nsplit) - kb0;
+    L in(A, B, M, N, K, tm, tn, kb0, nk, wave, lane, smem8);
+    floatx4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = (floatx4){0.f, 0.f, 0.f, 0.f};
+    struct Step {
+        i32x8 a[TM], b[TN];
+        uint32_t ea, eb;
+    };
+    auto read = [&](Step &f, int S) __attribute__((always_inline)) {
+        auto frag = [&](uint32_t at) __attribute__((always_inline)) {
+            const uint4 u = *reinterpret_cast<const uint4 *>(smem8 + at + lane * 16), v = *reinterpret_cast<const uint4 *>(smem8 + at + 1024 + lane * 16);
+            return (i32x8){(int)u.x, (int)u.y, (int)u.z, (int)u.w, (int)v.x, (int)v.y, (int)v.z, (int)v.w};
+        };
+        const unsigned char *const e = smem8 + L::EXPS + (wave * D + S) * 256 + (lane & 15) * 4;
+        f.ea = *reinterpret_cast<const uint32_t *>(e);
+        f.eb = *reinterpret_cast<const uint32_t *>(e + 128) >> (wave & 1) * 16;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) f.b[j] = frag(D * L::TILE_A + S * L::TILE_B + (wave * TN + j) * F8_FRAG);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) f.a[i] = frag(S * L::TILE_A + i * F8_FRAG);
+    };
+    auto product = [&](const Step &f, auto I, auto J) __attribute__((always_inline)) {
+        constexpr int i = decltype(I)::value, j = decltype(J)::value;
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f.b[j], f.a[i], acc[i][j], FB, FA, j, (int)f.eb, i, (int)f.ea);
+    };
+    auto products = [&](const Step &f) __attribute__((always_inline)) {
+        each([&](auto I) __attribute__((always_inline)) {
+            each([&](auto J) __attribute__((always_inline)) { product(f, I, J); }, std::make_integer_sequence<int, TN>{});
+        }, std::make_integer_sequence<int, TM>{});
+    };
+    constexpr auto wait_vm = [](int n) { return 0x0070 | (n & 15) | ((n >> 4) << 14); };      // s_waitcnt vmcnt(n) lgkmcnt(0)
+    static_assert((D - 1) * L::PER < 64, "loads in flight fit the counter");
+#pragma unroll
+    for (int t = 0; t < D; ++t) in.load_step(t);
+    __builtin_amdgcn_s_waitcnt(wait_vm((D - 1) * L::PER));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    Step even, odd;
+    int S = 0, kt = 0;
+    read(even, 0);
+    // the products of step kt, whose fragments are `now`
+    auto step = [&](const Step &now, Step &next) __attribute__((always_inline)) {
+        __builtin_amdgcn_s_waitcnt(wait_vm((D - 2) * L::PER));  // the next step has landed, and this one is in registers
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        in.load_step(S, kt + D < nk);
+        S = S + 1 < D ? S + 1 : 0;
+        read(next, S);
+        products(now);
+        return ++kt >= nk;
+    };
+    while (!step(even, odd) && !step(odd, even)) {}
+    __builtin_amdgcn_s_waitcnt(wait_vm(0));                    // nothing is on its way to LDS any more, for any wavefront: it takes the results
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    static_assert(4 * stage_bytes<TN>() <= (int)L::EXPS, "the results' places fit the fragments'");
+    store_part<bf16_t, TM, TN>(acc, smem8 + wave * stage_bytes<TN>(), lane, (int64_t)tm * 64, (int64_t)tn * 128 + wave * 32, M, N, bias, resid, ldr, C, ldc, ws, split,
+                               nsplit);
+}
+
 // ---- in fp32: the values, which bf16 holds exactly, in 16-bit products, whose sums are those of 32-bit arithmetic.  A quarter to half of the 8-bit products' rate.
 // 128 x 128 results; two workgroups to a compute unit cover each other's conversions and loads.
 template <int FA, int FB>
@@ -542,7 +626,7 @@ __global__ void __launch_bounds__(256, 2)
     store_part<float, TM, TN>(acc, smem8 + wave * stage_bytes<TN>(), lane, (int64_t)tm * L::BM + wm * 16 * TM, (int64_t)tn * L::BN + wn * 16 * TN, M, N, bias, resid, ldr, C, ldc, ws, split, nsplit);
 }
 
-// How a product is taken: tiles of 128 x 128 or 256 x 256 through LDS, `deep` steps at a time, the contraction cut into ranges, or (deep 1) smaller ones from the
+// How a product is taken: tiles of 64 x 128, 128 x 128 or 256 x 256 through LDS, `deep` steps at a time, the contraction cut into ranges, or (deep 1) smaller ones from the
 // caches, the contraction cut into the shares of four or eight wavefronts (gemm_fp8_direct_k).
 //
 // The least of an estimate of the time.  The large tiles' constants were fitted to 39 products, each taken in all ways: a workgroup's steps and its beginning and
@@ -552,7 +636,8 @@ __global__ void __launch_bounds__(256, 2)
 // fitted to 380 products with B in no cache, so that the choice is 1.6 % behind the best way on average (7 % with tiles of 16 x 16 and 32 x 32 by four wavefronts
 // alone): the larger of a wavefront's chain of steps, in rounds of workgroups, and the bytes from the caches.  us, bf16: 32 x 4096 x 11008: 18.4 in 32 x 32 by
 // four wavefronts, in 32 x 16 by eight 13.9, in 16 x 16 16.0; 64 x 4096 x 11008: 18.2 in 32 x 32 by four, by eight 16.4; 256 x 4096 x 4096: 21.7 in 128 x 128,
-// in 64 x 32 15.2, in 32 x 32 by eight 17.0; 1024 x 1000 x 1000: 8.2 in 128 x 128, 6.6 in 32 x 32 by four, by eight 7.2.
+// in 64 x 32 15.2, in 32 x 32 by eight 17.0; 1024 x 1000 x 1000: 8.2 in 128 x 128, 6.6 in 32 x 32 by four, by eight 7.2.  64 x 128 tiles' were fitted to 140 more (1.7 % behind the best way on
+// average, 4.6 % without them).
 struct Route {
     int rows, cols, deep, splits;                              // splits: ranges, or wavefronts that share a contraction
 };
@@ -577,23 +662,25 @@ Route route(bool bf16, int64_t M, int64_t N, int64_t K) {
     small(32, 32, 4, 0.58, 2, 18e6, 0.0006);
     small(32, 32, 8, 0.80, 1, 18.5e6, 0.00106);
     small(64, 32, 8, 1.2, 1, 18e6, 0.0046);
-    auto large = [&](int tile, int deep, int most, int per_unit, double step, double busy, double ends) {
+    auto large = [&](int rows, int cols, int deep, int most, int per_unit, double step, double busy, double ends) {
         for (int splits = 1; splits <= most && splits <= KB; ++splits) {
-            const double groups = tiles(tile, tile) * splits, full = std::min(1.0, groups / UNITS);
+            const double groups = tiles(rows, cols) * splits, full = std::min(1.0, groups / UNITS);
             if (per_unit > 1 && groups <= UNITS) continue;
             double t = std::ceil(groups / (UNITS * per_unit)) * ((KB + splits - 1) / splits * (step + busy * full) + ends);
             if (splits > 1) t += 3.0 + (double)M * N * 8 * (splits + 0.5) / 3.5e6;
-            take(t, {tile, tile, deep, splits});
+            take(t, {rows, cols, deep, splits});
         }
     };
     if (bf16) {
-        large(256, 2, 16, 1, 1.06, 0.28, 5.0);
-        large(128, 2, 16, 2, 0.88, 0.0, 4.0);
-        large(128, 2, 1, 1, 0.60, 0.0, 4.2);
-        large(128, 4, 32, 1, 0.32, 0.12, 5.0);
+        large(256, 256, 2, 16, 1, 1.06, 0.28, 5.0);
+        large(128, 128, 2, 16, 2, 0.88, 0.0, 4.0);
+        large(128, 128, 2, 1, 1, 0.60, 0.0, 4.2);
+        large(128, 128, 4, 32, 1, 0.32, 0.12, 5.0);
+        large(64, 128, 3, 8, 1, 0.25, 0.08, 3.8);
+        large(64, 128, 3, 1, 2, 0.50, 0.0, 4.4);
     } else {
-        large(128, 2, 16, 2, 1.8, 0.0, 4.0);
-        large(128, 2, 32, 1, 1.05, 0.0, 4.6);
+        large(128, 128, 2, 16, 2, 1.8, 0.0, 4.0);
+        large(128, 128, 2, 32, 1, 1.05, 0.0, 4.6);
     }
     return best;
 }
@@ -631,6 +718,7 @@ template <int FA, int FB, typename T> void launch(hipStream_t s, const Fp8Produc
     auto go = [&](auto kernel, uint32_t lds) { kernel<<<grid, 256, lds, s>>>(A, B, bias, resid, p.ldr, (T *)p.C, p.ldc, p.M, p.N, p.K, tiles_m, tiles_n, (float *)p.work); };
     if constexpr (sizeof(T) == 2) {
         if (r.rows == 256) allow_lds<gemm_fp8_tile_k<FA, FB, 8, 8, 2>, Loads<8, 8, 2>::LDS>(), go(gemm_fp8_tile_k<FA, FB, 8, 8, 2>, Loads<8, 8, 2>::LDS);
+        else if (r.rows == 64) allow_lds<gemm_fp8_strip_k<FA, FB>, StripLoads::LDS>(), go(gemm_fp8_strip_k<FA, FB>, StripLoads::LDS);
         else if (r.deep == 4) allow_lds<gemm_fp8_tile_k<FA, FB, 4, 4, 4>, Loads<4, 4, 4>::LDS>(), go(gemm_fp8_tile_k<FA, FB, 4, 4, 4>, Loads<4, 4, 4>::LDS);
         else allow_lds<gemm_fp8_tile_k<FA, FB, 4, 4, 2>, Loads<4, 4, 2>::LDS>(), go(gemm_fp8_tile_k<FA, FB, 4, 4, 2>, Loads<4, 4, 2>::LDS);
     } else allow_lds<gemm_fp8_tile32_k<FA, FB>, Loads<4, 4, 2>::LDS>(), go(gemm_fp8_tile32_k<FA, FB>, Loads<4, 4, 2>::LDS);

@@ -195,10 +195,13 @@ def test_scales_far_apart(dtype):
 
 
 WAYS = [("bf16", 9, 700, 1000, (16, 16, 1, 4)), ("bf16", 33, 500, 9000, (16, 16, 1, 8)), ("bf16", 70, 1101, 9000, (32, 16, 1, 8)),
-        ("bf16", 1000, 500, 300, (32, 32, 1, 4)), ("bf16", 1113, 158, 7105, (32, 32, 1, 8)), ("bf16", 250, 4090, 4100, (64, 32, 1, 8)),
-        ("bf16", 768, 768, 8000, (128, 128, 4, 4)), ("bf16", 768, 768, 16000, (128, 128, 4, 5)), ("bf16", 1000, 4000, 4000, (128, 128, 4, 1)),
-        ("bf16", 4100, 770, 700, (128, 128, 4, 1)), ("bf16", 8000, 750, 780, (128, 128, 2, 1)), ("bf16", 4000, 4100, 1000, (256, 256, 2, 1)),
-        ("bf16", 2048, 768, 30000, (128, 128, 4, 2)), ("bf16", 17, 4163, 38991, (128, 128, 2, 15)), ("bf16", 154, 5450, 30935, (256, 256, 2, 11)),
+        ("bf16", 1000, 500, 300, (32, 32, 1, 4)), ("bf16", 1113, 158, 7105, (32, 32, 1, 8)), ("bf16", 802, 588, 5470, (64, 32, 1, 8)),
+        ("bf16", 768, 768, 8000, (64, 128, 3, 3)), ("bf16", 143, 8633, 2554, (64, 128, 3, 1)),
+        ("bf16", 1443, 458, 16388, (128, 128, 4, 5)), ("bf16", 61, 3, 28095, (128, 128, 4, 32)),
+        ("bf16", 1000, 4000, 4000, (128, 128, 4, 1)),
+        ("bf16", 4100, 770, 700, (64, 128, 3, 1)), ("bf16", 8000, 750, 780, (128, 128, 2, 1)), ("bf16", 4000, 4100, 1000, (256, 256, 2, 1)),
+        ("bf16", 2048, 768, 30000, (128, 128, 4, 2)), ("bf16", 17, 4163, 38991, (64, 128, 3, 7)),
+        ("bf16", 1786, 1439, 29596, (128, 128, 2, 3)), ("bf16", 154, 5450, 30935, (256, 256, 2, 11)),
         ("bf16", 6000, 5000, 130, (256, 256, 2, 1)), ("fp32", 9, 700, 1000, (16, 16, 1, 4)), ("fp32", 33, 500, 9000, (16, 16, 1, 8)),
         ("fp32", 70, 1101, 9000, (32, 16, 1, 8)), ("fp32", 1000, 500, 300, (32, 32, 1, 4)), ("fp32", 1113, 158, 7105, (32, 32, 1, 8)),
         ("fp32", 1000, 1000, 8000, (64, 32, 1, 8)), ("fp32", 5093, 803, 26396, (128, 128, 2, 3)), ("fp32", 4000, 1500, 500, (128, 128, 2, 1)),
@@ -290,7 +293,7 @@ def test_rows_past_4_gib():
     tio.tio_op_fp8_load(0, "bf16", "e4m3", R, C, q[0].data_ptr(), near.data_ptr(), C)
     tio.tio_op_fp8_load(0, "bf16", "e4m3", R, C, q[0].data_ptr(), flat.data_ptr(), far)
     assert torch.equal(wide, near)
-    for M, N, tile in ((40, 200, 16), (1000, 600, 32), (2000, 2000, 128), (4000, 4104, 256)):
+    for M, N, tile in ((40, 200, 16), (1000, 600, 32), (2000, 2000, 64), (2000, 4000, 128), (4000, 4104, 256)):
         assert tio.tio_op_gemm_fp8_route("bf16", M, N, 1000)[0] == tile
         a, b = torch.randn((M, 1000), device="cuda"), torch.randn((N, 1000), device="cuda")
         s = [torch.zeros(tio.tio_fp8_bytes(len(v), 1000), device="cuda", dtype=torch.uint8) for v in (a, b)]

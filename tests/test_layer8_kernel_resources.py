@@ -18,6 +18,7 @@ FORMS = {
                           for a, b, t, (m, n, w) in ALL(FLAGS, FLAGS, T, ((1, 1, 4), (1, 1, 8), (2, 1, 8), (2, 2, 4), (2, 2, 8), (4, 2, 8)))],
     # forms; groups of 16 rows and columns to a wavefront, steps in LDS
     "gemm_fp8_tile_k": [f"ILi{a}ELi{b}ELi{n}ELi{n}ELi{d}E" for a, b, (n, d) in ALL(FLAGS, FLAGS, ((8, 2), (4, 4), (4, 2)))],
+    "gemm_fp8_strip_k": [f"ILi{a}ELi{b}E" for a, b in ALL(FLAGS, FLAGS)],
     "gemm_fp8_tile32_k": [f"ILi{a}ELi{b}E" for a, b in ALL(FLAGS, FLAGS)],
     "gemm_fp8_sums_k": [f"I{t}E" for t in T],
     # wavefronts to a row; root mean square; a norm behind the block

@@ -11,7 +11,7 @@
 //   S1 = sum of m bh,  S2 = sum of m:   dpost_gain = bs s gate S1,  dpost_bias = bs s gate S2,  dgate = bs s (post_gain S1 + post_bias S2).
 //
 // Bound: HBM; the vector ALU, with about 14 (forward) and 24 operations on an element beside the generator's, is not far behind (8192 x 4096 in bf16: forward
-// 51 us, 5.3 TB/s; backward 70, 5.8, and the sums 8).  A row is W
+// 51 us, 5.3 TB/s; backward 70, 5.8, and the sums 6).  A row is W
 // wavefronts', who hold it in registers from its loads to its stores; statistics and sums are in 32 bits, the layer norm's variance from centred values.  A
 // workgroup takes rows one after the other and keeps its share of the column sums in registers; a second launch adds the workgroups' shares in their
 // order, so that results do not depend on timing.
@@ -119,6 +119,8 @@ template <typename T, int W, bool RMS, bool POST> struct Columns {
         : lane(W == 1 ? threadIdx.x & 63 : threadIdx.x), col(lane * 8), bytes((uint32_t)((a.d + 7) / 8 * 8 * sizeof(T))), ragged(a.d % 8 != 0) {
         const int left = (int)a.d - (int)col;
         n = left < 0 ? 0 : left < 8 ? left : 8;
+    }
+    __device__ __forceinline__ void load_vectors(const ResidualArgs &a) {
         load(gain, a.gain);
         const float factor = a.branch_scale * (a.drop.limit ? a.drop.scale : 1.f);
         float f[8];
@@ -176,10 +178,11 @@ template <typename T, int W, bool RMS, bool POST>
 __global__ void __launch_bounds__(W == 1 ? 256 : W * 64) residual_norm_k(ResidualArgs a) {
     __shared__ float red[4 * W];
     RowSum<W> sum(red);
-    const Columns<T, W, RMS, POST> col(a);
+    Columns<T, W, RMS, POST> col(a);
     const void *const gate = a.ldg ? a.gate : nullptr;
     const uint32_t groups = (uint32_t)((a.d + 7) / 8);
     const float inv_d = 1.0f / (float)a.d;
+    col.load_vectors(a);
     float bias[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (!RMS && a.bias) col.load(bias, a.bias);
     const int team = W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
@@ -229,7 +232,7 @@ template <typename T, int W, bool RMS, bool POST>
 __global__ void __launch_bounds__(W == 1 ? 256 : W * 64, 4) residual_norm_bwd_k(ResidualArgs a) {
     __shared__ float red[4 * W];
     RowSum<W> sum(red);
-    const Columns<T, W, RMS, POST> col(a);
+    Columns<T, W, RMS, POST> col(a);
     const void *const gate = a.ldg ? a.gate : nullptr;
     const uint32_t groups = (uint32_t)((a.d + 7) / 8);
     const float inv_d = 1.0f / (float)a.d;
@@ -237,14 +240,6 @@ __global__ void __launch_bounds__(W == 1 ? 256 : W * 64, 4) residual_norm_bwd_k(
     float s_gain[8], s_bias[8], s1[8], s2[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) s_gain[j] = s_bias[j] = s1[j] = s2[j] = 0.f;
-    // with a gate for every row, what the layer norm's bias adds to its gradient: a thread's own, in LDS for want of registers
-    constexpr bool MOVED = POST && !RMS;
-    constexpr int THREADS = W == 1 ? 256 : W * 64;
-    __shared__ float4 moved[MOVED ? 2 : 1][MOVED ? THREADS : 1];
-    if (MOVED) {
-        moved[0][threadIdx.x] = make_float4(col.c[0], col.c[1], col.c[2], col.c[3]);
-        moved[MOVED][threadIdx.x] = make_float4(col.c[4], col.c[5], col.c[6], col.c[7]);
-    }
     const int team = W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
     const int64_t stride = (int64_t)gridDim.x * teams_of(W);
     int64_t row = (int64_t)blockIdx.x * teams_of(W) + team;
@@ -270,6 +265,16 @@ __global__ void __launch_bounds__(W == 1 ? 256 : W * 64, 4) residual_norm_bwd_k(
         fetch_others(at);
     };
     if (AHEAD) fetch(row);
+    __builtin_amdgcn_sched_barrier(0);
+    col.load_vectors(a);                                       // with the first row's loads under way (1021 x 6656 25.1 -> 23.3 us)
+    // with a gate for every row, what the layer norm's bias adds to its gradient: a thread's own, in LDS for want of registers
+    constexpr bool MOVED = POST && !RMS;
+    constexpr int THREADS = W == 1 ? 256 : W * 64;
+    __shared__ float4 moved[MOVED ? 2 : 1][MOVED ? THREADS : 1];
+    if (MOVED) {
+        moved[0][threadIdx.x] = make_float4(col.c[0], col.c[1], col.c[2], col.c[3]);
+        moved[MOVED][threadIdx.x] = make_float4(col.c[4], col.c[5], col.c[6], col.c[7]);
+    }
     for (; row < a.rows; row += stride) {
         if (!AHEAD) fetch_first(row);
         Row8<T> raw[5] = {next[0], next[1], next[2], next[3], next[4]};
@@ -369,12 +374,13 @@ __global__ void __launch_bounds__(W == 1 ? 256 : W * 64, 4) residual_norm_bwd_k(
     if (POST && !RMS) out(3, s2);
 }
 
-// A workgroup adds 16 columns, four wavefronts a kind: the workgroups' shares in their order within each of 64 slices, the slices in theirs.
+// A workgroup adds 16 columns, four wavefronts a kind: the workgroups' shares in their order within each of 64 slices, the slices in theirs.  Neighbouring
+// workgroups, whose columns are in the same 128-byte lines, are on one XCD (8192 x 4096: 8.3 -> 5.8 us).
 template <typename T> __global__ void __launch_bounds__(256 * KINDS) residual_sums_k(ResidualArgs a, int64_t parts) {
     __shared__ float4 part[KINDS][64][4];
     __shared__ float sums[KINDS][16];
     const int kind = threadIdx.x >> 8, q = threadIdx.x & 3, slice = threadIdx.x >> 2 & 63;
-    const int64_t d8 = (a.d + 7) / 8 * 8, col = (int64_t)blockIdx.x * 16 + q * 4;
+    const int64_t d8 = (a.d + 7) / 8 * 8, first = ((int64_t)(blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8) * 16, col = first + q * 4;
     const bool post = a.post_gain, shared = a.gate && !a.ldg;
     const bool there_is = kind == 0 || (kind == 1 ? post || shared : !a.rms && (kind == 2 || post));
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -395,7 +401,7 @@ template <typename T> __global__ void __launch_bounds__(256 * KINDS) residual_su
         sums[kind][threadIdx.x & 15] = t;
     }
     __syncthreads();
-    const int64_t at = (int64_t)blockIdx.x * 16 + threadIdx.x;
+    const int64_t at = first + threadIdx.x;
     if (threadIdx.x >= 16 || at >= a.d) return;
     const float factor = a.branch_scale * (a.drop.limit ? a.drop.scale : 1.f);
     auto value = [&](const void *p) __attribute__((always_inline)) { return p ? to_f32(((const T *)p)[at]) : 0.f; };
@@ -455,7 +461,7 @@ void residual_norm(hipStream_t s, int dtype, const ResidualArgs &a) {
 }
 
 void residual_norm_bwd(hipStream_t s, int dtype, const ResidualArgs &a) {
-    const unsigned grid = (unsigned)backward_groups(a.rows, a.d), columns = (unsigned)((a.d + 15) / 16);
+    const unsigned grid = (unsigned)backward_groups(a.rows, a.d), columns = (unsigned)((a.d + 127) / 128 * 8);
     TIO_BY_WIDTH(residual_norm_bwd_k);
     if (dtype == TIO_PREC_BF16) residual_sums_k<bf16_t><<<columns, 256 * KINDS, 0, s>>>(a, grid);
     else residual_sums_k<float><<<columns, 256 * KINDS, 0, s>>>(a, grid);

@@ -549,6 +549,8 @@ __global__ void __launch_bounds__(256, 2)
     read(even, 0);
     // the products of step kt, whose fragments are `now`
     auto step = [&](const Step &now, Step &next) __attribute__((always_inline)) {
+        asm volatile("" ::: "memory");                          // this step's reads stay before the wait, whose barrier frees their part of LDS
+        __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(wait_vm((D - 2) * L::PER));  // the next step has landed, and this one is in registers
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");

@@ -656,6 +656,7 @@ Route route(bool bf16, int64_t M, int64_t N, int64_t K) {
     };
     auto small = [&](int rows, int cols, int waves, double step, int per_unit, double per_us, double each) {
         const double groups = tiles(rows, cols), chain = step * (double)((KB + waves - 1) / waves) * std::ceil(groups / (UNITS * per_unit));
+        if (groups * waves * 64 >= 4294967296.0) return;       // threads that a launch may have
         take(2.0 + std::max(chain, groups * KB * (rows + cols) * 128 / per_us + groups * each), {rows, cols, 1, waves});
     };
     small(16, 16, 4, 0.17, 4, 17e6, 0.00016);

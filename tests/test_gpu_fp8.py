@@ -367,3 +367,21 @@ def test_two_products_at_once():
         call(i, y[1, i], 0)
     torch.cuda.synchronize()
     assert torch.equal(y[0], y[1]) and not torch.equal(y[0, 0], y[0, 1])
+
+
+@pytest.mark.parametrize("M,N", [(1 << 22, 5), (5, 1 << 22)])
+def test_the_most_rows(M, N):
+    """The largest number of rows of either operand, whole numbers: exact."""
+    import torch
+    import paper_2506_06472_amd as tio
+    K, ops, q = 100, [], []
+    for rows in (M, N):
+        v = torch.randint(-8, 9, (rows, 104), device="cuda", dtype=torch.bfloat16)
+        q.append(torch.empty(tio.tio_fp8_bytes(rows, K), device="cuda", dtype=torch.uint8))
+        tio.tio_op_fp8_store(0, "bf16", "e4m3", False, rows, K, v.data_ptr(), 104, q[-1].data_ptr())
+        ops.append(v[:, :K])
+    up = (N + 7) // 8 * 8
+    work = torch.empty(tio.tio_op_gemm_fp8_work(M, N, K) + 16, device="cuda", dtype=torch.uint8)
+    y = torch.full((M, up), 7.0, device="cuda", dtype=torch.bfloat16)
+    tio.tio_op_gemm_fp8(0, "bf16", M, N, K, "e4m3", q[0].data_ptr(), "e4m3", q[1].data_ptr(), y.data_ptr(), up, work_ptr=work.data_ptr())
+    assert torch.equal(y[:, :N], (ops[0].float() @ ops[1].float().t()).to(torch.bfloat16)) and (y[:, N:] == 0).all()

@@ -360,6 +360,17 @@ template <int TM, int TN, int D, bool STRIPS = false> struct Loads {
 // f of each number as a constant
 template <typename F, int... I> __device__ __forceinline__ void each(const F &f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
 
+// Waits until no more than LOADS of the wavefront's loads are on their way and all that it has read from LDS is in registers, then for the workgroup's other
+// wavefronts, whose loads may write from then on where it has read.  The compiler orders reads of LDS with neither the wait nor the barrier, and one whose value is used
+// only behind them might move there: so no access to memory moves over either end.
+template <int LOADS> __device__ __forceinline__ void meet() {
+    static_assert(LOADS < 64, "loads in flight fit the counter");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070 | (LOADS & 15) | ((LOADS >> 4) << 14));       // vmcnt(LOADS) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // A tile of 32 TM x 32 TN results: four wavefronts, 16 TM x 16 TN each.  A step of the contraction is one block of 128: TM TN products of 32 clocks.
 //  * Fragments are stored as the products take them, so that LDS is written and read in consecutive KiB.
 //  * While the products of a step run, all fragments of the next one are read into registers: B's into a second set, A's into the registers of the row
@@ -408,8 +419,6 @@ __global__ void __launch_bounds__(256)
         for (int w = 0; w < WB; ++w) eb[S() % 2][w] = *reinterpret_cast<const uint32_t *>(at + 128 + w * 64);
     };
     constexpr std::integral_constant<int, 0> c0{};
-    constexpr auto wait_vm = [](int n) { return 0x0070 | (n & 15) | ((n >> 4) << 14); };      // s_waitcnt vmcnt(n) lgkmcnt(0)
-    static_assert((D - 1) * L::PER < 64, "loads in flight fit the counter");
 
     // The products of a step from the registers of parity S.  Reads of the next step (read p at product RSTEP p / 8): B's groups in turn with A's last
     // two, then A's from the first on, each after its row group's products.  Loads D steps ahead at every NQ / 2 / NL-th product.
@@ -439,16 +448,13 @@ __global__ void __launch_bounds__(256)
         };
         each(product, std::make_integer_sequence<int, NQ>{});
         in.go_on();
-        __builtin_amdgcn_s_waitcnt(wait_vm((D - 2) * L::PER));  // the step after the next has landed, the next one is in registers
-        __builtin_amdgcn_s_barrier();
+        meet<(D - 2) * L::PER>();                              // the step after the next has landed, the next one is in registers
         __builtin_amdgcn_sched_barrier(0);
     };
 
 #pragma unroll
     for (int t = 0; t < D; ++t) in.load_step(t);
-    __builtin_amdgcn_s_waitcnt(wait_vm((D - 2) * L::PER));
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
+    meet<(D - 2) * L::PER>();
     each([&](auto I) __attribute__((always_inline)) { read_a(c0, I); }, std::make_integer_sequence<int, TM>{});
 #pragma unroll
     for (int j = 0; j < TN; ++j) read_b(c0, j);
@@ -461,8 +467,7 @@ __global__ void __launch_bounds__(256)
     };
     pin();
     settle();
-    __builtin_amdgcn_s_waitcnt(wait_vm((D - 2) * L::PER));
-    __builtin_amdgcn_s_barrier();
+    meet<(D - 2) * L::PER>();
     __builtin_amdgcn_sched_barrier(0);
     // One loop for all steps; behind the contraction's end the descriptors are empty, so that nothing is fetched
     int kt = 0;
@@ -477,9 +482,7 @@ __global__ void __launch_bounds__(256)
         static_assert(D == 4, "steps of the loop");
         while (!done(c0) && !done(std::integral_constant<int, 1>{}) && !done(std::integral_constant<int, 2>{}) && !done(std::integral_constant<int, 3>{})) {}
     }
-    __builtin_amdgcn_s_waitcnt(wait_vm(0));                    // nothing is on its way to LDS any more, for any wavefront: it takes the results
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
+    meet<0>();                                                 // nothing is on its way to LDS any more, for any wavefront: it takes the results
     settle();
     pin();
 
@@ -537,23 +540,16 @@ __global__ void __launch_bounds__(256, 2)
             each([&](auto J) __attribute__((always_inline)) { product(f, I, J); }, std::make_integer_sequence<int, TN>{});
         }, std::make_integer_sequence<int, TM>{});
     };
-    constexpr auto wait_vm = [](int n) { return 0x0070 | (n & 15) | ((n >> 4) << 14); };      // s_waitcnt vmcnt(n) lgkmcnt(0)
-    static_assert((D - 1) * L::PER < 64, "loads in flight fit the counter");
 #pragma unroll
     for (int t = 0; t < D; ++t) in.load_step(t);
-    __builtin_amdgcn_s_waitcnt(wait_vm((D - 1) * L::PER));
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
+    meet<(D - 1) * L::PER>();
     Step even, odd;
     int S = 0, kt = 0;
     read(even, 0);
     // the products of step kt, whose fragments are `now`
     auto step = [&](const Step &now, Step &next) __attribute__((always_inline)) {
-        asm volatile("" ::: "memory");                          // this step's reads stay before the wait, whose barrier frees their part of LDS
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(wait_vm((D - 2) * L::PER));  // the next step has landed, and this one is in registers
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+        meet<(D - 2) * L::PER>();                              // the next step has landed, and this one is in registers
         in.load_step(S, kt + D < nk);
         S = S + 1 < D ? S + 1 : 0;
         read(next, S);
@@ -561,9 +557,7 @@ __global__ void __launch_bounds__(256, 2)
         return ++kt >= nk;
     };
     while (!step(even, odd) && !step(odd, even)) {}
-    __builtin_amdgcn_s_waitcnt(wait_vm(0));                    // nothing is on its way to LDS any more, for any wavefront: it takes the results
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
+    meet<0>();                                                 // nothing is on its way to LDS any more, for any wavefront: it takes the results
     static_assert(4 * stage_bytes<TN>() <= (int)L::EXPS, "the results' places fit the fragments'");
     store_part<bf16_t, TM, TN>(acc, smem8 + wave * stage_bytes<TN>(), lane, (int64_t)tm * 64, (int64_t)tn * 128 + wave * 32, M, N, bias, resid, ldr, C, ldc, ws, split,
                                nsplit);
@@ -598,9 +592,7 @@ __global__ void __launch_bounds__(256, 2)
     in.load_step(0);
     for (int kt = 0; kt < nk; ++kt) {
         const int S = kt & 1;
-        __builtin_amdgcn_s_waitcnt(0x0070);                    // this step has landed, and the one before is in registers
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+        meet<0>();                                             // this step has landed, and the one before is in registers
         if (kt + 1 < nk) in.load_step(S ^ 1);
         const unsigned char *const e = smem8 + L::EXPS + (wave * 2 + S) * 256 + (lane & 15) * 4;
         const uint32_t ea = *reinterpret_cast<const uint32_t *>(e), eb = *reinterpret_cast<const uint32_t *>(e + 128);
@@ -622,9 +614,7 @@ __global__ void __launch_bounds__(256, 2)
             }
         }
     }
-    __builtin_amdgcn_s_waitcnt(0x0070);
-    __builtin_amdgcn_s_barrier();                              // every wavefront is done with the fragments: LDS takes the results
-    asm volatile("" ::: "memory");
+    meet<0>();                                                 // every wavefront is done with the fragments: LDS takes the results
     store_part<float, TM, TN>(acc, smem8 + wave * stage_bytes<TN>(), lane, (int64_t)tm * L::BM + wm * 16 * TM, (int64_t)tn * L::BN + wn * 16 * TN, M, N, bias, resid, ldr, C, ldc, ws, split, nsplit);
 }
 

@@ -1,0 +1,111 @@
+"""GPU: every way to take a product of stored matrices, in every pair of 8-bit types, with powers of two that differ from block to block and from row to row, with blocks that are
+not finite, and on normal values."""
+import pytest
+
+import layer8lib as l8
+from test_gpu_fp8 import WAYS
+
+pytestmark = pytest.mark.gpu
+
+PAIRS = [("e4m3", "e4m3"), ("e5m2", "e4m3"), ("e4m3", "e5m2"), ("e5m2", "e5m2")]
+
+
+def _up(n):
+    return (n + 7) // 8 * 8
+
+
+def _stored(v, form):
+    """fp32 [rows, cols] on the GPU -> its stored form; the padding holds NaN"""
+    import torch
+    import paper_2506_06472_amd as tio
+    rows, cols = v.shape
+    p = torch.full((rows, _up(cols) + 8), float("nan"), device="cuda")
+    p[:, :cols] = v
+    q = torch.empty(tio.tio_fp8_bytes(rows, cols), device="cuda", dtype=torch.uint8)
+    tio.tio_op_fp8_store(0, "fp32", form, False, rows, cols, p.data_ptr(), p.stride(0), q.data_ptr())
+    return q
+
+
+def _product(qa, qb, forms, dtype, M, N, K):
+    """C as it is, [M, N rounded up to 8]; nothing behind it is written"""
+    import torch
+    import paper_2506_06472_amd as tio
+    work = torch.full((tio.tio_op_gemm_fp8_work(M, N, K) + 64,), 255, device="cuda", dtype=torch.uint8)
+    c = torch.full((M + 1, _up(N) + 8), 7.0, device="cuda", dtype=l8.types(dtype))
+    tio.tio_op_gemm_fp8(0, dtype, M, N, K, forms[0], qa.data_ptr(), forms[1], qb.data_ptr(), c.data_ptr(), c.stride(0), work_ptr=work.data_ptr())
+    assert (work[-64:] == 255).all() and (c[:M, _up(N):] == 7.0).all() and (c[M:] == 7.0).all()
+    return c[:M, :_up(N)]
+
+
+def _two_to(e):
+    import torch
+    return torch.exp2(e.double()).float()
+
+
+def _operands(M, N, K, seed):
+    """Whole numbers up to 8, exact in both types, whose largest in a block is 1, 2, 4 or 8 by chance, times powers of two of their row and of their block; the blocks' cancel in the
+    product, so that C[m, n] is a whole number below 2^24 times one of m's and one of n's.  So every block has an exponent of its own, and with a wrong one for any of
+    them the sum is another."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    kb = (K + 127) // 128
+    pick = lambda lo, hi, *shape: torch.randint(lo, hi, shape, device="cuda", generator=g)
+    block = pick(-20, 21, 1, kb)
+    out = []
+    for rows, sign in ((M, 1), (N, -1)):
+        top = _two_to(pick(0, 4, rows, kb)).repeat_interleave(128, 1)[:, :K]
+        v = torch.round((torch.rand((rows, K), device="cuda", generator=g) * 2 - 1) * top)
+        v[:, ::128] = top[:, ::128]
+        v *= _two_to(pick(-20, 21, rows, 1))
+        v *= _two_to(sign * block).repeat_interleave(128, 1)[:, :K]
+        out.append(v)
+    assert K * 64 < 1 << 24
+    return out
+
+
+@pytest.mark.parametrize("forms", PAIRS, ids="-".join)
+@pytest.mark.parametrize("dtype,M,N,K,way", WAYS)
+def test_every_block_has_its_exponent(dtype, M, N, K, way, forms):
+    """Exact, and of blocks that are not finite (one in the first and one in the last row of A, one in a row of B) nothing but their rows and columns is NaN."""
+    import torch
+    import paper_2506_06472_amd as tio
+    assert tio.tio_op_gemm_fp8_route(dtype, M, N, K) == way
+    a, b = _operands(M, N, K, M + N + K)
+    want = (a.double() @ b.double().t()).to(l8.types(dtype))
+    got = _product(_stored(a, forms[0]), _stored(b, forms[1]), forms, dtype, M, N, K)
+    assert torch.equal(got[:, :N], want) and (got[:, N:] == 0).all()
+    bad = torch.zeros((M, N), device="cuda", dtype=torch.bool)
+    a[0, K // 2], a[M - 1, K - 1], b[N // 2, 0] = float("inf"), float("nan"), -float("inf")
+    bad[0] = bad[M - 1] = bad[:, N // 2] = True
+    got = _product(_stored(a, forms[0]), _stored(b, forms[1]), forms, dtype, M, N, K)
+    assert torch.isnan(got[:, :N][bad]).all() and torch.equal(got[:, :N][~bad], want[~bad]) and (got[:, N:] == 0).all()
+
+
+def _values_of(q, form, rows, cols):
+    import torch
+    import paper_2506_06472_amd as tio
+    v = torch.empty((rows, _up(cols)), device="cuda")
+    tio.tio_op_fp8_load(0, "fp32", form, rows, cols, q.data_ptr(), v.data_ptr(), v.stride(0))
+    return v[:, :cols].double()
+
+
+@pytest.mark.parametrize("forms", PAIRS, ids="-".join)
+@pytest.mark.parametrize("dtype,M,N,K", [(d, m, n, k) for d, m, n, k, _ in WAYS if m * n * k < 1 << 35]
+                         + [(d, *s) for d in ("bf16", "fp32") for s in ((257, 300, 100), (512, 520, 1152), (300, 200, 5000))])
+def test_normal_values(dtype, M, N, K, forms):
+    """Rows and columns of different sizes: within a rounding of the result (to the type, of a value that is off by the rest), one of 32 bits for each of K sums and four more, and in
+    bf16 what the matrix cores cut off, of each product in a block of 128 at most 2^-13 of the largest, which is at most the product of the operands' largest."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(K)
+    values = lambda rows: (torch.randn((rows, K), device="cuda", generator=g) * _two_to(torch.randint(-6, 7, (rows, 1), device="cuda", generator=g))
+                           * _two_to(torch.randint(-3, 4, (1, K), device="cuda", generator=g)))
+    q = [_stored(values(rows), form) for rows, form in zip((M, N), forms)]
+    got = _product(*q, forms, dtype, M, N, K)
+    a, b = (_values_of(v, form, rows, K) for v, form, rows in zip(q, forms, (M, N)))
+    want = a @ b.t()
+    err = (K + 4) * l8.E32 * (a.abs() @ b.abs().t())
+    if dtype == "bf16":
+        top = lambda v: torch.nn.functional.pad(v.abs(), (0, -K % 128)).view(len(v), -1, 128).amax(2)
+        err += 128 * 2.0 ** -13 * (top(a) @ top(b).t())
+    off = (got[:, :N].double() - want).abs() - l8.U[dtype] * want.abs() - 1.01 * err
+    assert (off <= 0).all() and (got[:, N:] == 0).all(), off.max()

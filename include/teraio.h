@@ -516,8 +516,10 @@ typedef struct tio_residual_cfg {
 int tio_op_residual_norm(void *stream, int32_t dtype, const tio_residual_cfg *cfg, int64_t rows, int64_t d, int64_t ld, const void *branch, const void *x,
                          const void *gate, int64_t ldg, const void *post_gain, const void *post_bias, const void *gain, const void *bias, void *y, void *h,
                          float *stats);
-/* Gradients from dy (of y where it goes on as the residual) and dh, the same cfg, branch, and the forward pass's y, as it was rounded, and stats.  dgate (where there is a
- * gate) is one row, the sum over the rows, or rows like the gate's; dpost_gain (where there is post_gain), dgain, and of the layer norm dpost_bias and
+/* Gradients from dy (of y where it goes on as the residual) and dh, the same cfg, branch, the forward pass's stats, and one of
+ *   its x, as it was then (tio_op_residual_norm_bwd_from_x): y is made again in 32 bits, as the forward pass had it, and the gradients are those of what it computed;
+ *   its y, as it was rounded (tio_op_residual_norm_bwd), where y took x's place: bf16 gains' gradients are then off by 1.4 times as much (2.4e-3 of their norm, not 1.7e-3).
+ * dgate (where there is a gate) is one row, the sum over the rows, or rows like the gate's; dpost_gain (where there is post_gain), dgain, and of the layer norm dpost_bias and
  * dbias (NULL: not wanted) are rows summed over all rows, in 32 bits and always in the same order.  dx may be dy.  work: device memory of
  * tio_op_residual_norm_bwd_work bytes, contents of no interest before and after, used by one call at a time. */
 int tio_op_residual_norm_bwd_work(int64_t rows, int64_t d, uint64_t *out_bytes);
@@ -525,6 +527,10 @@ int tio_op_residual_norm_bwd(void *stream, int32_t dtype, const tio_residual_cfg
                              const void *gate, int64_t ldg, const void *post_gain, const void *post_bias, const void *gain, const float *stats,
                              const void *dy, const void *dh, void *dx, void *dbranch, void *dgate, void *dpost_gain, void *dpost_bias, void *dgain, void *dbias,
                              void *work);
+int tio_op_residual_norm_bwd_from_x(void *stream, int32_t dtype, const tio_residual_cfg *cfg, int64_t rows, int64_t d, int64_t ld, const void *branch, const void *x,
+                                    const void *gate, int64_t ldg, const void *post_gain, const void *post_bias, const void *gain, const float *stats,
+                                    const void *dy, const void *dh, void *dx, void *dbranch, void *dgate, void *dpost_gain, void *dpost_bias, void *dgain, void *dbias,
+                                    void *work);
 
 /* Rotary positions with several axes (time, height, width) on rows that begin with `heads` heads of dh elements (a multiple of 8, at most
  * 256), say the q and k heads of a packed qkv: x's heads, rotated, in y, which may be x; nothing behind them is touched.  Axis a (1 to 8 of them) has

@@ -116,6 +116,7 @@ _SIGNATURES = {
     "tio_op_fp8_store": "piiillplpp", "tio_op_fp8_load": "piillppl", "tio_op_gemm_fp8": "pilll" "ipip" "pplplp",
     "tio_op_dropout": "pillplplpl" "duu", "tio_op_rope_axes": "pilll" "plplp" "ipfii",
     "tio_op_residual_norm": "piplll" "ppplppppppp", "tio_op_residual_norm_bwd": "piplll" "ppplpppp" "pppppppppp",
+    "tio_op_residual_norm_bwd_from_x": "piplll" "ppplpppp" "pppppppppp",
 }
 
 
@@ -665,6 +666,15 @@ def tio_op_residual_norm_bwd(stream_handle, dtype, cfg, rows, d, ld, branch_ptr,
     rc = lib().tio_op_residual_norm_bwd(stream_handle, PREC[dtype], C.byref(cfg), rows, d, ld, branch_ptr, y_ptr, gate_ptr, ldg, post_gain_ptr,
                                         post_bias_ptr, gain_ptr, stats_ptr, dy_ptr, dh_ptr, dx_ptr, dbranch_ptr, dgate_ptr, dpost_gain_ptr,
                                         dpost_bias_ptr, dgain_ptr, dbias_ptr, work_ptr)
+    if rc:
+        _check(rc)
+
+
+def tio_op_residual_norm_bwd_from_x(stream_handle, dtype, cfg, rows, d, ld, branch_ptr, x_ptr, gate_ptr, ldg, post_gain_ptr, post_bias_ptr, gain_ptr, stats_ptr,
+                                    dy_ptr, dh_ptr, dx_ptr, dbranch_ptr, dgate_ptr, dpost_gain_ptr, dpost_bias_ptr, dgain_ptr, dbias_ptr, work_ptr):
+    rc = lib().tio_op_residual_norm_bwd_from_x(stream_handle, PREC[dtype], C.byref(cfg), rows, d, ld, branch_ptr, x_ptr, gate_ptr, ldg, post_gain_ptr,
+                                               post_bias_ptr, gain_ptr, stats_ptr, dy_ptr, dh_ptr, dx_ptr, dbranch_ptr, dgate_ptr, dpost_gain_ptr,
+                                               dpost_bias_ptr, dgain_ptr, dbias_ptr, work_ptr)
     if rc:
         _check(rc)
 

@@ -165,7 +165,8 @@ struct ResidualArgs {
     const void *branch, *x, *gate, *post_gain, *post_bias, *gain, *bias;     // gate, post_gain, biases: nullptr for none
     void *y, *h;
     float *stats;
-    const void *dy, *dh;                         // the backward pass
+    bool from_x;                                 // the backward pass: y is the forward pass's x
+    const void *dy, *dh;
     void *dx, *dbranch, *dgate, *dpost_gain, *dpost_bias, *dgain, *dbias, *work;
 };
 constexpr int64_t RESIDUAL_WIDEST = 8192;

@@ -10,6 +10,10 @@
 // factor more); and with m = kept ? D : 0 the gradients of gate, post_gain and post_bias are a column's factors of the same two sums over the rows,
 //   S1 = sum of m bh,  S2 = sum of m:   dpost_gain = bs s gate S1,  dpost_bias = bs s gate S2,  dgate = bs s (post_gain S1 + post_bias S2).
 //
+// The backward pass needs y.  From x (from_x) it makes it again in 32 bits, as the forward pass had it when it took its norm: x has as many bytes as y, and the branch and the
+// mask are there anyway.  From y as it was rounded, which is all that is left where y took x's place, vh is off by the rounding, and in bf16 dgain by 2.4e-3 of its norm
+// where its own rounding is 1.7e-3.
+//
 // Bound: HBM; the vector ALU, with about 14 (forward) and 24 operations on an element beside the generator's, is not far behind (8192 x 4096 in bf16: forward
 // 51 us, 5.3 TB/s; backward 70, 5.8, and the sums 6).  A row is W
 // wavefronts', who hold it in registers from its loads to its stores; statistics and sums are in 32 bits, the layer norm's variance from centred values.  A
@@ -43,8 +47,9 @@ __device__ __forceinline__ float wave_total(float v) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// Sums over a row's W wavefronts, in all of their threads.  `red`: LDS of 4 W floats, halves used in turn (one barrier a sum).
-template <int W> struct RowSum {
+// Sums over a row's W wavefronts, in all of their threads.  `red`: LDS of 4 W floats, halves used in turn (one barrier a sum).  AT_ONCE: wavefronts' sums that a thread
+// reads at a time, a register each.
+template <int W, int AT_ONCE = W> struct RowSum {
     float *red;
     int turn = 0;
     __device__ __forceinline__ explicit RowSum(float *r) : red(r) {}
@@ -55,7 +60,7 @@ template <int W> struct RowSum {
         if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = u;
         __syncthreads();
         u = at[0];
-#pragma unroll
+#pragma unroll AT_ONCE
         for (int w = 1; w < W; ++w) u += at[w];
     }
     __device__ __forceinline__ void operator()(float &u, float &v) {
@@ -228,10 +233,11 @@ __global__ void __launch_bounds__(W == 1 ? 256 : W * 64) residual_norm_k(Residua
 
 // The column sums of a workgroup's rows: [kind][workgroup][columns rounded up to 8], kinds dgain, S1, dbias, S2.
 constexpr int KINDS = 4;
-template <typename T, int W, bool RMS, bool POST>
-__global__ void __launch_bounds__(W == 1 ? 256 : W * 64, 4) residual_norm_bwd_k(ResidualArgs a) {
+// FROM_X: a.y is the forward pass's x.  About eight operations more on an element (8192 x 4096 in bf16 with both norms 71 us, from y 72; 2000 x 5120, whose sixteen wavefronts
+// meet for every row, 37, from y 32): its sums are read five at a time there, as all sixteen would be more registers than there are.
+template <typename T, int W, bool RMS, bool POST, bool FROM_X> __device__ __forceinline__ void residual_backward(const ResidualArgs &a) {
     __shared__ float red[4 * W];
-    RowSum<W> sum(red);
+    RowSum<W, FROM_X && W == 16 ? 5 : W> sum(red);
     Columns<T, W, RMS, POST> col(a);
     const void *const gate = a.ldg ? a.gate : nullptr;
     const uint32_t groups = (uint32_t)((a.d + 7) / 8);
@@ -284,7 +290,29 @@ __global__ void __launch_bounds__(W == 1 ? 256 : W * 64, 4) residual_norm_bwd_k(
         Mask8 m;
         if (a.drop.limit) m.draw(row, groups, col.lane, a.drop);
         float r[8], g[8], D[8], v[8], t = 0.f, u = 0.f;
-        col.get(r, raw[0]);
+        if constexpr (!FROM_X) col.get(r, raw[0]);
+        else {                                                 // y as the forward pass had it: from x, before its rounding
+            if (!AHEAD) {                                      // once more below, from the caches
+                row_load(raw[3], col.row(a.branch, at), col.col);
+                row_load(raw[4], col.row_or_none(gate, row * a.ldg), col.col);
+            }
+            raw[0].get(r);
+            raw[3].get(v);
+            raw[4].get(g);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float n = POST ? (v[j] - (RMS ? 0.f : st.x)) * st.y * col.w[j] : v[j] * col.w[j];
+                if (MOVED) n += reinterpret_cast<const float *>(&moved[j >> 2 & MOVED][threadIdx.x])[j & 3];
+                if (gate) n *= g[j];
+                if (a.drop.limit) n = m.kept(j, a.drop) ? n : 0.f;
+                r[j] = a.resid_scale * r[j] + n;
+                asm volatile("" : "+v"(r[j]));                 // one element after the other: there are no registers for all at once,
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            raw[3].forget();                                   // and none to keep what is found again below
+            m.forget();
+            if (col.ragged) cut8(r, col.n);
+        }
         col.get(g, raw[1]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -372,6 +400,12 @@ __global__ void __launch_bounds__(W == 1 ? 256 : W * 64, 4) residual_norm_bwd_k(
     if (sum1) out(1, s1);
     if (!RMS) out(2, s_bias);
     if (POST && !RMS) out(3, s2);
+}
+template <typename T, int W, bool RMS, bool POST> __global__ void __launch_bounds__(W == 1 ? 256 : W * 64, 4) residual_norm_bwd_k(ResidualArgs a) {
+    residual_backward<T, W, RMS, POST, false>(a);
+}
+template <typename T, int W, bool RMS, bool POST> __global__ void __launch_bounds__(W == 1 ? 256 : W * 64, 4) residual_norm_bwd_x_k(ResidualArgs a) {
+    residual_backward<T, W, RMS, POST, true>(a);
 }
 
 // A workgroup adds 16 columns, four wavefronts a kind: the workgroups' shares in their order within each of 64 slices, the slices in theirs.  Neighbouring
@@ -462,7 +496,8 @@ void residual_norm(hipStream_t s, int dtype, const ResidualArgs &a) {
 
 void residual_norm_bwd(hipStream_t s, int dtype, const ResidualArgs &a) {
     const unsigned grid = (unsigned)backward_groups(a.rows, a.d), columns = (unsigned)((a.d + 127) / 128 * 8);
-    TIO_BY_WIDTH(residual_norm_bwd_k);
+    if (a.from_x) TIO_BY_WIDTH(residual_norm_bwd_x_k);
+    else TIO_BY_WIDTH(residual_norm_bwd_k);
     if (dtype == TIO_PREC_BF16) residual_sums_k<bf16_t><<<columns, 256 * KINDS, 0, s>>>(a, grid);
     else residual_sums_k<float><<<columns, 256 * KINDS, 0, s>>>(a, grid);
 }

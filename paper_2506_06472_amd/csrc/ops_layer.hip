@@ -59,6 +59,33 @@ bool residual_of(const tio_residual_cfg &c, k::ResidualArgs &a) {
     return make_dropout(c.p, c.seed, c.offset, a.drop);
 }
 
+// the backward pass, from y or (from_x) from the forward pass's x in its place
+int residual_backward(void *stream, int32_t dtype, const tio_residual_cfg *cfg, int64_t rows, int64_t d, int64_t ld, const void *branch, bool from_x, const void *y,
+                      const void *gate, int64_t ldg, const void *post_gain, const void *post_bias, const void *gain, const float *stats,
+                      const void *dy, const void *dh, void *dx, void *dbranch, void *dgate, void *dpost_gain, void *dpost_bias, void *dgain, void *dbias,
+                      void *work) {
+    TIO_OP_BEGIN
+    if (!branch || !y || !stats || !dy || !dh || !dx || !dbranch || !dgain || !work) return fail(TIO_ERR_INVALID_ARG, "null argument");
+    if (const char *wrong = residual_args(dtype, cfg, rows, d, ld, gate, ldg, post_gain, post_bias, gain)) return fail(TIO_ERR_INVALID_ARG, wrong);
+    if (cfg->rms && (post_bias || dpost_bias || dbias)) return fail(TIO_ERR_INVALID_ARG, "the root-mean-square norm has no bias");
+    if (!gate != !dgate || !post_gain != !dpost_gain || (dpost_bias && !post_gain))
+        return fail(TIO_ERR_INVALID_ARG, "a gradient is given exactly where its operand is");
+    if (!aligned(branch) || !aligned(y) || !aligned(stats) || !aligned(dy) || !aligned(dh) || !aligned(dx) || !aligned(dbranch) || !aligned(dgate) ||
+        !aligned(dpost_gain) || !aligned(dpost_bias) || !aligned(dgain) || !aligned(dbias) || !aligned(work))
+        return fail(TIO_ERR_INVALID_ARG, BAD_POINTER);
+    k::ResidualArgs a = {};
+    if (!residual_of(*cfg, a)) return fail(TIO_ERR_INVALID_ARG, BAD_PROBABILITY);
+    a.rows = rows; a.d = d; a.ld = ld; a.ldg = ldg;
+    a.branch = branch; a.gate = gate; a.post_gain = post_gain; a.post_bias = post_bias; a.gain = gain;
+    a.from_x = from_x; a.y = const_cast<void *>(y); a.stats = const_cast<float *>(stats);
+    a.dy = dy; a.dh = dh; a.dx = dx; a.dbranch = dbranch; a.dgate = dgate; a.dpost_gain = dpost_gain; a.dpost_bias = dpost_bias;
+    a.dgain = dgain; a.dbias = dbias; a.work = work;
+    const OnDeviceOf device((hipStream_t)stream);
+    k::residual_norm_bwd((hipStream_t)stream, dtype, a);
+    return launched();
+    TIO_OP_END
+}
+
 }  // namespace
 
 extern "C" {
@@ -164,26 +191,16 @@ int tio_op_residual_norm_bwd(void *stream, int32_t dtype, const tio_residual_cfg
                              const void *gate, int64_t ldg, const void *post_gain, const void *post_bias, const void *gain, const float *stats,
                              const void *dy, const void *dh, void *dx, void *dbranch, void *dgate, void *dpost_gain, void *dpost_bias, void *dgain, void *dbias,
                              void *work) {
-    TIO_OP_BEGIN
-    if (!branch || !y || !stats || !dy || !dh || !dx || !dbranch || !dgain || !work) return fail(TIO_ERR_INVALID_ARG, "null argument");
-    if (const char *wrong = residual_args(dtype, cfg, rows, d, ld, gate, ldg, post_gain, post_bias, gain)) return fail(TIO_ERR_INVALID_ARG, wrong);
-    if (cfg->rms && (post_bias || dpost_bias || dbias)) return fail(TIO_ERR_INVALID_ARG, "the root-mean-square norm has no bias");
-    if (!gate != !dgate || !post_gain != !dpost_gain || (dpost_bias && !post_gain))
-        return fail(TIO_ERR_INVALID_ARG, "a gradient is given exactly where its operand is");
-    if (!aligned(branch) || !aligned(y) || !aligned(stats) || !aligned(dy) || !aligned(dh) || !aligned(dx) || !aligned(dbranch) || !aligned(dgate) ||
-        !aligned(dpost_gain) || !aligned(dpost_bias) || !aligned(dgain) || !aligned(dbias) || !aligned(work))
-        return fail(TIO_ERR_INVALID_ARG, BAD_POINTER);
-    k::ResidualArgs a = {};
-    if (!residual_of(*cfg, a)) return fail(TIO_ERR_INVALID_ARG, BAD_PROBABILITY);
-    a.rows = rows; a.d = d; a.ld = ld; a.ldg = ldg;
-    a.branch = branch; a.gate = gate; a.post_gain = post_gain; a.post_bias = post_bias; a.gain = gain;
-    a.y = const_cast<void *>(y); a.stats = const_cast<float *>(stats);
-    a.dy = dy; a.dh = dh; a.dx = dx; a.dbranch = dbranch; a.dgate = dgate; a.dpost_gain = dpost_gain; a.dpost_bias = dpost_bias;
-    a.dgain = dgain; a.dbias = dbias; a.work = work;
-    const OnDeviceOf device((hipStream_t)stream);
-    k::residual_norm_bwd((hipStream_t)stream, dtype, a);
-    return launched();
-    TIO_OP_END
+    return residual_backward(stream, dtype, cfg, rows, d, ld, branch, false, y, gate, ldg, post_gain, post_bias, gain, stats, dy, dh, dx, dbranch, dgate, dpost_gain, dpost_bias,
+                             dgain, dbias, work);
+}
+
+int tio_op_residual_norm_bwd_from_x(void *stream, int32_t dtype, const tio_residual_cfg *cfg, int64_t rows, int64_t d, int64_t ld, const void *branch, const void *x,
+                                    const void *gate, int64_t ldg, const void *post_gain, const void *post_bias, const void *gain, const float *stats,
+                                    const void *dy, const void *dh, void *dx, void *dbranch, void *dgate, void *dpost_gain, void *dpost_bias, void *dgain, void *dbias,
+                                    void *work) {
+    return residual_backward(stream, dtype, cfg, rows, d, ld, branch, true, x, gate, ldg, post_gain, post_bias, gain, stats, dy, dh, dx, dbranch, dgate, dpost_gain, dpost_bias,
+                             dgain, dbias, work);
 }
 
 int tio_op_dropout(void *stream, int32_t dtype, int64_t rows, int64_t cols, const void *x, int64_t ldx, const void *resid, int64_t ldr, void *y, int64_t ldy,

@@ -31,6 +31,8 @@ __device__ __forceinline__ uint4 philox(uint64_t index, const Dropout &d) {
 struct Mask8 {
     uint4 w;
     __device__ __forceinline__ void draw(uint64_t row, uint32_t groups, uint32_t group, const Dropout &d) { w = philox(row * groups + group, d); }
+    // what the compiler has found from it it finds again, rather than keep it in registers
+    __device__ __forceinline__ void forget() { asm volatile("" : "+v"(w.x), "+v"(w.y), "+v"(w.z), "+v"(w.w)); }
     __device__ __forceinline__ bool kept(int j, const Dropout &d) const {
         const uint32_t v = j < 2 ? w.x : j < 4 ? w.y : j < 6 ? w.z : w.w;
         return (j & 1 ? v >> 16 : v & 0xffffu) >= d.limit;

@@ -14,6 +14,8 @@ template <> struct Row8<bf16_t> {
     __device__ __forceinline__ void put(bf16_t *p) const { __builtin_nontemporal_store(__builtin_bit_cast(tio_u32x4, v.raw), reinterpret_cast<tio_u32x4 *>(p)); }
     __device__ __forceinline__ void get(float *f) const { v.get(f); }
     __device__ __forceinline__ void set(const float *f) { v.set(f); }
+    // what the compiler has found from them it finds again, rather than keep it in registers
+    __device__ __forceinline__ void forget() { asm volatile("" : "+v"(v.raw.x), "+v"(v.raw.y), "+v"(v.raw.z), "+v"(v.raw.w)); }
 };
 template <> struct Row8<float> {
     Vec16<float> lo, hi;
@@ -26,6 +28,7 @@ template <> struct Row8<float> {
     }
     __device__ __forceinline__ void get(float *f) const { lo.get(f); hi.get(f + 4); }
     __device__ __forceinline__ void set(const float *f) { lo.set(f); hi.set(f + 4); }
+    __device__ __forceinline__ void forget() {}
 };
 // through a buffer descriptor over a row: columns past its end read as zeros, and are not written; stores go past the caches
 __device__ __forceinline__ void row_load(Row8<bf16_t> &v, __amdgpu_buffer_rsrc_t row, uint32_t col) { buffer_load16(v.v, row, col * 2); }

@@ -457,9 +457,9 @@ def _own_residual(s, c, tio, stream, at):
                              at("bias"), at("y"), at("h"), at("stats"))
     out = {"y": s["y"][:, :d], "h": s["h"][:, :d]}
     if c["train"]:
-        tio.tio_op_residual_norm_bwd(stream, dt, s["cfg"], R, d, ld, at("branch"), at("y"), at("gate"), ldg, at("post_gain"), at("post_bias"),
-                                     at("gain"), at("stats"), at("dy"), at("dh"), at("dx"), at("dbranch"), at("dgate"), at("dpost_gain"),
-                                     at("dpost_bias"), at("dgain"), at("dbias"), at("work"))
+        tio.tio_op_residual_norm_bwd_from_x(stream, dt, s["cfg"], R, d, ld, at("branch"), at("x"), at("gate"), ldg, at("post_gain"), at("post_bias"),
+                                            at("gain"), at("stats"), at("dy"), at("dh"), at("dx"), at("dbranch"), at("dgate"), at("dpost_gain"),
+                                            at("dpost_bias"), at("dgain"), at("dbias"), at("work"))
         for n in ("x", "branch", "gate", "post_gain", "post_bias", "gain", "bias"):
             if n in s:
                 t = s["d" + n][:, :d]

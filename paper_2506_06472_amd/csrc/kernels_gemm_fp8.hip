@@ -2,7 +2,7 @@
 // C[M,N] = A[M,K] . B[N,K]^T (+ bias[N]) (+ resid[M,N]).
 //
 // bf16 results: v_mfma_scale_f32_16x16x128_f8f6f4, one instruction for a block of 128 of 16 rows and 16 columns, which applies both operands' powers of two
-// itself.  Measured on it: the accumulator is exact to 24 bits, but within a group of neighbouring products those more than 13 bits below the largest are cut off:
+// itself.  Measured on it: the accumulator is exact to 24 bits, but of the products of eight neighbours the bits below 2^-13 of the largest are cut off:
 // errors of 1.2e-5 of the result's norm on normal values, a hundredth of what the rounding to bf16 leaves.  fp32 results need more, so there the codes
 // become bf16 numbers, exactly, whose products and sums are those of 32 bits (error 4e-8).
 //

@@ -109,3 +109,28 @@ def test_normal_values(dtype, M, N, K, forms):
         err += 128 * 2.0 ** -13 * (top(a) @ top(b).t())
     off = (got[:, :N].double() - want).abs() - l8.U[dtype] * want.abs() - 1.01 * err
     assert (off <= 0).all() and (got[:, N:] == 0).all(), off.max()
+
+
+# one product of each kernel that hands 8-bit numbers to the matrix cores: the two smallest tiles from the caches, 64 x 128, 128 x 128 four and two deep, 256 x 256
+CUT = [(9, 700, 1000), (70, 1101, 9000), (4100, 770, 700), (1000, 4000, 4000), (8000, 750, 780), (4000, 4100, 1000)]
+
+
+@pytest.mark.parametrize("forms", [("e4m3", "e4m3"), ("e5m2", "e4m3")], ids="-".join)
+@pytest.mark.parametrize("M,N,K", CUT)
+def test_what_the_matrix_cores_cut_off(M, N, K, forms):
+    """bf16 results: of the products of eight neighbours the bits below 2^-13 of the largest, so at most 7 2^-13 of it, less than a quarter of the type's half step for products of one
+    sign.  In blocks of 0 and 2 one large number among others 2^-10 to 2^-17 of it; the large numbers of block 2 take those of block 0 away, so that nothing else
+    is left to see."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(M)
+    pick = lambda lo, hi, *shape: torch.randint(lo, hi, shape, device="cuda", generator=g)
+    a, b = torch.zeros((M, K), device="cuda"), torch.ones((N, K), device="cuda")
+    for start, sign in ((0, 1.0), (256, -1.0)):
+        n = min(128, K - start)
+        a[:, start:start + n] = _two_to(8 - pick(10, 18, M, n))
+        a[torch.arange(M, device="cuda"), start + pick(0, n, M)] = 256.0 * sign
+    got = _product(_stored(a, forms[0]), _stored(b, forms[1]), forms, "bf16", M, N, K)[:, :N].double()
+    assert torch.equal(_values_of(_stored(a, forms[0]), forms[0], M, K), a.double())
+    want = a.double() @ b.double().t()
+    eight = torch.nn.functional.pad(a.abs(), (0, -K % 8)).view(M, -1, 8).amax(2).double().sum(1, keepdim=True)
+    assert ((got - want).abs() <= l8.U["bf16"] * want.abs() + 1.01 * (7 * 2.0 ** -13 * eight + (K + 4) * l8.E32 * a.abs().double().sum(1, keepdim=True))).all()

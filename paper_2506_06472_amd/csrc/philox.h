@@ -27,7 +27,7 @@ __device__ __forceinline__ uint4 philox(uint64_t index, const Dropout &d) {
     return make_uint4(c0, c1, c2, c3);
 }
 
-// the masks of eight neighbours: 0 or the scale
+// the random bits of eight neighbours, sixteen each
 struct Mask8 {
     uint4 w;
     __device__ __forceinline__ void draw(uint64_t row, uint32_t groups, uint32_t group, const Dropout &d) { w = philox(row * groups + group, d); }

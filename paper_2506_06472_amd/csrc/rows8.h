@@ -8,7 +8,6 @@ namespace k {
 template <typename T> struct Row8;
 template <> struct Row8<bf16_t> {
     Vec16<bf16_t> v;
-    __device__ __forceinline__ void clear() { v.raw = make_uint4(0, 0, 0, 0); }
     __device__ __forceinline__ void load(const bf16_t *p) { v.load(p); }
     __device__ __forceinline__ void store(bf16_t *p) const { v.store(p); }
     __device__ __forceinline__ void put(bf16_t *p) const { __builtin_nontemporal_store(__builtin_bit_cast(tio_u32x4, v.raw), reinterpret_cast<tio_u32x4 *>(p)); }
@@ -19,7 +18,6 @@ template <> struct Row8<bf16_t> {
 };
 template <> struct Row8<float> {
     Vec16<float> lo, hi;
-    __device__ __forceinline__ void clear() { lo.raw = hi.raw = make_float4(0.f, 0.f, 0.f, 0.f); }
     __device__ __forceinline__ void load(const float *p) { lo.load(p); hi.load(p + 4); }
     __device__ __forceinline__ void store(float *p) const { lo.store(p); hi.store(p + 4); }
     __device__ __forceinline__ void put(float *p) const {                    // past the caches

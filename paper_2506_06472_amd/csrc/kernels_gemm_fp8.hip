@@ -6,8 +6,9 @@
 // errors of 1.2e-5 of the result's norm on normal values, a hundredth of what the rounding to bf16 leaves.  fp32 results need more, so there the codes
 // become bf16 numbers, exactly, whose products and sums are those of 32 bits (error 4e-8).
 //
-// Bound, large products: the power limit with operands in the caches (8192^3 355 us, 3.1 PFLOP/s at 2.0 GHz; zeros 3.4; the instruction alone 4.0), memory
-// without (390 us; 8192 x 11008 x 4096 297 us, 259 without its stores, which nothing overlaps; a large library product of plain 8-bit matrices 2.1 to 2.7).
+// Bound, large products: the power limit with operands in the caches (8192^3 350 us, 3.1 PFLOP/s at 2.0 GHz; zeros 3.4; the instruction alone 4.0; 8192 x 11008 x 4096
+// 278 us), memory without (400 and 306 us, 2.7 and 2.4 PFLOP/s, of the latter some 40 us its stores, which nothing overlaps; a large library product of plain 8-bit matrices
+// 2.1 to 2.7).  A bias or residual takes the way out in 32 bits (8192 x 4096 x 4096 109 us, with both 162, of which 13 are the residual's bytes).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -91,7 +92,8 @@ __global__ void __launch_bounds__(NW * 64) gemm_fp8_direct_k(const uint8_t *__re
         eb[j] = B + sb.code_bytes() + (g >> 2) * KB * 64 + (g & 3);
     }
     // U blocks' loads before the first one's products: one after the other a wavefront waits for each (16 x 4096 x 11008, operands in no cache: 16.6 us, with
-    // eight wavefronts of four at once 11.2); larger tiles have as many loads in one block
+    // eight wavefronts of four at once 11.2); larger tiles have as many bytes on their way for one block.  None are while a wavefront multiplies: others cover that,
+    // or nothing does (64 x 4096 x 11008 16.4 us, of which the matrix from HBM is 8.8)
     constexpr int U = TM * TN > 2 ? 1 : TM * TN == 2 ? (sizeof(T) == 2 ? 4 : 2) : NW == 8 ? 4 : 2;
     for (int64_t kb = wave; kb < KB; kb += NW * U) {
         Piece8 a[U][TM], b[U][TN];
@@ -494,8 +496,9 @@ __global__ void __launch_bounds__(256)
 using StripLoads = Loads<2, 4, 3, true>;
 
 // Tiles of 64 x 128 for products of some hundred rows or columns, which have too few tiles of 128 x 128 for all compute units (512 x 4096 x 11008 50 -> 39 us,
-// 128 x 11008 x 4096 23 -> 18.8): each wavefront has all rows and 32 columns.  A step's fragments are read into a second set of registers while the products of the
-// one before run, as above, in the compiler's order; two workgroups to a compute unit cover each other's waits (six steps deep and one to a unit: 40 and 20).
+// 128 x 11008 x 4096 23 -> 18.8): each wavefront has all rows and 32 columns.  A step's fragments have a second set of registers, but the compiler
+// puts their reads behind most or all products of the step before: it is two workgroups to a compute unit that cover each other's waits (six steps deep and one to a
+// unit: 40 and 20 us).
 template <int FA, int FB>
 __global__ void __launch_bounds__(256, 2)
     gemm_fp8_strip_k(const uint8_t *__restrict__ A, const uint8_t *__restrict__ B, const bf16_t *__restrict__ bias, const bf16_t *resid, int64_t ldr, bf16_t *C, int64_t ldc,
@@ -624,7 +627,7 @@ __global__ void __launch_bounds__(256, 2)
 // The least of an estimate of the time.  The large tiles' constants were fitted to 39 products, each taken in all ways: a workgroup's steps and its beginning and
 // end (us), times the rounds of workgroups, and the sums of the ranges.  A step of a 128 tile is mostly waiting for loads where a compute unit has one
 // such tile: 0.32 us four steps deep (0.44 where all units work), two deep 0.6, but two tiles to a unit share 0.88.  us, 768 x 768 x 8192 in one range: 26.9 four
-// deep, 41.4 two deep, 69.8 in 256 tiles, and 19.1 in three ranges; 8192 x 768 x 768: 13.3, 10.8, 15.5; 8192 x 11008 x 4096: 377, 328, 285.  The small ones' were
+// deep, 41.4 two deep, 69.8 in 256 tiles, and 19.1 in three ranges; 8192 x 768 x 768: 13.3, 10.8, 15.5; 8192 x 11008 x 4096: 380, 330, 288 (all with operands in the caches; without 455, 379, 323).  The small ones' were
 // fitted to 380 products with B in no cache, so that the choice is 1.6 % behind the best way on average (7 % with tiles of 16 x 16 and 32 x 32 by four wavefronts
 // alone): the larger of a wavefront's chain of steps, in rounds of workgroups, and the bytes from the caches.  us, bf16: 32 x 4096 x 11008: 18.4 in 32 x 32 by
 // four wavefronts, in 32 x 16 by eight 13.9, in 16 x 16 16.0; 64 x 4096 x 11008: 18.2 in 32 x 32 by four, by eight 16.4; 256 x 4096 x 4096: 21.7 in 128 x 128,

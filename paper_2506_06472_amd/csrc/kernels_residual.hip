@@ -15,7 +15,7 @@
 // where its own rounding is 1.7e-3.
 //
 // Bound: HBM; the vector ALU, with about 14 (forward) and 24 operations on an element beside the generator's, is not far behind (8192 x 4096 in bf16: forward
-// 51 us, 5.3 TB/s; backward 70, 5.8, and the sums 6).  A row is W
+// 52 us, 5.2 TB/s; backward 65, 6.2, partly from the memory-side cache, and the sums 6).  A row is W
 // wavefronts', who hold it in registers from its loads to its stores; statistics and sums are in 32 bits, the layer norm's variance from centred values.  A
 // workgroup takes rows one after the other and keeps its share of the column sums in registers; a second launch adds the workgroups' shares in their
 // order, so that results do not depend on timing.
@@ -233,8 +233,8 @@ __global__ void __launch_bounds__(W == 1 ? 256 : W * 64) residual_norm_k(Residua
 
 // The column sums of a workgroup's rows: [kind][workgroup][columns rounded up to 8], kinds dgain, S1, dbias, S2.
 constexpr int KINDS = 4;
-// FROM_X: a.y is the forward pass's x.  About eight operations more on an element (8192 x 4096 in bf16 with both norms 71 us, from y 72; 2000 x 5120, whose sixteen wavefronts
-// meet for every row, 37, from y 32): its sums are read five at a time there, as all sixteen would be more registers than there are.
+// FROM_X: a.y is the forward pass's x.  About eight operations more on an element (with the sums, bf16: 8192 x 4096 with both norms 71 us, from y 72; 2000 x 5120, whose sixteen
+// wavefronts meet for every row, 37, from y 32): its sums are read five at a time there, as all sixteen would be more registers than there are.
 template <typename T, int W, bool RMS, bool POST, bool FROM_X> __device__ __forceinline__ void residual_backward(const ResidualArgs &a) {
     __shared__ float red[4 * W];
     RowSum<W, FROM_X && W == 16 ? 5 : W> sum(red);

@@ -222,6 +222,7 @@ __global__ void __launch_bounds__(W == 1 ? 256 : W * 64) residual_norm_k(Residua
             if (a.drop.limit) t = m.kept(j, a.drop) ? t : 0.f;
             v[j] = a.resid_scale * r[j] + t;
         }
+        cut8(v, col.n);                                        // where no columns are, a mean or 1 / sqrt that is large or no number left more than zeros
         col.put(a.y, row * a.ld, v);
         stats_of<RMS, W>(v, col.n, inv_d, a.eps, sum, mean, rstd);
         if (col.lane == 0) *reinterpret_cast<float2 *>(a.stats + row * 4 + 2) = make_float2(mean, rstd);
@@ -311,7 +312,7 @@ template <typename T, int W, bool RMS, bool POST, bool FROM_X> __device__ __forc
             }
             raw[3].forget();                                   // and none to keep what is found again below
             m.forget();
-            if (col.ragged) cut8(r, col.n);
+            cut8(r, col.n);
         }
         col.get(g, raw[1]);
 #pragma unroll

@@ -520,6 +520,7 @@ int tio_op_residual_norm(void *stream, int32_t dtype, const tio_residual_cfg *cf
 /* Gradients from dy (of y where it goes on as the residual) and dh, the same cfg, branch, the forward pass's stats, and one of
  *   its x, as it was then (tio_op_residual_norm_bwd_from_x): y is made again in 32 bits, as the forward pass had it, and the gradients are those of what it computed;
  *   its y, as it was rounded (tio_op_residual_norm_bwd), where y took x's place: bf16 gains' gradients are then off by 1.4 times as much (2.4e-3 of their norm, not 1.7e-3).
+ * A dropped element of the branch counts for nothing in the gradients of gate, gain and bias, whatever it was.
  * dgate (where there is a gate) is one row, the sum over the rows, or rows like the gate's; dpost_gain (where there is post_gain), dgain, and of the layer norm dpost_bias and
  * dbias (NULL: not wanted) are rows summed over all rows, in 32 bits and always in the same order.  dx may be dy.  work: device memory of
  * tio_op_residual_norm_bwd_work bytes, contents of no interest before and after, used by one call at a time. */

@@ -342,11 +342,15 @@ template <typename T, int W, bool RMS, bool POST, bool FROM_X> __device__ __forc
         }
         col.put(a.dx, at, r);
         col.get(v, raw[3]);
+        const bool finite = POST && st.y > 0.f && st.y < __builtin_inff();          // else what is dropped is not a number, perhaps
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            if (a.drop.limit) D[j] = m.kept(j, a.drop) ? D[j] : 0.f;
             if (POST) v[j] = RMS ? v[j] * st.y : j < col.n ? (v[j] - st.x) * st.y : 0.f;
-            else if (a.drop.limit) v[j] = m.kept(j, a.drop) ? v[j] : 0.f;            // not a number, perhaps
+            if (a.drop.limit) {
+                const bool kept = m.kept(j, a.drop);
+                D[j] = kept ? D[j] : 0.f;
+                v[j] = kept || finite ? v[j] : 0.f;
+            }
         }
         if (gate) {
             col.get(g, raw[4]);
